@@ -127,6 +127,61 @@ void hb_destroy_layer(hb_layer* layer);
 hb_status hb_append_kv(hb_layer* layer, const int32_t* block_table, int32_t n_blocks,
                        int32_t context_len, int32_t n_tokens, const void* k, const void* v);
 
+/* Copy whole blocks of the layer's pool, K and V of every kv head: block dst[i]
+ * takes the contents of block src[i]. Pages of a cache move this way when a
+ * sequence is forked (the two share their full blocks through their block
+ * tables, and the fork gets a copy of the last, partly filled one before either
+ * appends to it) and when a pool is compacted (hb_plan_compaction).
+ *   src, dst  host int32 [n] block ids. A source may occur more than once; a
+ *             destination occurs once and is no copy's source, so the copies
+ *             have no order among themselves.
+ * Enqueues on the layer's stream and returns. Every other byte of the pool is
+ * left untouched. Errors: HB_ERR_INVALID (null pointer, n < 0, a destination
+ * that occurs again), HB_ERR_RANGE (an id outside [0, num_blocks)), HB_ERR_OOM,
+ * HB_ERR_HIP (among others: the layer's stream is under graph capture).
+ * n == 0 is a no-op. */
+hb_status hb_copy_blocks(hb_layer* layer, const int32_t* src, const int32_t* dst, int32_t n);
+
+/* Plan a compaction: with n_used blocks named by any of the tables, every named
+ * block at or above n_used is to move to an id below it that no table names,
+ * both in ascending order. A block that several tables (or several entries of
+ * one) share moves once. Afterwards the tables name blocks of [0, n_used) alone
+ * and the rest of the pool is free.
+ *   tables    host [n_tables] block tables, host int32 [n_blocks[t]] each,
+ *             rewritten in place; entries -1 (a page given back, see
+ *             hb_window_dead_blocks) stay
+ *   src, dst  host int32 [num_blocks / 2] receive the *n_moves moves, for
+ *             hb_copy_blocks / hb_copy_model_blocks
+ * The caller enqueues the copies on the stream of whatever reads the blocks
+ * before it uses the rewritten tables. Host only. Errors, with nothing written:
+ * HB_ERR_INVALID (null pointer, num_blocks < 1, n_tables < 0, a negative table
+ * length), HB_ERR_RANGE (an entry outside [-1, num_blocks)), HB_ERR_OOM. */
+hb_status hb_plan_compaction(int32_t num_blocks, int32_t* const* tables, const int32_t* n_blocks, int32_t n_tables,
+                             int32_t* src, int32_t* dst, int32_t* n_moves, int32_t* n_used);
+
+/* Sliding-window attention with sinks: the row at position p attends to the
+ * keys j <= p with j > p - window (the last `window` positions, its own among
+ * them) or j < sinks (the first tokens stay visible). window == 0, the state
+ * after creation: every j <= p, and `sinks` says nothing. Holds for the layer's
+ * later iterations, profiles among them (hb_latency_features keeps counting
+ * every cached token: it does not know a layer's window). The window bounds
+ * what an iteration reads, and the blocks that it hides from every row of a
+ * request need not be there any more (hb_window_dead_blocks). Each layer of a
+ * model has its own window (hb_model_layer). Key and value slots that no row of
+ * a request sees may hold any bits; those that some row sees must be finite.
+ * Errors: HB_ERR_INVALID (null layer, a value outside [0, 2^30]). */
+hb_status hb_set_attention_window(hb_layer* layer, int32_t window, int32_t sinks);
+
+/* The entries [*first, *first + *count) of a request's block table that no row
+ * at a position >= context_len sees through the window: blocks past the sinks'
+ * last one whose every key lies at or before context_len - window. Their
+ * blocks may be given to others, and the entries hold anything (-1, say) in
+ * calls under that window (every layer of a model must have such a window)
+ * whose context_len is not smaller. Host only.
+ * Errors: HB_ERR_INVALID (null pointer, context_len < 0, window or sinks
+ * outside [0, 2^30]). */
+hb_status hb_window_dead_blocks(int32_t context_len, int32_t window, int32_t sinks, int32_t* first, int32_t* count);
+
 /* One request of a hybrid batch (Section 3.1, step 5). A decode has
  * chunk_len == 1; a prefill chunk has chunk_len >= 1 new prompt tokens.
  *   context_len  tokens of this request already in the cache; the new tokens
@@ -184,8 +239,65 @@ hb_status hb_run_iteration(hb_layer* layer, const hb_batch_desc* desc);
  * enqueued then). */
 hb_status hb_run_iteration_noalloc(hb_layer* layer, const hb_batch_desc* desc);
 
+/* Attention over the paged cache on its own, for programs that compute the rest
+ * of the layer themselves: o_h = softmax(q_h K^T / sqrt(head_dim)) V for every
+ * query row and head, K and V read from a pool in the layouts above, keys
+ * visible as in hb_run_iteration or under a sliding window with sinks
+ * (hb_set_attention_window). Softmax statistics and sums are fp32; the
+ * probabilities enter the product with V as bf16.
+ *
+ * A handle holds the plan of one batch, which every layer's call runs: an
+ * iteration plans once and calls hb_run_attention per layer, each with its own
+ * pool. A handle serves one stream; work on another stream needs another
+ * handle. It is used from one host thread at a time. */
+typedef struct hb_attention hb_attention; /* opaque, library-owned */
+
+/* Create a handle for batches of up to max_batch_tokens rows and max_requests
+ * requests over pools of num_blocks blocks, on a HIP stream of the current
+ * device (hipStream_t; NULL selects the null stream). Of the configuration only
+ * the heads, head_dim, kv_block_size and the two limits matter; the whole of it
+ * is checked. Errors: HB_ERR_INVALID (null pointer, num_blocks < 1),
+ * HB_ERR_UNSUPPORTED (configuration outside the limits), HB_ERR_OOM, HB_ERR_HIP.
+ * On error *out is set to NULL. */
+hb_status hb_create_attention(const hb_layer_config* cfg, int32_t num_blocks, void* hip_stream, hb_attention** out);
+
+/* Free the handle (after synchronising its stream). NULL is a no-op. */
+void hb_destroy_attention(hb_attention* attention);
+
+/* Plan a batch: `requests` as for hb_run_iteration (host tables, copied during
+ * the call), their new tokens' keys and values already in the cache
+ * (hb_append_kv) when a run reads them. Table entries that the window hides from
+ * every row of their request are not looked at. Replaces the plan before it;
+ * runs enqueued earlier keep theirs. Allocates device memory only where a plan
+ * needs more than every one before it. n_requests == 0 plans nothing: runs are
+ * no-ops.
+ * Errors: HB_ERR_INVALID and HB_ERR_RANGE as hb_validate_batch for the requests,
+ * and a window or sinks outside [0, 2^30] (the plan before stays); HB_ERR_OOM,
+ * HB_ERR_HIP (the handle holds no plan afterwards, except that a stream under
+ * graph capture, which is refused, leaves the plan before). */
+hb_status hb_plan_attention(hb_attention* attention, int32_t n_requests, const hb_request* requests, int32_t window,
+                            int32_t sinks);
+
+/* Run the planned batch. Enqueues on the handle's stream and returns; allocates
+ * nothing.
+ *   pool        the pool the plan's tables name blocks of: at least the
+ *               handle's num_blocks, each pointer 16-byte aligned
+ *   q           device bf16 [T] rows of n_q_heads * head_dim values, the
+ *               requests' new tokens in plan order, rotated; rows q_stride
+ *               elements apart (a multiple of 8: a slice of a fused QKV output
+ *               will do), 16-byte aligned
+ *   out         device bf16 [T] rows likewise, out_stride elements apart; what
+ *               lies between the rows is left untouched. The memory from the
+ *               first to the last row must not overlap that of q
+ * Errors: HB_ERR_INVALID (null pointer, no plan, a pool of fewer blocks, a
+ * stride below n_q_heads * head_dim or not a multiple of 8, misaligned pointer,
+ * overlap), HB_ERR_HIP (among others: the stream is under graph capture). */
+hb_status hb_run_attention(hb_attention* attention, const hb_kv_pool* pool, const void* q, int64_t q_stride,
+                           void* out, int64_t out_stride);
+
 /* Check a batch against a layer configuration and pool size without touching
- * any device (no HIP call). Errors: HB_ERR_INVALID (null pointer,
+ * any device (no HIP call). The check knows no window: a table entry that only
+ * a window makes unnecessary is out of range here. Errors: HB_ERR_INVALID (null pointer,
  * chunk_len < 1, context_len < 0, short block table, T > max_batch_tokens,
  * n_requests > max_requests or < 0, bad out_dtype, overlapping x_in/x_out,
  * two requests writing one slot), HB_ERR_RANGE (a used block id outside
@@ -342,6 +454,10 @@ void hb_destroy_model(hb_model* model);
  * by the model: for hb_append_kv into that layer's pool, hb_layer_stage and
  * the per-kernel timing calls; not to be destroyed by the caller. */
 hb_layer* hb_model_layer(hb_model* model, int32_t index);
+
+/* hb_copy_blocks in the pools of every layer of the model, on its stream: the
+ * request's block table names the same blocks in each of them. */
+hb_status hb_copy_model_blocks(hb_model* model, const int32_t* src, const int32_t* dst, int32_t n);
 
 /* One model iteration over a hybrid batch: requests as for hb_run_iteration
  * (their K/V are written into every layer's pool); token_ids device int32

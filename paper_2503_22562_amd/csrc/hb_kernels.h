@@ -115,9 +115,25 @@ void launch_append_kv(hipStream_t s, const uint16_t* k, const uint16_t* v, int n
 void launch_append_kv_inline(hipStream_t s, const uint16_t* k, const uint16_t* v, int n_tokens, int ctx,
                              const int32_t* bt, int nkv, int hd, uint16_t* k_pool, uint16_t* v_pool);
 
+// Copy whole blocks, all kv heads of K and V, inside each of n_pools pools: block
+// dst[i] becomes block src[i]. No block of dst occurs again in src or dst. The ids
+// are in device memory or (inline) in host memory, at most kCopyInlinePairs, and
+// travel with the launch.
+constexpr int kCopyPools = 64;          // pools of one launch
+constexpr int kCopyInlinePairs = 320;   // with the pools' addresses within the 4 KB of a launch's arguments
+struct CopyPools {
+  void* k[kCopyPools];
+  void* v[kCopyPools];
+};
+void launch_copy_blocks(hipStream_t s, const CopyPools& pools, int n_pools, const int32_t* src, const int32_t* dst,
+                        int n, int nkv, int hd);
+void launch_copy_blocks_inline(hipStream_t s, const CopyPools& pools, int n_pools, const int32_t* src,
+                               const int32_t* dst, int n, int nkv, int hd);
+
 struct AttnArgs {
-  const uint16_t* q;   // [T][nq*hd], rotated
-  uint16_t* o;         // [T][nq*hd]
+  const uint16_t* q;   // [T] rows of nq*hd, rotated
+  uint16_t* o;         // [T] rows of nq*hd
+  int64_t q_stride, o_stride;  // elements from row to row
   const uint16_t* k_pool;
   const uint16_t* v_pool;
   const int32_t* tiles;   // workgroup tiles (AttnItem)
@@ -136,7 +152,16 @@ struct AttnArgs {
   float* part_ml;  // [slots][2]
   int nq, nkv, hd;
   float scale_log2;  // log2(e) / sqrt(hd)
+  // windowed plans only (Plan.windowed): the window, and the units' shifts (UnitShift)
+  int windowed;
+  int window, sinks, sink_blocks;
+  const int32_t* tile_shift;
+  const int32_t* item_shift;
 };
+// The arguments of a plan's attention: its uploaded metadata, the pools and the
+// split partials. q, o and their strides are left to the caller.
+AttnArgs attention_args(const Dims& d, const Plan& p, const int32_t* meta, const void* k_pool, const void* v_pool,
+                        float* part_o, float* part_ml);
 void launch_attention(hipStream_t s, const AttnArgs& a);
 void launch_attn_merge(hipStream_t s, const AttnArgs& a);
 

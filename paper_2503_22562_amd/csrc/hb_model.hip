@@ -113,15 +113,20 @@ hb_layer* hb_model_layer(hb_model* m, int32_t index) {
   return m->layers[index];
 }
 
+hb_status hb_copy_model_blocks(hb_model* m, const int32_t* src, const int32_t* dst, int32_t n) {
+  if (!m) return fail(HB_ERR_INVALID, "null model");
+  return guarded([&] { return copy_stack_blocks(m->layers.data(), (int)m->layers.size(), src, dst, n); });
+}
+
 hb_status hb_run_model(hb_model* m, const hb_model_batch* b) {
   if (!m || !b) return fail(HB_ERR_INVALID, "null model or batch");
   if (!b->token_ids || !b->next_tokens) return fail(HB_ERR_INVALID, "null token_ids or next_tokens");
   if (b->n_requests < 1) return fail(HB_ERR_INVALID, "empty batch");
   const hb_layer_config& c = m->cfg;
   const int H = c.hidden, R = b->n_requests;
-  // validate through the first layer's check (all layers share shape and pool size)
+  // all layers share shape and pool size; their windows may differ
   hb_batch_desc desc{b->n_requests, b->requests, m->x[0], m->x[1], HB_OUT_BF16};
-  hb_status st = hb_validate_batch(&c, m->num_blocks, &desc);
+  hb_status st = check_layer_stack(m->layers.data(), (int)m->layers.size(), &desc);
   if (st == HB_OK) st = refuse_capture(m->stream);
   if (st != HB_OK) return st;
   int T = 0;

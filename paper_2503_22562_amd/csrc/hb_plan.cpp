@@ -5,6 +5,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <new>
 
 namespace hb {
 
@@ -82,7 +83,51 @@ hb_status check_window(const char* what, int64_t rows, int64_t cols) {
 
 static int64_t blocks_for(int64_t kv_len) { return (kv_len + 15) / 16; }
 
-hb_status check_batch(const Dims& d, int num_blocks, const hb_batch_desc* desc, SlotMarks* marks) {
+hb_status check_window_args(int window, int sinks) {
+  if (window < 0 || sinks < 0) return fail(HB_ERR_INVALID, "window %d or sinks %d below 0", window, sinks);
+  if (window > (1 << 30) || sinks > (1 << 30)) return fail(HB_ERR_INVALID, "window %d or sinks %d above 2^30", window, sinks);
+  return HB_OK;
+}
+
+DeadBlocks dead_blocks(const Window& w, int pos) {
+  if (w.window <= 0) return {};
+  const int first = (w.sinks + 15) / 16, end = std::max(0, pos - w.window + 1) / 16;
+  if (end <= first) return {};
+  return {first, end - first};
+}
+
+hb_status check_requests(const Dims& d, int num_blocks, const hb_request* requests, int n, const Window& w,
+                         int64_t* n_tokens) {
+  if (n < 0) return fail(HB_ERR_INVALID, "n_requests < 0");
+  if (n > d.max_R) return fail(HB_ERR_INVALID, "n_requests %d exceeds max_requests %d", n, d.max_R);
+  if (n > 0 && !requests) return fail(HB_ERR_INVALID, "null request array");
+  if (num_blocks <= 0) return fail(HB_ERR_INVALID, "pool has no blocks");
+  int64_t T = 0;
+  for (int r = 0; r < n; ++r) {
+    const hb_request& q = requests[r];
+    if (q.chunk_len < 1) return fail(HB_ERR_INVALID, "request %d: chunk_len %d < 1", r, q.chunk_len);
+    if (q.context_len < 0) return fail(HB_ERR_INVALID, "request %d: context_len %d < 0", r, q.context_len);
+    int64_t kv = (int64_t)q.context_len + q.chunk_len;
+    if (kv > (int64_t)1 << 30) return fail(HB_ERR_INVALID, "request %d: context too long", r);
+    if (!q.block_table) return fail(HB_ERR_INVALID, "request %d: null block_table", r);
+    if (q.n_blocks < blocks_for(kv))
+      return fail(HB_ERR_INVALID, "request %d: block table has %d blocks, needs %lld", r, q.n_blocks,
+                  (long long)blocks_for(kv));
+    const DeadBlocks dead = dead_blocks(w, q.context_len);
+    for (int64_t i = 0; i < blocks_for(kv); ++i) {
+      if (i == dead.first) i += dead.count;
+      int32_t b = q.block_table[i];
+      if (b < 0 || b >= num_blocks)
+        return fail(HB_ERR_RANGE, "request %d: block_table[%lld] = %d outside [0, %d)", r, (long long)i, b, num_blocks);
+    }
+    T += q.chunk_len;
+  }
+  if (T > d.max_T) return fail(HB_ERR_INVALID, "batch has %lld tokens, max_batch_tokens is %d", (long long)T, d.max_T);
+  *n_tokens = T;
+  return HB_OK;
+}
+
+hb_status check_batch(const Dims& d, int num_blocks, const hb_batch_desc* desc, SlotMarks* marks, const Window& w) {
   if (!desc) return fail(HB_ERR_INVALID, "null batch descriptor");
   const int R = desc->n_requests;
   if (R < 0) return fail(HB_ERR_INVALID, "n_requests < 0");
@@ -92,26 +137,9 @@ hb_status check_batch(const Dims& d, int num_blocks, const hb_batch_desc* desc, 
   if (!desc->x_in || !desc->x_out) return fail(HB_ERR_INVALID, "null x_in or x_out");
   if (desc->out_dtype != HB_OUT_F32 && desc->out_dtype != HB_OUT_BF16)
     return fail(HB_ERR_INVALID, "out_dtype must be HB_OUT_F32 or HB_OUT_BF16");
-  if (num_blocks <= 0) return fail(HB_ERR_INVALID, "pool has no blocks");
   int64_t T = 0;
-  for (int r = 0; r < R; ++r) {
-    const hb_request& q = desc->requests[r];
-    if (q.chunk_len < 1) return fail(HB_ERR_INVALID, "request %d: chunk_len %d < 1", r, q.chunk_len);
-    if (q.context_len < 0) return fail(HB_ERR_INVALID, "request %d: context_len %d < 0", r, q.context_len);
-    int64_t kv = (int64_t)q.context_len + q.chunk_len;
-    if (kv > (int64_t)1 << 30) return fail(HB_ERR_INVALID, "request %d: context too long", r);
-    if (!q.block_table) return fail(HB_ERR_INVALID, "request %d: null block_table", r);
-    if (q.n_blocks < blocks_for(kv))
-      return fail(HB_ERR_INVALID, "request %d: block table has %d blocks, needs %lld", r, q.n_blocks,
-                  (long long)blocks_for(kv));
-    for (int64_t i = 0; i < blocks_for(kv); ++i) {
-      int32_t b = q.block_table[i];
-      if (b < 0 || b >= num_blocks)
-        return fail(HB_ERR_RANGE, "request %d: block_table[%lld] = %d outside [0, %d)", r, (long long)i, b, num_blocks);
-    }
-    T += q.chunk_len;
-  }
-  if (T > d.max_T) return fail(HB_ERR_INVALID, "batch has %lld tokens, max_batch_tokens is %d", (long long)T, d.max_T);
+  hb_status st = check_requests(d, num_blocks, desc->requests, R, w, &T);
+  if (st != HB_OK) return st;
   // x_in (bf16) and x_out must not overlap
   {
     uintptr_t a0 = (uintptr_t)desc->x_in, a1 = a0 + (uintptr_t)T * d.H * 2;
@@ -123,7 +151,6 @@ hb_status check_batch(const Dims& d, int num_blocks, const hb_batch_desc* desc, 
   SlotMarks* m = marks ? marks : &local;
   if ((int)m->mask.size() < num_blocks) m->mask.assign(num_blocks, 0);
   m->touched.clear();
-  hb_status st = HB_OK;
   for (int r = 0; r < R && st == HB_OK; ++r) {
     const hb_request& q = desc->requests[r];
     for (int64_t p = q.context_len; p < (int64_t)q.context_len + q.chunk_len; ++p) {
@@ -143,15 +170,59 @@ hb_status check_batch(const Dims& d, int num_blocks, const hb_batch_desc* desc, 
   return st;
 }
 
+static hb_status plan_compaction(int num_blocks, int32_t* const* tables, const int32_t* n_blocks, int n_tables,
+                                 int32_t* src, int32_t* dst, int32_t* n_moves, int32_t* n_used) {
+  if (!src || !dst || !n_moves || !n_used) return fail(HB_ERR_INVALID, "hb_plan_compaction: null output pointer");
+  if (num_blocks < 1 || n_tables < 0) return fail(HB_ERR_INVALID, "num_blocks %d < 1 or n_tables %d < 0", num_blocks, n_tables);
+  if (n_tables > 0 && (!tables || !n_blocks)) return fail(HB_ERR_INVALID, "null tables or n_blocks");
+  std::vector<int32_t> to(num_blocks, -1);  // -1: not named; else where the block goes
+  int used = 0;
+  for (int t = 0; t < n_tables; ++t) {
+    if (n_blocks[t] < 0 || (n_blocks[t] > 0 && !tables[t])) return fail(HB_ERR_INVALID, "table %d: null or negative length", t);
+    for (int i = 0; i < n_blocks[t]; ++i) {
+      const int32_t b = tables[t][i];
+      if (b < -1 || b >= num_blocks)
+        return fail(HB_ERR_RANGE, "table %d: entry %d = %d outside [-1, %d)", t, i, b, num_blocks);
+      if (b >= 0 && to[b] < 0) {
+        to[b] = b;
+        ++used;
+      }
+    }
+  }
+  int moves = 0;
+  for (int b = used, hole = 0; b < num_blocks; ++b) {
+    if (to[b] < 0) continue;
+    while (to[hole] >= 0) ++hole;  // as many holes below `used` as named blocks from it on
+    src[moves] = b;
+    dst[moves++] = hole;
+    to[b] = to[hole] = hole;  // (the latter for a table given twice, whose ids are new already)
+    ++hole;
+  }
+  for (int t = 0; t < n_tables; ++t)
+    for (int i = 0; i < n_blocks[t]; ++i)
+      if (tables[t][i] >= 0) tables[t][i] = to[tables[t][i]];
+  *n_moves = moves;
+  *n_used = used;
+  return HB_OK;
+}
+
 static int align16(int x) { return (x + 15) & ~15; }
 
-void iteration_work(const Dims& d, const hb_request* reqs, int n, double* flops, double* bytes) {
+void iteration_work(const Dims& d, const hb_request* reqs, int n, double* flops, double* bytes, const Window& w) {
   double T = 0, pairs = 0, kv_tokens = 0;
   for (int r = 0; r < n; ++r) {
     double c = reqs[r].chunk_len, x = reqs[r].context_len;
     T += c;
     pairs += c * x + c * (c + 1) / 2;
     kv_tokens += x + c;
+    if (w.window > 0) {
+      // the window hides h(p) = max(0, p + 1 - window - sinks) keys from the row at p:
+      // h(x) of them from every row, and b the last row's
+      const double a = std::max(0.0, x + 1 - w.window - w.sinks), b = std::max(0.0, x + c - w.window - w.sinks);
+      const double hiding = std::min(c, b);  // rows from which something is hidden: h counts up to b over them
+      pairs -= hiding * (2 * b - hiding + 1) / 2;
+      kv_tokens -= a;
+    }
   }
   double p_lin = (double)d.H * d.qkv_n + (double)d.nq * d.hd * d.H + 3.0 * d.H * d.F;
   *flops = 2.0 * T * p_lin + 4.0 * d.nq * d.hd * pairs;
@@ -169,11 +240,17 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   const hb_request* rq = desc->requests;
   int T = 0, nbt = 0;
   std::vector<int> tok_start(R + 1, 0);
+  const Window& win = opt.window;
+  p->windowed = false;
   for (int r = 0; r < R; ++r) {
     tok_start[r] = T;
     T += rq[r].chunk_len;
-    nbt += (int)blocks_for((int64_t)rq[r].context_len + rq[r].chunk_len) + kBtPad;
+    const int64_t kv = (int64_t)rq[r].context_len + rq[r].chunk_len;
+    nbt += (int)blocks_for(kv) - dead_blocks(win, rq[r].context_len).count + kBtPad;
+    p->windowed |= win.window > 0 && kv - win.window > win.sinks;  // the last row's window hides a key
   }
+  p->window = win;
+  p->sink_blocks = p->windowed ? (win.sinks + 15) / 16 : 0;
   tok_start[R] = T;
   p->T = T;
   p->R = R;
@@ -184,7 +261,9 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   double tile_keys = 0, item_keys = 0;
   for (int r = 0; r < R; ++r) {
     const int c = rq[r].chunk_len, x = rq[r].context_len, w = is_tile(r) ? d.BQ : d.P;
-    for (int i0 = 0; i0 < c; i0 += w) (is_tile(r) ? tile_keys : item_keys) += (double)d.nkv * (x + std::min(c, i0 + w));
+    for (int i0 = 0; i0 < c; i0 += w)
+      (is_tile(r) ? tile_keys : item_keys) +=
+          (double)d.nkv * (x + std::min(c, i0 + w) - 16 * dead_blocks(win, x + i0).count);
   }
   // split lengths (multiples of 64 keys): about one round of tile workgroups
   // (each split also writes kTileCols columns of fp32 partials). Items: a
@@ -229,6 +308,7 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   // waves (n = its split count); each workgroup's four waves take
   // consecutive sub-ranges and combine them in LDS, so only ranges that need
   // more than one workgroup leave partial results for the merge kernel.
+  // In a windowed plan every length here is one of the unit's key axis (AttnItem).
   std::vector<AttnItem> tiles, singles;
   struct Unit {
     int64_t len;     // keys of the unit's longest wave
@@ -250,7 +330,8 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
     for (int g = 0; g < d.nkv; ++g) {
       for (int i0 = 0; i0 < c; i0 += w) {
         const int npos = std::min(w, c - i0);
-        const int kv_len = x + i0 + npos;
+        const int gap = 16 * dead_blocks(win, x + i0).count;
+        const int pos0 = x + i0 - gap, kv_len = pos0 + npos;
         const int nspl = (kv_len + S - 1) / S;
         if (tile) {
           int part0 = -1;
@@ -261,12 +342,12 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
           }
           if (nspl > 1) split_tiles.push_back({(int)tiles.size(), nspl, kv_len});
           for (int s = 0; s < nspl; ++s)
-            tiles.push_back({r, g, tok_start[r] + i0, x + i0, npos, s * S, std::min(kv_len, (s + 1) * S),
+            tiles.push_back({r, g, tok_start[r] + i0, pos0, npos, s * S, std::min(kv_len, (s + 1) * S),
                              nspl > 1 ? part0 + s * kTileCols : -1});
           continue;
         }
         if (nspl == 1) {
-          singles.push_back({r, g, tok_start[r] + i0, x + i0, npos, 0, kv_len, -1});
+          singles.push_back({r, g, tok_start[r] + i0, pos0, npos, 0, kv_len, -1});
           continue;
         }
         const int k = (nspl + kItemsPerUnit - 1) / kItemsPerUnit;
@@ -283,7 +364,7 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
           merged_units.push_back({plen, (int)merged_items.size(), true});
           for (int q = 0; q < kItemsPerUnit; ++q) {
             const int pb = std::min(e, b + q * plen), pe = std::min(e, pb + plen);
-            merged_items.push_back({r, g, tok_start[r] + i0, x + i0, npos, pb, pe, k > 1 ? part0 + 16 * j : -1});
+            merged_items.push_back({r, g, tok_start[r] + i0, pos0, npos, pb, pe, k > 1 ? part0 + 16 * j : -1});
           }
         }
       }
@@ -383,6 +464,8 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   p->off_units = off;    off += align16(p->n_units);
   p->off_groups = off;   off += align16(8 * p->n_groups);
   p->off_merge = off;    off += align16(p->n_merge_units);
+  p->off_tile_shift = off;  off += p->windowed ? align16(2 * nt) : 0;
+  p->off_item_shift = off;  off += p->windowed ? align16(2 * p->n_items) : 0;
   p->meta.assign(off, 0);
   int32_t* m = p->meta.data();
   int bt_off = 0;
@@ -391,18 +474,59 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
       m[p->off_tok_pos + tok_start[r] + i] = rq[r].context_len + i;
       m[p->off_tok_req + tok_start[r] + i] = r;
     }
-    m[p->off_req_bt + r] = bt_off;
+    // dead blocks are left out: block i behind them stands at req_bt + i all the same
+    const DeadBlocks dead = dead_blocks(win, rq[r].context_len);
     const int nb = (int)blocks_for((int64_t)rq[r].context_len + rq[r].chunk_len);
-    std::memcpy(m + p->off_bt + bt_off, rq[r].block_table, sizeof(int32_t) * nb);
-    for (int i = 0; i < kBtPad; ++i) m[p->off_bt + bt_off + nb + i] = rq[r].block_table[nb - 1];
-    bt_off += nb + kBtPad;
+    m[p->off_req_bt + r] = bt_off - dead.count;
+    int32_t* bt = m + p->off_bt + bt_off;
+    std::memcpy(bt, rq[r].block_table, sizeof(int32_t) * dead.first);
+    std::memcpy(bt + dead.first, rq[r].block_table + dead.first + dead.count,
+                sizeof(int32_t) * (nb - dead.first - dead.count));
+    for (int i = 0; i < kBtPad; ++i) bt[nb - dead.count + i] = rq[r].block_table[nb - 1];
+    bt_off += nb - dead.count + kBtPad;
+  }
+  if (p->windowed) {
+    // a unit's first row: its token's position tells its own gap
+    auto shifts = [&](const std::vector<AttnItem>& v, int at) {
+      for (size_t i = 0; i < v.size(); ++i) {
+        const int x = rq[v[i].req].context_len, pos = x + v[i].tok0 - tok_start[v[i].req];
+        m[at + 2 * i] = dead_blocks(win, x).count;
+        m[at + 2 * i + 1] = dead_blocks(win, pos).count;
+      }
+    };
+    shifts(tiles, p->off_tile_shift);
+    shifts(items, p->off_item_shift);
   }
   if (nt) std::memcpy(m + p->off_tiles, tiles.data(), sizeof(AttnItem) * nt);
   if (!items.empty()) std::memcpy(m + p->off_items, items.data(), sizeof(AttnItem) * items.size());
   if (!units.empty()) std::memcpy(m + p->off_units, units.data(), sizeof(int32_t) * units.size());
   if (!groups.empty()) std::memcpy(m + p->off_groups, groups.data(), sizeof(MergeGroup) * groups.size());
   if (!merge.empty()) std::memcpy(m + p->off_merge, merge.data(), sizeof(int32_t) * merge.size());
-  iteration_work(d, rq, R, &p->flops, &p->bytes);
+  iteration_work(d, rq, R, &p->flops, &p->bytes, win);
 }
 
 }  // namespace hb
+
+using namespace hb;
+
+extern "C" hb_status hb_plan_compaction(int32_t num_blocks, int32_t* const* tables, const int32_t* n_blocks,
+                                        int32_t n_tables, int32_t* src, int32_t* dst, int32_t* n_moves,
+                                        int32_t* n_used) {
+  try {
+    return plan_compaction(num_blocks, tables, n_blocks, n_tables, src, dst, n_moves, n_used);
+  } catch (const std::bad_alloc&) {
+    return fail(HB_ERR_OOM, "host allocation failed");
+  }
+}
+
+extern "C" hb_status hb_window_dead_blocks(int32_t context_len, int32_t window, int32_t sinks, int32_t* first,
+                                           int32_t* count) {
+  if (!first || !count) return fail(HB_ERR_INVALID, "null first or count");
+  if (context_len < 0) return fail(HB_ERR_INVALID, "context_len %d < 0", context_len);
+  const hb_status st = check_window_args(window, sinks);
+  if (st != HB_OK) return st;
+  const DeadBlocks b = dead_blocks({window, sinks}, context_len);
+  *first = b.first;
+  *count = b.count;
+  return HB_OK;
+}

@@ -40,6 +40,21 @@ hb_status check_config(const hb_layer_config* cfg, Dims* d);
 // HB_ERR_UNSUPPORTED unless rows x cols bf16 values fit the operand window.
 hb_status check_window(const char* what, int64_t rows, int64_t cols);
 
+// Sliding window with sinks. A row at position p sees key j <= p when
+// j > p - window or j < sinks (window 0: every j <= p).
+struct Window {
+  int window = 0, sinks = 0;
+  bool operator==(const Window& o) const { return window == o.window && (window == 0 || sinks == o.sinks); }
+};
+hb_status check_window_args(int window, int sinks);
+
+// Blocks [first, first + count) of a table that no row at a position >= pos
+// sees: past the sinks' last block, before the block of key pos - window + 1.
+struct DeadBlocks {
+  int first = 0, count = 0;
+};
+DeadBlocks dead_blocks(const Window& w, int pos);
+
 // Attention work over the key positions [kv_begin, kv_end) of one request
 // and kv head: a wave item covers 16 query columns (P positions x G heads), a
 // workgroup tile kTileCols columns (BQ positions x G heads). part < 0: the unit
@@ -48,12 +63,20 @@ hb_status check_window(const char* what, int64_t rows, int64_t cols);
 struct AttnItem {
   int32_t req, kv_head, tok0, pos0, npos, kv_begin, kv_end, part;
 };
+// Where a windowed unit's axis block i stands in its request's uploaded table:
+// i + sink below Plan.sink_blocks, i + window from there on (the upload leaves
+// out the blocks that no row of the request sees, and req_bt points as if it
+// had not).
+struct UnitShift {
+  int32_t sink, window;
+};
 // Columns whose key range was split: part s of column c sits in slot
 // part0 + s * stride + c.
 struct MergeGroup {
   int32_t part0, nparts, stride, tok0, npos, kv_head, pad0, pad1;
 };
 static_assert(sizeof(AttnItem) == 32 && sizeof(MergeGroup) == 32, "packed as 8 int32");
+static_assert(sizeof(UnitShift) == 8, "packed as 2 int32");
 
 // Each request's block ids are followed by kBtPad copies of its last id, so
 // the four ids of a 64-key step can be read as one vector even at the end.
@@ -75,9 +98,15 @@ struct Plan {
   int n_tiles = 0, n_items = 0, n_units = 0, n_groups = 0, n_merge_units = 0;
   int n_slots = 0;  // partial-result column slots
   int split_tile = 0, split_item = 0;
+  // some row's window hides a key from it: the units have shifts, and the
+  // kernels that apply `window` run
+  bool windowed = false;
+  Window window;
+  int sink_blocks = 0;
   // offsets (int32 units) of each section inside meta
   int off_tok_pos = 0, off_tok_req = 0, off_req_bt = 0, off_bt = 0;
   int off_tiles = 0, off_items = 0, off_units = 0, off_groups = 0, off_merge = 0;
+  int off_tile_shift = 0, off_item_shift = 0;
   std::vector<int32_t> meta;
   // algorithmic work of the iteration (for roofline accounting)
   double flops = 0, bytes = 0;
@@ -89,8 +118,13 @@ struct SlotMarks {
   std::vector<int32_t> touched;  // blocks to clear afterwards
 };
 
-// Validate `desc` against the layer shape and a pool of num_blocks blocks.
-hb_status check_batch(const Dims& d, int num_blocks, const hb_batch_desc* desc, SlotMarks* marks);
+// Validate `desc` against the layer shape and a pool of num_blocks blocks. Table
+// entries that the window hides from every row of their request are not looked at.
+hb_status check_batch(const Dims& d, int num_blocks, const hb_batch_desc* desc, SlotMarks* marks,
+                      const Window& w = Window());
+// The part of it that concerns the requests alone; *n_tokens receives their rows.
+hb_status check_requests(const Dims& d, int num_blocks, const hb_request* requests, int n, const Window& w,
+                         int64_t* n_tokens);
 
 // Fixed split lengths (keys, multiples of 64; 0 = chosen from the batch),
 // for tuning and tests.
@@ -98,6 +132,7 @@ struct PlanOptions {
   int split_tile = 0, split_item = 0;
   int min_item = 64;   // least item split the planner chooses by itself
   int unit_block = 0;  // runs of tiles / item groups in the unit order (0: one per CU; < 0: fine interleave)
+  Window window;
 };
 
 // Build the plan of a validated batch for a GPU with cu_count compute units.
@@ -106,6 +141,7 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
 
 // Algorithmic flops and HBM bytes of one iteration (what the method must
 // compute and move, not what an implementation happens to do).
-void iteration_work(const Dims& d, const hb_request* reqs, int n, double* flops, double* bytes);
+void iteration_work(const Dims& d, const hb_request* reqs, int n, double* flops, double* bytes,
+                    const Window& w = Window());
 
 }  // namespace hb

@@ -454,18 +454,9 @@ hb_status launch_layer(hb_layer* L, const hb_batch_desc* desc, const Prepared& p
   st = timed(L, tm, HB_K_GEMM_QKV, [&] { launch_gemm(s, gq, pq, pp.splitk); });
   if (st != HB_OK) return st;
 
-  AttnArgs at{};
+  AttnArgs at = attention_args(d, p, meta, gq.k_pool, gq.v_pool, pp.part_o, pp.part_ml);
   at.q = L->q_rot; at.o = L->attn;
-  at.k_pool = gq.k_pool; at.v_pool = gq.v_pool;
-  at.tiles = meta + p.off_tiles; at.n_tiles = p.n_tiles;
-  at.items = meta + p.off_items; at.n_items = p.n_items;
-  at.units = meta + p.off_units; at.n_units = p.n_units;
-  at.groups = meta + p.off_groups; at.n_groups = p.n_groups;
-  at.merge_units = meta + p.off_merge; at.n_merge_units = p.n_merge_units;
-  at.req_bt = rp.req_bt; at.bt = rp.bt;
-  at.part_o = pp.part_o; at.part_ml = pp.part_ml;
-  at.nq = d.nq; at.nkv = d.nkv; at.hd = d.hd;
-  at.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)d.hd));
+  at.q_stride = at.o_stride = (int64_t)d.nq * d.hd;
   st = timed(L, tm, HB_K_ATTENTION, [&] { launch_attention(s, at); });
   if (st != HB_OK) return st;
   if (p.n_groups > 0) {
@@ -527,7 +518,7 @@ hb_status settle_device(hb_layer* L, const hb_batch_desc* desc, hipEvent_t e0, h
 // the kernels alone. Fills the cell.
 hb_status time_batch(hb_layer* L, const hb_batch_desc* desc, int warmup, int iters, void* flush,
                      int64_t flush_bytes, std::vector<hipEvent_t>& ev, std::vector<float>& lat, hb_profile_cell* cell) {
-  hb_status st = check_batch(L->d, L->pool.num_blocks, desc, &L->marks);
+  hb_status st = check_batch(L->d, L->pool.num_blocks, desc, &L->marks, L->plan_opt.window);
   if (st != HB_OK) return st;
   for (int i = 0; i < warmup && st == HB_OK; ++i) st = hb_run_iteration(L, desc);
   if (st != HB_OK) return st;
@@ -555,7 +546,7 @@ hb_status time_batch(hb_layer* L, const hb_batch_desc* desc, int warmup, int ite
   cell->p10_ms = pct(0.1);
   cell->p90_ms = pct(0.9);
   double flops, bytes;
-  iteration_work(L->d, desc->requests, desc->n_requests, &flops, &bytes);
+  iteration_work(L->d, desc->requests, desc->n_requests, &flops, &bytes, L->plan_opt.window);
   int64_t T = 0;
   for (int r = 0; r < desc->n_requests; ++r) T += desc->requests[r].chunk_len;
   const double sec = cell->median_ms * 1e-3;
@@ -586,39 +577,132 @@ hb_status refuse_capture(hipStream_t s) {
                           "refill (hb_run_iteration_noalloc can be captured)");
 }
 
+// The layers' distinct windows, in order of first use, and each layer's index among them.
+static std::vector<Window> stack_windows(hb_layer* const* layers, int n, std::vector<int>* index) {
+  std::vector<Window> w;
+  if (index) index->assign(n, 0);
+  for (int l = 0; l < n; ++l) {
+    const size_t k = std::find(w.begin(), w.end(), layers[l]->plan_opt.window) - w.begin();
+    if (k == w.size()) w.push_back(layers[l]->plan_opt.window);
+    if (index) (*index)[l] = (int)k;
+  }
+  return w;
+}
+
+hb_status check_layer_stack(hb_layer* const* layers, int n, const hb_batch_desc* desc) {
+  if (n < 1 || !layers) return fail(HB_ERR_INVALID, "empty layer stack");
+  for (int l = 0; l < n; ++l)
+    if (!layers[l] || layers[l]->stream != layers[0]->stream)
+      return fail(HB_ERR_INVALID, "layer %d is null or runs on another stream", l);
+  hb_layer* L0 = layers[0];
+  hb_status st = check_batch(L0->d, L0->pool.num_blocks, desc, &L0->marks, L0->plan_opt.window);
+  // what another window sees of the tables; the rest is the same for all
+  const std::vector<Window> w = stack_windows(layers, n, nullptr);
+  int64_t T = 0;
+  for (size_t k = 1; k < w.size() && st == HB_OK; ++k)
+    st = check_requests(L0->d, L0->pool.num_blocks, desc->requests, desc->n_requests, w[k], &T);
+  return st;
+}
+
 // Every layer is checked and its buffers sized before anything is enqueued,
 // so a failure leaves every pool untouched. The metadata goes through the
 // first layer's ring; its slot is released after the last layer's kernels.
 hb_status run_layer_stack(hb_layer* const* layers, int n, const hb_batch_desc* desc, const void* const* x_in,
                           void* const* x_out) {
-  if (n < 1 || !layers || !x_in || !x_out) return fail(HB_ERR_INVALID, "empty layer stack");
-  for (int l = 0; l < n; ++l)
-    if (!layers[l] || layers[l]->stream != layers[0]->stream)
-      return fail(HB_ERR_INVALID, "layer %d is null or runs on another stream", l);
-  hb_layer* L0 = layers[0];
-  hb_status st = check_batch(L0->d, L0->pool.num_blocks, desc, &L0->marks);
+  if (!x_in || !x_out) return fail(HB_ERR_INVALID, "empty layer stack");
+  hb_status st = check_layer_stack(layers, n, desc);
   if (st != HB_OK) return st;
+  hb_layer* L0 = layers[0];
   if (desc->n_requests == 0) return HB_OK;
-  build_plan(L0->d, desc, L0->cu_count, &L0->plan, L0->plan_opt);
+  // one plan per window; their metadata, one after the other, is one upload
+  std::vector<int> kind;
+  const std::vector<Window> windows = stack_windows(layers, n, &kind);
+  std::vector<Plan> more(windows.size() - 1);
+  std::vector<size_t> meta_at(windows.size(), 0);
+  std::vector<int32_t> joined;
+  for (size_t k = 0; k < windows.size(); ++k) {
+    Plan& p = k == 0 ? L0->plan : more[k - 1];
+    PlanOptions opt = L0->plan_opt;
+    opt.window = windows[k];
+    build_plan(L0->d, desc, L0->cu_count, &p, opt);
+    if (windows.size() == 1) break;
+    meta_at[k] = joined.size();
+    joined.insert(joined.end(), p.meta.begin(), p.meta.end());
+  }
+  const std::vector<int32_t>& up = windows.size() == 1 ? L0->plan.meta : joined;
   std::vector<hb_batch_desc> dl(n, *desc);
   std::vector<Prepared> pp(n);
   for (int l = 0; l < n; ++l) {
     dl[l].x_in = x_in[l];
     dl[l].x_out = x_out[l];
-    st = prepare_gemms(layers[l], &dl[l], L0->plan, &pp[l]);
+    st = prepare_gemms(layers[l], &dl[l], kind[l] == 0 ? L0->plan : more[kind[l] - 1], &pp[l]);
     if (st != HB_OK) return st;
   }
   const int32_t* meta = nullptr;
   int slot = -1;
-  st = stage_upload(L0, L0->plan.meta.data(), L0->plan.meta.size(), &meta, &slot);
+  st = stage_upload(L0, up.data(), up.size(), &meta, &slot);
   if (st != HB_OK) return st;
   for (int l = 0; l < n && st == HB_OK; ++l) {
-    pp[l].meta = meta;
+    pp[l].meta = meta + meta_at[kind[l]];
     pp[l].slot = -1;
     st = launch_layer(layers[l], &dl[l], pp[l]);
   }
   const hb_status sc = stage_consumed(L0, slot);
   return st != HB_OK ? st : sc;
+}
+
+hb_status copy_stack_blocks(hb_layer* const* layers, int n_layers, const int32_t* src, const int32_t* dst, int n) {
+  hb_layer* L = layers[0];
+  if (n < 0) return fail(HB_ERR_INVALID, "n %d < 0", n);
+  if (n == 0) return HB_OK;
+  if (!src || !dst) return fail(HB_ERR_INVALID, "null src or dst");
+  const int nb = L->pool.num_blocks;
+  for (int i = 0; i < n; ++i)
+    if (src[i] < 0 || src[i] >= nb || dst[i] < 0 || dst[i] >= nb)
+      return fail(HB_ERR_RANGE, "copy %d: block %d to %d, outside [0, %d)", i, src[i], dst[i], nb);
+  // a block written is neither read nor written by another copy, so that their order is free
+  SlotMarks& m = L->marks;
+  if ((int)m.mask.size() < nb) m.mask.assign(nb, 0);
+  int bad = -1;
+  for (int i = 0; i < n && bad < 0; ++i) {
+    if (m.mask[dst[i]]) bad = i;
+    m.mask[dst[i]] = 1;
+  }
+  for (int i = 0; i < n && bad < 0; ++i)
+    if (m.mask[src[i]]) bad = i;
+  for (int i = 0; i < n; ++i) m.mask[dst[i]] = 0;
+  if (bad >= 0)
+    return fail(HB_ERR_INVALID, "copy %d (block %d to %d): a block that is written occurs again in the list", bad,
+                src[bad], dst[bad]);
+  const DeviceGuard on(L->device);
+  hb_status st = refuse_capture(L->stream);
+  if (st != HB_OK) return st;
+  const int32_t *s_dev = nullptr, *d_dev = nullptr;
+  int slot = -1;
+  if (n > kCopyInlinePairs) {
+    std::vector<int32_t> both(2 * (size_t)n);
+    std::copy(src, src + n, both.begin());
+    std::copy(dst, dst + n, both.begin() + n);
+    st = stage_upload(L, both.data(), both.size(), &s_dev, &slot);
+    if (st != HB_OK) return st;
+    d_dev = s_dev + n;
+  }
+  for (int l0 = 0; l0 < n_layers; l0 += kCopyPools) {
+    CopyPools pools{};
+    const int nl = std::min(kCopyPools, n_layers - l0);
+    for (int l = 0; l < nl; ++l) {
+      pools.k[l] = layers[l0 + l]->pool.k_pool;
+      pools.v[l] = layers[l0 + l]->pool.v_pool;
+    }
+    if (slot < 0) launch_copy_blocks_inline(L->stream, pools, nl, src, dst, n, L->d.nkv, L->d.hd);
+    else launch_copy_blocks(L->stream, pools, nl, s_dev, d_dev, n, L->d.nkv, L->d.hd);
+  }
+  st = check_hip("block copy launch");
+  if (slot >= 0) {
+    const hb_status sc = stage_consumed(L, slot);
+    if (st == HB_OK) st = sc;
+  }
+  return st;
 }
 
 }  // namespace hb
@@ -734,9 +818,23 @@ hb_status hb_append_kv(hb_layer* L, const int32_t* block_table, int32_t n_blocks
   return check_hip("append_kv launch");
 }
 
+hb_status hb_copy_blocks(hb_layer* L, const int32_t* src, const int32_t* dst, int32_t n) {
+  if (!L) return fail(HB_ERR_INVALID, "null layer");
+  return guarded([&] { return copy_stack_blocks(&L, 1, src, dst, n); });
+}
+
+hb_status hb_set_attention_window(hb_layer* L, int32_t window, int32_t sinks) {
+  if (!L) return fail(HB_ERR_INVALID, "null layer");
+  const hb_status st = check_window_args(window, sinks);
+  if (st != HB_OK) return st;
+  L->plan_opt.window.window = window;
+  L->plan_opt.window.sinks = window > 0 ? sinks : 0;
+  return HB_OK;
+}
+
 hb_status hb_run_iteration(hb_layer* L, const hb_batch_desc* desc) {
   if (!L) return fail(HB_ERR_INVALID, "null layer");
-  hb_status st = check_batch(L->d, L->pool.num_blocks, desc, &L->marks);
+  hb_status st = check_batch(L->d, L->pool.num_blocks, desc, &L->marks, L->plan_opt.window);
   if (st != HB_OK) return st;
   if (desc->n_requests == 0) return HB_OK;
   st = refuse_capture(L->stream);
@@ -747,7 +845,7 @@ hb_status hb_run_iteration(hb_layer* L, const hb_batch_desc* desc) {
 
 hb_status hb_run_iteration_noalloc(hb_layer* L, const hb_batch_desc* desc) {
   if (!L) return fail(HB_ERR_INVALID, "null layer");
-  hb_status st = check_batch(L->d, L->pool.num_blocks, desc, &L->marks);
+  hb_status st = check_batch(L->d, L->pool.num_blocks, desc, &L->marks, L->plan_opt.window);
   if (st != HB_OK) return st;
   if (desc->n_requests == 0) return HB_OK;
   const Dims& d = L->d;
@@ -1037,7 +1135,7 @@ hb_status hb_profile_batches(hb_layer* L, const hb_batch_desc* batches, int32_t 
   if (!L || !out || n_batches < 0 || (n_batches > 0 && !batches)) return fail(HB_ERR_INVALID, "null argument");
   if (iters < 1 || warmup < 0) return fail(HB_ERR_INVALID, "iters < 1 or warmup < 0");
   for (int b = 0; b < n_batches; ++b) {
-    const hb_status st = check_batch(L->d, L->pool.num_blocks, &batches[b], &L->marks);
+    const hb_status st = check_batch(L->d, L->pool.num_blocks, &batches[b], &L->marks, L->plan_opt.window);
     if (st != HB_OK) return st;
     if (batches[b].n_requests == 0) return fail(HB_ERR_INVALID, "batch %d is empty", b);
   }

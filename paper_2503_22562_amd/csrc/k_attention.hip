@@ -32,7 +32,16 @@
 // workgroups run side by side. Key ranges longer than one work unit takes
 // are divided over several units; a merge kernel combines their partial
 // results with the log-sum-exp rule.
+//
+// Sliding windows (WIN): a row at position p also leaves out the keys
+// j <= p - window that are no sinks (j >= sinks). The planner gives every unit
+// a key axis without the blocks that none of its rows sees, on which both
+// rules keep their form (AttnItem), so a windowed unit differs in its block
+// lookups (one select per id) and in the masks of the steps at the window's
+// far edge; the steps between the two edges run unmasked as ever.
 #include <algorithm>
+#include <cmath>
+#include <type_traits>
 
 #include "hb_device.h"
 #include "hb_kernels.h"
@@ -111,6 +120,32 @@ __device__ __forceinline__ bf16x8 p_operand(const float (&p)[N], int kk) {
   return as_bf16x8(w);
 }
 
+// A unit's block ids: entry i of its key axis, the last block's past the end.
+template <bool WIN>
+struct BlockIds {
+  const int32_t* tab;
+  int last;
+  int sinks, sink_shift, window_shift;  // WIN: sink blocks, and the table shifts below and from them on
+  __device__ __forceinline__ int at(int i) const {
+    i = min(i, last);
+    if (WIN) i += i < sinks ? sink_shift : window_shift;
+    return const_load(tab + i);
+  }
+};
+template <bool WIN>
+__device__ __forceinline__ BlockIds<WIN> block_ids(const AttnArgs& a, const AttnItem& it, UnitShift sh) {
+  return {a.bt + const_load(a.req_bt + it.req), (it.kv_end - 1) >> 4, a.sink_blocks, sh.sink, sh.window};
+}
+
+// First key of the axis that the window hides from no row of the unit, sinks aside.
+__device__ __forceinline__ int window_edge(const AttnArgs& a, const AttnItem& it) {
+  const int e = it.pos0 + it.npos - a.window;
+  return e > a.sinks ? e : 0;
+}
+
+// Whether the window hides key j from the row at position pos.
+__device__ __forceinline__ bool hidden(const AttnArgs& a, int j, int pos) { return j <= pos - a.window && j >= a.sinks; }
+
 // Write the result of one column: normalised bf16 output, or fp32 partials.
 template <int HD>
 __device__ __forceinline__ void store_column(const AttnArgs& a, const AttnItem& it, int c, const f32x4 (&o)[HD / 16],
@@ -121,7 +156,7 @@ __device__ __forceinline__ void store_column(const AttnArgs& a, const AttnItem& 
   if (it.part < 0) {
     const int h = it.kv_head * G + (c - pi * G);
     const float inv = 1.0f / l;
-    uint16_t* orow = a.o + (size_t)(it.tok0 + pi) * a.nq * HD + h * HD + 4 * grp;
+    uint16_t* orow = a.o + (int64_t)(it.tok0 + pi) * a.o_stride + h * HD + 4 * grp;
 #pragma unroll
     for (int dt = 0; dt < HD / 16; ++dt) {
       u32x2 w = {pack_bf16x2(o[dt][0] * inv, o[dt][1] * inv), pack_bf16x2(o[dt][2] * inv, o[dt][3] * inv)};
@@ -190,10 +225,23 @@ __device__ __forceinline__ u32x4 v_key_mask(int j0, int kv_end, int grp) {
   return vm;
 }
 
-template <int HD>
-__device__ __forceinline__ void wave_compute(const WaveStep<HD>& st, int j0, const AttnItem& it, int pos, int grp,
-                                             float sc, const bf16x8 (&qf)[HD / 32], f32x4 (&o)[HD / 16], float& m,
-                                             float& l) {
+// The same for a windowed unit, whose first row sees the furthest back: keys
+// hidden from it may be slots of a block that has other contents by now.
+__device__ __forceinline__ u32x4 v_window_mask(const AttnArgs& a, const AttnItem& it, int j0, int grp) {
+  u32x4 vm;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const int k = j0 + 8 * grp + 2 * w;
+    vm[w] = (k < it.kv_end && !hidden(a, k, it.pos0) ? 0xFFFFu : 0u) |
+            (k + 1 < it.kv_end && !hidden(a, k + 1, it.pos0) ? 0xFFFF0000u : 0u);
+  }
+  return vm;
+}
+
+template <int HD, bool WIN>
+__device__ __forceinline__ void wave_compute(const AttnArgs& a, const WaveStep<HD>& st, int j0, const AttnItem& it,
+                                             int pos, int grp, float sc, const bf16x8 (&qf)[HD / 32],
+                                             f32x4 (&o)[HD / 16], float& m, float& l) {
   f32x4 s[2];
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
@@ -206,13 +254,16 @@ __device__ __forceinline__ void wave_compute(const WaveStep<HD>& st, int j0, con
   for (int b = 0; b < 2; ++b)
 #pragma unroll
     for (int i = 0; i < 4; ++i) sv[4 * b + i] = s[b][i];
-  if (j0 + WSTEP > it.kv_end || j0 + WSTEP > it.pos0) {  // causal / tail masking (wave-uniform)
+  const bool edge = WIN && j0 < window_edge(a, it);              // the window's far edge (wave-uniform)
+  if (j0 + WSTEP > it.kv_end || j0 + WSTEP > it.pos0 || edge) {  // causal / tail masking (wave-uniform)
     const int lim = min(pos, it.kv_end - 1);
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (j0 + 8 * grp + 4 * b + i > lim) sv[4 * b + i] = -INFINITY;
+      for (int i = 0; i < 4; ++i) {
+        const int j = j0 + 8 * grp + 4 * b + i;
+        if (j > lim || (WIN && hidden(a, j, pos))) sv[4 * b + i] = -INFINITY;
+      }
   }
   float ps;
   bf16x8 pf;
@@ -224,8 +275,8 @@ __device__ __forceinline__ void wave_compute(const WaveStep<HD>& st, int j0, con
   }
   l += ps;
   pf = p_operand(p, 0);
-  if (j0 + WSTEP > it.kv_end) {  // tail step (wave-uniform)
-    const u32x4 vm = v_key_mask(j0, it.kv_end, grp);
+  if (j0 + WSTEP > it.kv_end || edge) {  // tail step (wave-uniform)
+    const u32x4 vm = WIN ? v_window_mask(a, it, j0, grp) : v_key_mask(j0, it.kv_end, grp);
 #pragma unroll
     for (int dt = 0; dt < HD / 16; ++dt) o[dt] = mfma16x16x32(as_bf16x8(st.v[dt] & vm), pf, o[dt]);
   } else {
@@ -237,9 +288,9 @@ __device__ __forceinline__ void wave_compute(const WaveStep<HD>& st, int j0, con
 // One wave item's 16 columns over its key range: the unnormalised O^T, the
 // running maximum m and the weight sum l of the lane's column (l summed over
 // the column's four lanes; m is the same on all four).
-template <int HD>
-__device__ __forceinline__ void wave_run(const AttnArgs& a, const AttnItem& it, int lane, f32x4 (&o)[HD / 16],
-                                         float& m, float& l) {
+template <int HD, bool WIN>
+__device__ __forceinline__ void wave_run(const AttnArgs& a, const AttnItem& it, UnitShift sh, int lane,
+                                         f32x4 (&o)[HD / 16], float& m, float& l) {
   const int G = a.nq / a.nkv;
   const int col = lane & 15, grp = lane >> 4;
   const int pi = col / G;
@@ -250,21 +301,23 @@ __device__ __forceinline__ void wave_run(const AttnArgs& a, const AttnItem& it, 
 #pragma unroll
   for (int kc = 0; kc < HD / 32; ++kc) {
     u32x4 v = {0u, 0u, 0u, 0u};
-    if (valid) v = ld16(a.q + (size_t)(it.tok0 + pi) * a.nq * HD + h * HD + 32 * kc + 8 * grp);
+    if (valid) v = ld16(a.q + (int64_t)(it.tok0 + pi) * a.q_stride + h * HD + 32 * kc + 8 * grp);
     qf[kc] = as_bf16x8(v);
   }
-  const int32_t* btab = a.bt + const_load(a.req_bt + it.req);
-  const int kb_last = (it.kv_end - 1) >> 4;
+  const BlockIds<WIN> blocks = block_ids<WIN>(a, it, sh);
 #pragma unroll
   for (int dt = 0; dt < HD / 16; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
   m = NEG_BIG;
   l = 0.f;
   const int nsteps = (it.kv_end - it.kv_begin + WSTEP - 1) / WSTEP;
   // the table is padded with copies of its last id (kBtPad), so the two ids
-  // of a step are one 8-byte read; steps past the end re-read the last block
+  // of a step are one 8-byte read; steps past the end re-read the last block.
+  // (On a windowed axis the two may stand apart.)
   typedef int32_t i32x2 __attribute__((ext_vector_type(2)));
   auto ids_of = [&](int s) {
-    return const_load(reinterpret_cast<const i32x2*>(btab + min((it.kv_begin >> 4) + 2 * s, kb_last)));
+    const int i = (it.kv_begin >> 4) + 2 * s;
+    if constexpr (WIN) return i32x2{blocks.at(i), blocks.at(i + 1)};
+    else return const_load(reinterpret_cast<const i32x2*>(blocks.tab + min(i, blocks.last)));
   };
   // Block ids are fetched one step before the loads that use them. Loads in
   // the steady-state loop are unconditional so the compiler can wait for one
@@ -279,29 +332,36 @@ __device__ __forceinline__ void wave_run(const AttnArgs& a, const AttnItem& it, 
     wave_load(B, a, ids[0], ids[1], g, col, grp);
     ids = ids_of(s + 2);
     __builtin_amdgcn_sched_barrier(0);  // keep the prefetch ahead of the compute
-    wave_compute(A, it.kv_begin + WSTEP * s, it, pos, grp, a.scale_log2, qf, o, m, l);
+    wave_compute<HD, WIN>(a, A, it.kv_begin + WSTEP * s, it, pos, grp, a.scale_log2, qf, o, m, l);
     __builtin_amdgcn_sched_barrier(0);
     wave_load(A, a, ids[0], ids[1], g, col, grp);
     ids = ids_of(s + 3);
     __builtin_amdgcn_sched_barrier(0);
-    wave_compute(B, it.kv_begin + WSTEP * (s + 1), it, pos, grp, a.scale_log2, qf, o, m, l);
+    wave_compute<HD, WIN>(a, B, it.kv_begin + WSTEP * (s + 1), it, pos, grp, a.scale_log2, qf, o, m, l);
     __builtin_amdgcn_sched_barrier(0);
   }
   if (s + 1 < nsteps) {
     wave_load(B, a, ids[0], ids[1], g, col, grp);
-    wave_compute(A, it.kv_begin + WSTEP * s, it, pos, grp, a.scale_log2, qf, o, m, l);
-    wave_compute(B, it.kv_begin + WSTEP * (s + 1), it, pos, grp, a.scale_log2, qf, o, m, l);
+    wave_compute<HD, WIN>(a, A, it.kv_begin + WSTEP * s, it, pos, grp, a.scale_log2, qf, o, m, l);
+    wave_compute<HD, WIN>(a, B, it.kv_begin + WSTEP * (s + 1), it, pos, grp, a.scale_log2, qf, o, m, l);
   } else {
-    wave_compute(A, it.kv_begin + WSTEP * s, it, pos, grp, a.scale_log2, qf, o, m, l);
+    wave_compute<HD, WIN>(a, A, it.kv_begin + WSTEP * s, it, pos, grp, a.scale_log2, qf, o, m, l);
   }
   l = rows_sum(l);
 }
 
-template <int HD>
-__device__ __forceinline__ void wave_item(const AttnArgs& a, const AttnItem& it, int lane) {
+// Shift of item idx / tile idx (none without a window).
+template <bool WIN>
+__device__ __forceinline__ UnitShift shift_of(const int32_t* shifts, int idx) {
+  if constexpr (WIN) return const_load(reinterpret_cast<const UnitShift*>(shifts) + idx);
+  else return {0, 0};
+}
+
+template <int HD, bool WIN>
+__device__ __forceinline__ void wave_item(const AttnArgs& a, const AttnItem& it, UnitShift sh, int lane) {
   f32x4 o[HD / 16];
   float m, l;
-  wave_run<HD>(a, it, lane, o, m, l);
+  wave_run<HD, WIN>(a, it, sh, lane, o, m, l);
   store_column<HD>(a, it, lane & 15, o, m, l, lane >> 4);
 }
 
@@ -311,7 +371,7 @@ __device__ __forceinline__ void wave_item(const AttnArgs& a, const AttnItem& it,
 // M = max_w m_w, O = sum_w O_w 2^(m_w - M) and l = sum_w l_w 2^(m_w - M).
 // Wave w then finishes dimension tiles w DT/4 .. (w + 1) DT/4 - 1 of every
 // column and writes them, normalised, or as a partial result (O, M, l).
-template <int HD>
+template <int HD, bool WIN>
 __device__ __forceinline__ void merged_unit(const AttnArgs& a, int v, uint8_t* smem) {
   constexpr int DT = HD / 16, PER = DT / WAVES;
   static_assert(PER * WAVES == DT, "dimension tiles per wave");
@@ -321,7 +381,7 @@ __device__ __forceinline__ void merged_unit(const AttnArgs& a, int v, uint8_t* s
   f32x4 o[DT];
   float m = NEG_BIG, l = 0.f;
   if (it.kv_begin < it.kv_end) {
-    wave_run<HD>(a, it, lane, o, m, l);
+    wave_run<HD, WIN>(a, it, shift_of<WIN>(a.item_shift, WAVES * v + wave), lane, o, m, l);
   } else {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -360,7 +420,7 @@ __device__ __forceinline__ void merged_unit(const AttnArgs& a, int v, uint8_t* s
   if (it.part < 0) {
     const int h = it.kv_head * G + (col - pi * G);
     const float inv = 1.0f / L;
-    uint16_t* orow = a.o + (size_t)(it.tok0 + pi) * a.nq * HD + h * HD + 4 * grp;
+    uint16_t* orow = a.o + (int64_t)(it.tok0 + pi) * a.o_stride + h * HD + 4 * grp;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int dt = wave * PER + i;
@@ -445,11 +505,12 @@ __device__ __forceinline__ void tile_read_v(u32x4 (&vf)[HD / 16], const uint8_t*
   for (int dt = 0; dt < HD / 16; ++dt) vf[dt] = *reinterpret_cast<const u32x4*>(vs + dt * 256);
 }
 
-// MASKED: the V lanes of keys past kv_end are cleared.
-template <int HD, bool MASKED>
-__device__ __forceinline__ void tile_mask_v(u32x4 (&vf)[HD / 16], int j0, int kv_end, int grp) {
+// MASKED: the V lanes of keys past kv_end (or hidden from every row) are cleared.
+template <int HD, bool MASKED, bool WIN>
+__device__ __forceinline__ void tile_mask_v(u32x4 (&vf)[HD / 16], const AttnArgs& a, const AttnItem& it, int j0,
+                                            int grp) {
   if (!MASKED) return;
-  const u32x4 vm = v_key_mask(j0, kv_end, grp);
+  const u32x4 vm = WIN ? v_window_mask(a, it, j0, grp) : v_key_mask(j0, it.kv_end, grp);
 #pragma unroll
   for (int dt = 0; dt < HD / 16; ++dt) vf[dt] &= vm;
 }
@@ -471,11 +532,11 @@ __device__ __forceinline__ void tile_scores(f32x4 (&sc)[CT][2], const bf16x8 (&k
 // case (branch-free, so the score MFMAs can be scheduled across it) gives
 // the weights pf and their sums ps against the running maxima; it returns
 // whether tile_rescale must run. MASKED: keys past a column's position or
-// past kv_end get no weight.
-template <int HD, int CT, bool MASKED>
-__device__ __forceinline__ bool tile_softmax(const f32x4 (&sc)[CT][2], float (&sv)[CT][8], float (&p)[CT][8],
-                                             float (&ps)[CT], const float (&m)[CT], const int (&pos)[CT], int j0,
-                                             int kv_end, int grp, float scale) {
+// past kv_end, or hidden by its window, get no weight.
+template <int HD, int CT, bool MASKED, bool WIN>
+__device__ __forceinline__ bool tile_softmax(const AttnArgs& a, const f32x4 (&sc)[CT][2], float (&sv)[CT][8],
+                                             float (&p)[CT][8], float (&ps)[CT], const float (&m)[CT],
+                                             const int (&pos)[CT], int j0, int kv_end, int grp, float scale) {
   bool rescale = false;
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
@@ -488,8 +549,10 @@ __device__ __forceinline__ bool tile_softmax(const f32x4 (&sc)[CT][2], float (&s
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (j0 + 8 * grp + 4 * b + i > lim) sv[ct][4 * b + i] = -INFINITY;
+        for (int i = 0; i < 4; ++i) {
+          const int j = j0 + 8 * grp + 4 * b + i;
+          if (j > lim || (WIN && hidden(a, j, pos[ct]))) sv[ct][4 * b + i] = -INFINITY;
+        }
     }
     rescale |= softmax_fast<8>(sv[ct], scale, m[ct], ps[ct], p[ct]);
   }
@@ -507,10 +570,10 @@ __device__ __forceinline__ void tile_pv(f32x4 (&o)[CT][HD / 16], const u32x4 (&v
 // One key step of a tile. The scores of this step (sc_cur) were formed one
 // step earlier; while their softmax runs on the vector ALUs, the next step's
 // scores go to the matrix cores (sc_next), so the two overlap within the wave.
-template <int HD, int CT, bool MASKED, bool LAST>
+template <int HD, int CT, bool WIN, bool MASKED, bool LAST>
 __device__ __forceinline__ void tile_step(const AttnArgs& a, const AttnItem& it, uint8_t* smem, int kt, int nsteps,
-                                          const int32_t* btab, int kb0, int kb_last, int& next_id, int wave,
-                                          int lane, int k_lane, int v_lane, const bf16x8 (&qf)[CT][HD / 32],
+                                          const BlockIds<WIN>& blocks, int kb0, int& next_id, int wave, int lane,
+                                          int k_lane, int v_lane, const bf16x8 (&qf)[CT][HD / 32],
                                           const int (&pos)[CT], f32x4 (&o)[CT][HD / 16], float (&m)[CT],
                                           float (&l)[CT], f32x4 (&sc_cur)[CT][2], f32x4 (&sc_next)[CT][2]) {
   using TG = TileGeom<HD>;
@@ -527,14 +590,15 @@ __device__ __forceinline__ void tile_step(const AttnArgs& a, const AttnItem& it,
     __builtin_amdgcn_s_barrier();
     if (kt + TSTAGES - 1 < nsteps) {
       tile_issue<HD>(smem + ((kt + TSTAGES - 1) % TSTAGES) * TG::STAGE, a, next_id, it.kv_head, wave, lane);
-      if (kt + TSTAGES < nsteps) next_id = const_load(btab + min(kb0 + 2 * (kt + TSTAGES) + (wave & 1), kb_last));
+      if (kt + TSTAGES < nsteps) next_id = blocks.at(kb0 + 2 * (kt + TSTAGES) + (wave & 1));
     }
     bf16x8 kf[2][HD / 32];
     tile_read_k<HD>(kf, smem + ((kt + 1) % TSTAGES) * TG::STAGE, k_lane);
     tile_scores<HD, CT>(sc_next, kf, qf);
   }
   float sv[CT][8], p[CT][8], ps[CT];
-  const bool rescale = tile_softmax<HD, CT, MASKED>(sc_cur, sv, p, ps, m, pos, j0, it.kv_end, grp, a.scale_log2);
+  const bool rescale =
+      tile_softmax<HD, CT, MASKED, WIN>(a, sc_cur, sv, p, ps, m, pos, j0, it.kv_end, grp, a.scale_log2);
   bf16x8 pf[CT];
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) pf[ct] = p_operand(p[ct], 0);
@@ -559,12 +623,12 @@ __device__ __forceinline__ void tile_step(const AttnArgs& a, const AttnItem& it,
   }
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) l[ct] += ps[ct];
-  tile_mask_v<HD, MASKED>(vf, j0, it.kv_end, grp);
+  tile_mask_v<HD, MASKED, WIN>(vf, a, it, j0, grp);
   tile_pv<HD, CT>(o, vf, pf);
 }
 
-template <int HD>
-__device__ __forceinline__ void tile_unit(const AttnArgs& a, const AttnItem& it, uint8_t* smem) {
+template <int HD, bool WIN>
+__device__ __forceinline__ void tile_unit(const AttnArgs& a, const AttnItem& it, UnitShift sh, uint8_t* smem) {
   using TG = TileGeom<HD>;
   constexpr int KC = HD / 32, DT = HD / 16;
   constexpr int CT = 2;  // 16-column tiles per wave (4 waves x 32 columns)
@@ -584,12 +648,11 @@ __device__ __forceinline__ void tile_unit(const AttnArgs& a, const AttnItem& it,
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc) {
       u32x4 v = {0u, 0u, 0u, 0u};
-      if (valid) v = ld16(a.q + (size_t)(it.tok0 + pi) * a.nq * HD + h * HD + 32 * kc + 8 * grp);
+      if (valid) v = ld16(a.q + (int64_t)(it.tok0 + pi) * a.q_stride + h * HD + 32 * kc + 8 * grp);
       qf[ct][kc] = as_bf16x8(v);
     }
   }
-  const int32_t* btab = a.bt + const_load(a.req_bt + it.req);
-  const int kb_last = (it.kv_end - 1) >> 4;
+  const BlockIds<WIN> blocks = block_ids<WIN>(a, it, sh);
   const int kb0 = it.kv_begin >> 4;
   const int nsteps = (it.kv_end - it.kv_begin + TSTEP - 1) / TSTEP;
   // steps whose keys all lie below the tile's first position and kv_end need no mask
@@ -607,11 +670,11 @@ __device__ __forceinline__ void tile_unit(const AttnArgs& a, const AttnItem& it,
   const int k_lane = TG::off(col >> 3) + (8 * grp + (col & 7)) * 16;
   const int v_lane = grp * HD * 16 + col * 16;
   // prologue: steps 0..TSTAGES-2 in flight, scores of step 0
-  int next_id = const_load(btab + min(kb0 + (wave & 1), kb_last));
+  int next_id = blocks.at(kb0 + (wave & 1));
 #pragma unroll
   for (int s0 = 0; s0 < TSTAGES - 1; ++s0) {
     if (s0 < nsteps) tile_issue<HD>(smem + s0 * TG::STAGE, a, next_id, g, wave, lane);
-    if (s0 + 1 < nsteps) next_id = const_load(btab + min(kb0 + 2 * (s0 + 1) + (wave & 1), kb_last));
+    if (s0 + 1 < nsteps) next_id = blocks.at(kb0 + 2 * (s0 + 1) + (wave & 1));
   }
   if (nsteps >= 3) wait_vmcnt<2 * TG::LOADS>();
   else if (nsteps == 2) wait_vmcnt<TG::LOADS>();
@@ -624,45 +687,54 @@ __device__ __forceinline__ void tile_unit(const AttnArgs& a, const AttnItem& it,
     tile_scores<HD, CT>(sa, kf, qf);
   }
   // steps alternate the two score buffers; the last step is peeled
+  auto step = [&](auto masked, auto last, int t, f32x4(&cur)[CT][2], f32x4(&next)[CT][2]) {
+    tile_step<HD, CT, WIN, decltype(masked)::value, decltype(last)::value>(
+        a, it, smem, t, nsteps, blocks, kb0, next_id, wave, lane, k_lane, v_lane, qf, pos, o, m, l, cur, next);
+  };
+  constexpr std::true_type yes{};
+  constexpr std::false_type no{};
   int kt = 0;
+  if (WIN) {
+    // steps with keys that the window hides from some row
+    const int far = (window_edge(a, it) - it.kv_begin + TSTEP - 1) / TSTEP;
+    for (; kt < far && kt + 2 < nsteps; kt += 2) {
+      step(yes, no, kt, sa, sb);
+      step(yes, no, kt + 1, sb, sa);
+    }
+  }
   for (; kt + 2 <= full && kt + 2 < nsteps; kt += 2) {
-    tile_step<HD, CT, false, false>(a, it, smem, kt, nsteps, btab, kb0, kb_last, next_id, wave, lane, k_lane, v_lane,
-                                    qf, pos, o, m, l, sa, sb);
-    tile_step<HD, CT, false, false>(a, it, smem, kt + 1, nsteps, btab, kb0, kb_last, next_id, wave, lane, k_lane,
-                                    v_lane, qf, pos, o, m, l, sb, sa);
+    step(no, no, kt, sa, sb);
+    step(no, no, kt + 1, sb, sa);
   }
   for (; kt + 2 < nsteps; kt += 2) {
-    tile_step<HD, CT, true, false>(a, it, smem, kt, nsteps, btab, kb0, kb_last, next_id, wave, lane, k_lane, v_lane,
-                                   qf, pos, o, m, l, sa, sb);
-    tile_step<HD, CT, true, false>(a, it, smem, kt + 1, nsteps, btab, kb0, kb_last, next_id, wave, lane, k_lane,
-                                   v_lane, qf, pos, o, m, l, sb, sa);
+    step(yes, no, kt, sa, sb);
+    step(yes, no, kt + 1, sb, sa);
   }
   if (kt + 1 < nsteps) {
-    tile_step<HD, CT, true, false>(a, it, smem, kt, nsteps, btab, kb0, kb_last, next_id, wave, lane, k_lane, v_lane,
-                                   qf, pos, o, m, l, sa, sb);
-    tile_step<HD, CT, true, true>(a, it, smem, kt + 1, nsteps, btab, kb0, kb_last, next_id, wave, lane, k_lane, v_lane,
-                                  qf, pos, o, m, l, sb, sa);
+    step(yes, no, kt, sa, sb);
+    step(yes, yes, kt + 1, sb, sa);
   } else {
-    tile_step<HD, CT, true, true>(a, it, smem, kt, nsteps, btab, kb0, kb_last, next_id, wave, lane, k_lane, v_lane,
-                                  qf, pos, o, m, l, sa, sb);
+    step(yes, yes, kt, sa, sb);
   }
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) store_column<HD>(a, it, 32 * wave + 16 * ct + col, o[ct], m[ct], rows_sum(l[ct]), grp);
 }
 
-template <int HD>
+template <int HD, bool WIN>
 __global__ __launch_bounds__(64 * WAVES, 2) void attn_kernel(AttnArgs a) {
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
   const int unit = const_load(a.units + blockIdx.x);
   if (unit >= 0) {
-    tile_unit<HD>(a, const_load(reinterpret_cast<const AttnItem*>(a.tiles) + unit), smem);
+    tile_unit<HD, WIN>(a, const_load(reinterpret_cast<const AttnItem*>(a.tiles) + unit),
+                       shift_of<WIN>(a.tile_shift, unit), smem);
   } else if ((-unit - 1) & kUnitMerged) {
-    merged_unit<HD>(a, (-unit - 1) & ~kUnitMerged, smem);
+    merged_unit<HD, WIN>(a, (-unit - 1) & ~kUnitMerged, smem);
   } else {
     const int idx = (-unit - 1) * WAVES + wave_id();
     if (idx < a.n_items) {
       const AttnItem it = const_load(reinterpret_cast<const AttnItem*>(a.items) + idx);
-      if (it.kv_begin < it.kv_end) wave_item<HD>(a, it, threadIdx.x & 63);
+      if (it.kv_begin < it.kv_end)
+        wave_item<HD, WIN>(a, it, shift_of<WIN>(a.item_shift, idx), threadIdx.x & 63);
     }
   }
 }
@@ -744,7 +816,7 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a) {
   const int pi = c / G, h = gr.kv_head * G + (c - pi * G);
   u32x4 w = {pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv),
              pack_bf16x2(acc[4] * inv, acc[5] * inv), pack_bf16x2(acc[6] * inv, acc[7] * inv)};
-  st16(a.o + (size_t)(gr.tok0 + pi) * a.nq * HD + h * HD + d, w);
+  st16(a.o + (int64_t)(gr.tok0 + pi) * a.o_stride + h * HD + d, w);
 }
 
 // A launch without chunk tiles only streams K/V through wave items, and one
@@ -755,21 +827,41 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a) {
 // stay far faster.
 constexpr int kItemOnlyLds = 96 * 1024;
 
-template <int HD>
+template <int HD, bool WIN>
 void launch(hipStream_t s, const AttnArgs& a) {
   constexpr int lds = TSTAGES * TileGeom<HD>::STAGE;
   static_assert(2 * lds <= 160 * 1024 && 2 * kItemOnlyLds > 160 * 1024 && kItemOnlyLds <= 160 * 1024, "occupancy");
   static std::atomic<uint64_t> lds_raised{0};
-  raise_dynamic_lds(reinterpret_cast<const void*>(&attn_kernel<HD>), kItemOnlyLds, lds_raised);
-  attn_kernel<HD><<<a.n_units, 64 * WAVES, a.n_tiles > 0 ? lds : kItemOnlyLds, s>>>(a);
+  raise_dynamic_lds(reinterpret_cast<const void*>(&attn_kernel<HD, WIN>), kItemOnlyLds, lds_raised);
+  attn_kernel<HD, WIN><<<a.n_units, 64 * WAVES, a.n_tiles > 0 ? lds : kItemOnlyLds, s>>>(a);
 }
 
 }  // namespace attn_detail
 
+AttnArgs attention_args(const Dims& d, const Plan& p, const int32_t* meta, const void* k_pool, const void* v_pool,
+                        float* part_o, float* part_ml) {
+  AttnArgs at{};
+  at.k_pool = static_cast<const uint16_t*>(k_pool); at.v_pool = static_cast<const uint16_t*>(v_pool);
+  at.tiles = meta + p.off_tiles; at.n_tiles = p.n_tiles;
+  at.items = meta + p.off_items; at.n_items = p.n_items;
+  at.units = meta + p.off_units; at.n_units = p.n_units;
+  at.groups = meta + p.off_groups; at.n_groups = p.n_groups;
+  at.merge_units = meta + p.off_merge; at.n_merge_units = p.n_merge_units;
+  at.req_bt = meta + p.off_req_bt; at.bt = meta + p.off_bt;
+  at.part_o = part_o; at.part_ml = part_ml;
+  at.nq = d.nq; at.nkv = d.nkv; at.hd = d.hd;
+  at.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)d.hd));
+  at.windowed = p.windowed;
+  at.window = p.window.window; at.sinks = p.window.sinks; at.sink_blocks = p.sink_blocks;
+  at.tile_shift = meta + p.off_tile_shift;
+  at.item_shift = meta + p.off_item_shift;
+  return at;
+}
+
 void launch_attention(hipStream_t s, const AttnArgs& a) {
   if (a.n_units <= 0) return;
-  if (a.hd == 128) attn_detail::launch<128>(s, a);
-  else attn_detail::launch<64>(s, a);
+  if (a.hd == 128) a.windowed ? attn_detail::launch<128, true>(s, a) : attn_detail::launch<128, false>(s, a);
+  else a.windowed ? attn_detail::launch<64, true>(s, a) : attn_detail::launch<64, false>(s, a);
 }
 
 void launch_attn_merge(hipStream_t s, const AttnArgs& a) {

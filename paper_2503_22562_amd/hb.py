@@ -26,7 +26,9 @@ EXPORTED = ("hb_create_layer", "hb_destroy_layer", "hb_append_kv", "hb_run_itera
             "hb_create_model", "hb_destroy_model", "hb_model_layer", "hb_run_model",
             "hb_set_kernel_timing", "hb_kernel_times", "hb_kernel_name", "hb_layer_stage", "hb_last_error",
             "hb_gemm_tile_count", "hb_plan_gemms", "hb_layer_gemm_plans", "hb_run_iteration_noalloc",
-            "hb_measure_device_rates")
+            "hb_measure_device_rates", "hb_set_attention_window", "hb_window_dead_blocks", "hb_create_attention",
+            "hb_destroy_attention", "hb_plan_attention", "hb_run_attention", "hb_copy_blocks", "hb_copy_model_blocks",
+            "hb_plan_compaction")
 HB_LAT_FEATURES = 5
 
 
@@ -167,6 +169,25 @@ def load() -> C.CDLL:
     lib.hb_layer_gemm_plans.restype = st
     lib.hb_measure_device_rates.argtypes = [C.c_void_p, C.c_int64, C.c_void_p, C.POINTER(hb_device_rates)]
     lib.hb_measure_device_rates.restype = st
+    i32p = C.POINTER(C.c_int32)
+    lib.hb_set_attention_window.argtypes = [C.c_void_p, C.c_int32, C.c_int32]
+    lib.hb_set_attention_window.restype = st
+    lib.hb_window_dead_blocks.argtypes = [C.c_int32, C.c_int32, C.c_int32, i32p, i32p]
+    lib.hb_window_dead_blocks.restype = st
+    lib.hb_create_attention.argtypes = [C.POINTER(hb_layer_config), C.c_int32, C.c_void_p, C.POINTER(C.c_void_p)]
+    lib.hb_create_attention.restype = st
+    lib.hb_destroy_attention.argtypes = [C.c_void_p]
+    lib.hb_destroy_attention.restype = None
+    lib.hb_plan_attention.argtypes = [C.c_void_p, C.c_int32, C.POINTER(hb_request), C.c_int32, C.c_int32]
+    lib.hb_plan_attention.restype = st
+    lib.hb_run_attention.argtypes = [C.c_void_p, C.POINTER(hb_kv_pool), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64]
+    lib.hb_run_attention.restype = st
+    for f in (lib.hb_copy_blocks, lib.hb_copy_model_blocks):
+        f.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32]
+        f.restype = st
+    lib.hb_plan_compaction.argtypes = [C.c_int32, C.POINTER(C.c_void_p), i32p, C.c_int32, C.c_void_p, C.c_void_p,
+                                       i32p, i32p]
+    lib.hb_plan_compaction.restype = st
     _lib = lib
     return lib
 
@@ -347,6 +368,117 @@ def hb_run_iteration_noalloc(layer: Layer, requests: Sequence[Tuple[int, int, It
         out_dtype = HB_OUT_F32 if x_out.dtype == torch.float32 else HB_OUT_BF16
     d, keep = _desc(requests, _ptr(x_in), _ptr(x_out), out_dtype)
     _check(load().hb_run_iteration_noalloc(layer.handle, C.byref(d)))
+
+
+def hb_set_attention_window(layer: Layer, window: int, sinks: int = 0) -> None:
+    """Sliding window of the layer's later iterations (0: every earlier key)."""
+    _check(load().hb_set_attention_window(layer.handle, int(window), int(sinks)))
+
+
+def hb_window_dead_blocks(context_len: int, window: int, sinks: int = 0) -> Tuple[int, int]:
+    """(first, count): the block-table entries that no row at a position >= context_len sees."""
+    first, count = C.c_int32(), C.c_int32()
+    _check(load().hb_window_dead_blocks(int(context_len), int(window), int(sinks), C.byref(first), C.byref(count)))
+    return first.value, count.value
+
+
+class Attention:
+    """Owns an hb_attention handle; n_tokens: rows of the current plan."""
+
+    def __init__(self, handle: C.c_void_p, cfg: hb_layer_config, num_blocks: int):
+        self.handle = handle
+        self.cfg = cfg
+        self.num_blocks = num_blocks
+        self.n_tokens = 0
+
+    def __del__(self):
+        try:
+            hb_destroy_attention(self)
+        except Exception:
+            pass
+
+
+def hb_create_attention(cfg: hb_layer_config, num_blocks: int, stream: Optional[int] = None) -> Attention:
+    if stream is None:
+        import torch
+        stream = torch.cuda.current_stream().cuda_stream
+    h = C.c_void_p()
+    _check(load().hb_create_attention(C.byref(cfg), int(num_blocks), C.c_void_p(stream), C.byref(h)))
+    return Attention(h, cfg, int(num_blocks))
+
+
+def hb_destroy_attention(attention: Attention) -> None:
+    if attention.handle is not None and attention.handle.value:
+        load().hb_destroy_attention(attention.handle)
+        attention.handle = None
+
+
+def hb_plan_attention(attention: Attention, requests: Sequence[Tuple[int, int, Iterable[int]]], window: int = 0,
+                      sinks: int = 0) -> None:
+    """requests: (chunk_len, context_len, block_table) per request, in row order."""
+    d, keep = _desc(requests, 0, 0, HB_OUT_BF16)
+    _check(load().hb_plan_attention(attention.handle, d.n_requests, d.requests, int(window), int(sinks)))
+    attention.n_tokens = sum(int(r[0]) for r in requests)
+
+
+def _rows(name: str, t, n: int, row: int) -> int:
+    """Row stride of n rows of `row` contiguous bf16 values ([n][heads][head_dim] or [n][heads * head_dim])."""
+    import torch
+    if t.dtype != torch.bfloat16 or not t.is_cuda:
+        raise ValueError(f"{name}: a bf16 tensor on the GPU, not {t.dtype} on {t.device}")
+    if t.dim() < 2 or t.shape[0] != n or t.numel() != n * row:
+        raise ValueError(f"{name}: {n} rows of {row} values, not {tuple(t.shape)}")
+    if n and not t[0].is_contiguous():
+        raise ValueError(f"{name}: the values of a row must be contiguous, strides {t.stride()}")
+    return int(t.stride(0)) if n > 1 else row
+
+
+def hb_run_attention(attention: Attention, q, k_pool, v_pool, out) -> None:
+    """q, out: bf16 [T][n_q_heads][head_dim] (or [T][n_q_heads * head_dim]), rows any multiple of 8 elements apart."""
+    import torch
+    c = attention.cfg
+    for name, p in (("k_pool", k_pool), ("v_pool", v_pool)):
+        if p.dtype != torch.bfloat16 or not p.is_cuda or not p.is_contiguous():
+            raise ValueError(f"{name}: a contiguous bf16 tensor on the GPU")
+        if p.shape[0] < attention.num_blocks or p.numel() != p.shape[0] * c.n_kv_heads * 16 * c.head_dim:
+            raise ValueError(f"{name}: at least {attention.num_blocks} blocks of {c.n_kv_heads} kv heads, "
+                             f"16 slots and {c.head_dim} dimensions, not {tuple(p.shape)}")
+    row = c.n_q_heads * c.head_dim
+    qs, os_ = (_rows(n, t, attention.n_tokens, row) for n, t in (("q", q), ("out", out)))
+    pool = hb_kv_pool(_ptr(k_pool), _ptr(v_pool), min(int(k_pool.shape[0]), int(v_pool.shape[0])))
+    _check(load().hb_run_attention(attention.handle, C.byref(pool), C.c_void_p(_ptr(q)), qs, C.c_void_p(_ptr(out)),
+                                   os_))
+
+
+def _block_pairs(src, dst):
+    s, d = _i32(src), _i32(dst)
+    if s.ndim != 1 or s.shape != d.shape:
+        raise ValueError(f"src and dst: one list of block ids each, of equal length, not {s.shape} and {d.shape}")
+    return s, d
+
+
+def hb_copy_blocks(layer: Layer, src, dst) -> None:
+    """Block dst[i] of the layer's pool takes the contents of block src[i]."""
+    s, d = _block_pairs(src, dst)
+    _check(load().hb_copy_blocks(layer.handle, s.ctypes.data, d.ctypes.data, len(s)))
+
+
+def hb_copy_model_blocks(model: Model, src, dst) -> None:
+    """hb_copy_blocks in the pools of every layer."""
+    s, d = _block_pairs(src, dst)
+    _check(load().hb_copy_model_blocks(model.handle, s.ctypes.data, d.ctypes.data, len(s)))
+
+
+def hb_plan_compaction(num_blocks: int, tables: Sequence[Iterable[int]]):
+    """(tables, src, dst, n_used): the tables over blocks [0, n_used), and the moves that make them true."""
+    ts = [np.array(t, dtype=np.int32).reshape(-1) for t in tables]
+    ptrs = (C.c_void_p * max(1, len(ts)))(*[t.ctypes.data for t in ts])
+    lens = _i32([len(t) for t in ts] or [0])
+    src, dst = (np.zeros(max(1, int(num_blocks) // 2), np.int32) for _ in range(2))
+    moves, used = C.c_int32(), C.c_int32()
+    _check(load().hb_plan_compaction(int(num_blocks), ptrs, lens.ctypes.data_as(C.POINTER(C.c_int32)), len(ts),
+                                     src.ctypes.data, dst.ctypes.data, C.byref(moves), C.byref(used)))
+    return ts, src[:moves.value], dst[:moves.value], used.value
 
 
 def hb_validate_batch(cfg: hb_layer_config, num_blocks: int, requests, x_in_ptr: int, x_out_ptr: int,

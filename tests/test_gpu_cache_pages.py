@@ -1,0 +1,296 @@
+"""Pages of the cache in use: hb_copy_blocks and its model form against NumPy, and
+whole runs that slide a window, give its dead blocks away, fork sequences and
+compact the pool, against runs that do none of it."""
+import numpy as np
+import pytest
+
+from hb_workloads import TINY, LayerShape, make_model_weights, make_weights
+
+pytestmark = pytest.mark.gpu
+
+
+def _bits(t):
+    import torch
+    return t.view(torch.int16).cpu().numpy()
+
+
+@pytest.mark.parametrize("nq,nkv,hd", [(1, 1, 64), (4, 2, 64), (6, 3, 128), (8, 8, 128), (40, 40, 128)])
+@pytest.mark.parametrize("n", [0, 1, 7, 320, 321, 1500])
+def test_copy(hb, nq, nkv, hd, n):
+    import torch
+    from paper_2503_22562_amd import hb as H
+    from paper_2503_22562_amd.harness import DeviceLayer
+    shape = LayerShape("copy", 64, nq, nkv, hd, 16, weight_seed=3)
+    nb = 2 * n + 11 if nkv < 40 else n + 60
+    dl = DeviceLayer(shape, make_weights(shape), nb, 16, 4, pool_fill_bits=None)
+    for p in (dl.k_pool, dl.v_pool):  # every bit pattern, NaNs among them
+        p.view(torch.int16).random_(-(1 << 15), 1 << 15)
+    want = [_bits(p).copy() for p in (dl.k_pool, dl.v_pool)]
+    rng = np.random.default_rng(n + nkv)
+    ids = rng.permutation(nb).astype(np.int32)
+    dst, rest = ids[:n], ids[n:]
+    src = rest[rng.integers(0, len(rest), n)] if n else rest[:0]  # sources may occur again
+    H.hb_copy_blocks(dl.layer, src, dst)
+    for p, w in zip((dl.k_pool, dl.v_pool), want):
+        w[dst] = w[src]
+        assert np.array_equal(_bits(p), w)
+
+
+def test_copy_in_every_layer_of_a_model(hb):
+    import torch
+    from paper_2503_22562_amd import hb as H
+    from paper_2503_22562_amd.harness import DeviceModel
+    shape = LayerShape("copy", 64, 2, 2, 64, 16, weight_seed=3)
+    mw = make_model_weights(shape, 1, 8)
+    mw["layers"] = mw["layers"] * 67  # more layers than one launch takes
+    dm = DeviceModel(shape, mw, 900, 16, 4)
+    for p in [p for layer in dm.pools for p in layer]:
+        p.view(torch.int16).random_(-(1 << 15), 1 << 15)
+    rng = np.random.default_rng(1)
+    for n in (3, 400):
+        want = [[_bits(p).copy() for p in layer] for layer in dm.pools]
+        ids = rng.permutation(900).astype(np.int32)
+        H.hb_copy_model_blocks(dm.model, ids[:n], ids[n:2 * n])
+        for layer, w2 in zip(dm.pools, want):
+            for p, w in zip(layer, w2):
+                w[ids[n:2 * n]] = w[ids[:n]]
+                assert np.array_equal(_bits(p), w)
+
+
+def test_copy_refusals(hb):
+    import torch
+    from paper_2503_22562_amd import hb as H
+    from paper_2503_22562_amd.harness import DeviceLayer
+    dl = DeviceLayer(TINY, make_weights(TINY), 600, 16, 4)
+    dl.k_pool.normal_()
+    before = [_bits(p).copy() for p in (dl.k_pool, dl.v_pool)]
+    many = np.arange(300, dtype=np.int32)
+    for src, dst, status in (([0], [600], "RANGE"), ([-1], [0], "RANGE"), ([600], [0], "RANGE"), ([0], [-1], "RANGE"),
+                             ([5], [5], "INVALID"), ([0, 1], [2, 2], "INVALID"), ([0, 2], [2, 3], "INVALID"),
+                             ([2, 0], [3, 2], "INVALID"), (many, np.r_[many[1:] + 300, 299], "INVALID")):
+        with pytest.raises(H.HBError) as e:
+            H.hb_copy_blocks(dl.layer, src, dst)
+        assert e.value.status == getattr(H, "HB_ERR_" + status), (src, dst)
+    for src, dst in (([0, 1], [2]), ([[0]], [[1]])):
+        with pytest.raises(ValueError):
+            H.hb_copy_blocks(dl.layer, src, dst)
+    lib = H.load()
+    assert lib.hb_copy_blocks(dl.layer.handle, None, None, 1) == H.HB_ERR_INVALID
+    assert lib.hb_copy_blocks(dl.layer.handle, None, None, -1) == H.HB_ERR_INVALID
+    torch.cuda.synchronize()
+    assert all(np.array_equal(_bits(p), b) for p, b in zip((dl.k_pool, dl.v_pool), before))
+    # a refused list leaves nothing behind: the same blocks are copied, and written by an iteration, right after
+    H.hb_copy_blocks(dl.layer, [0, 1], [2, 3])
+    x = torch.randn(2, TINY.hidden, device="cuda").to(torch.bfloat16)
+    assert bool(torch.isfinite(dl.run([(1, 0, [5]), (1, 0, [2])], x)).all())
+
+
+# --- whole runs -----------------------------------------------------------------
+SHAPE = LayerShape("run", 256, 8, 2, 64, 688, weight_seed=5)
+
+
+class Pool:
+    """The caller's free list of one layer's or model's pool."""
+
+    def __init__(self, n, seed):
+        self.free = list(np.random.default_rng(seed).permutation(n))
+
+    def grow(self, table, tokens):
+        need = -(-tokens // 16) - len(table)
+        return np.r_[table, [self.free.pop() for _ in range(max(0, need))]].astype(np.int32)
+
+
+def _poison(pools, blocks):
+    import torch
+    idx = torch.as_tensor([int(b) for b in blocks], device="cuda")
+    for p in pools:
+        p[idx] = float("nan")
+
+
+@pytest.mark.parametrize("window,sinks", [(40, 4), (33, 20), (64, 0)])
+def test_a_sliding_run_needs_no_dead_block(hb, window, sinks):
+    """Chunked prefill and decodes of one sequence under a window, the dead blocks' contents destroyed and their
+    entries -1 after every call: bit for bit the run that keeps them."""
+    import torch
+    from paper_2503_22562_amd import hb as H
+    from paper_2503_22562_amd.harness import DeviceLayer
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(2)
+    steps = [100, 7, 90, 1, 1, 1, 30] + [1] * 20
+    xs = [torch.randn(c, SHAPE.hidden, device="cuda", generator=gen).to(torch.bfloat16) for c in steps]
+    outs = []
+    for free in (False, True):
+        dl = DeviceLayer(SHAPE, make_weights(SHAPE), 40, 128, 4)
+        H.hb_set_attention_window(dl.layer, window, sinks)
+        pool, table, n, ys, dead = Pool(40, 3), np.zeros(0, np.int32), 0, [], 0
+        for c, x in zip(steps, xs):
+            table = pool.grow(table, n + c)
+            ys.append(dl.run([(c, n, table)], x))
+            n += c
+            first, count = H.hb_window_dead_blocks(n, window, sinks)
+            gone = [b for b in table[first:first + count] if b >= 0]
+            if free and gone:
+                torch.cuda.synchronize()
+                _poison((dl.k_pool, dl.v_pool), gone)
+                table[first:first + count] = -1
+                dead += len(gone)
+        torch.cuda.synchronize()
+        outs.append(torch.cat(ys))
+    assert dead > 5 and bool(torch.isfinite(outs[0]).all())
+    assert torch.equal(outs[0], outs[1])
+
+
+def test_fork_compact_and_free(hb):
+    """A prompt's sequence is forked (shared full blocks, the partly filled one copied), both go on with different
+    tokens, a third request's blocks are given back, the pool is compacted, and all go on: as the two sequences run
+    apart with blocks of their own."""
+    import torch
+    from paper_2503_22562_amd import hb as H
+    from paper_2503_22562_amd.harness import DeviceLayer
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(4)
+    rand = lambda c: torch.randn(c, SHAPE.hidden, device="cuda", generator=gen).to(torch.bfloat16)
+    prompt, tails = rand(77), [rand(30), rand(30)]
+
+    def layer():
+        dl = DeviceLayer(SHAPE, make_weights(SHAPE), 64, 128, 4)
+        H.hb_set_attention_window(dl.layer, 60, 3)
+        return dl
+
+    def apart(tail):
+        dl = layer()
+        table = np.arange(10, 20, dtype=np.int32)
+        dl.run([(77, 0, table)], prompt)
+        return [dl.run([(1, 77 + i, table)], tail[i:i + 1].contiguous()).clone() for i in range(30)]
+
+    want = [apart(t) for t in tails]
+    dl, pool = layer(), Pool(64, 6)
+    bystander = pool.grow(np.zeros(0, np.int32), 300)
+    dl.run([(100, 0, bystander)], rand(100))
+    a = pool.grow(np.zeros(0, np.int32), 77)
+    dl.run([(77, 0, a)], prompt)
+    # fork
+    b = a.copy()
+    b[-1] = pool.free.pop()
+    H.hb_copy_blocks(dl.layer, a[-1:], b[-1:])
+    got = [[], []]
+    for i in range(30):
+        if i == 13:
+            # the bystander ends; compact what is left
+            tables, src, dst, used = H.hb_plan_compaction(64, [a, b])
+            assert len(src) and used <= 12
+            H.hb_copy_blocks(dl.layer, src, dst)
+            torch.cuda.synchronize()
+            _poison((dl.k_pool, dl.v_pool), range(used, 64))
+            a, b = tables
+            pool.free = list(range(63, used - 1, -1))
+        a, b = pool.grow(a, 78 + i), pool.grow(b, 78 + i)
+        x = torch.cat([tails[0][i:i + 1], tails[1][i:i + 1]])
+        y = dl.run([(1, 77 + i, a), (1, 77 + i, b)], x)
+        for s in range(2):
+            got[s].append(y[s:s + 1].clone())
+    torch.cuda.synchronize()
+    for s in range(2):
+        for i in range(30):
+            # one decode and two take different GEMM plans: each is within the layer's parity bar of the exact value
+            d = (got[s][i] - want[s][i]).double()
+            assert d.abs().max() <= 2 * 2e-2 and d.norm() <= 2 * 1e-2 * want[s][i].double().norm(), (s, i)
+
+
+def test_layers_of_different_windows_in_a_model(hb):
+    """hb_run_model over layers with windows of their own against each layer run by itself on the model's hidden
+    states; under windows in every layer the tables need no dead block."""
+    import torch
+    from paper_2503_22562_amd import hb as H
+    from paper_2503_22562_amd.harness import DeviceModel
+    mw = make_model_weights(SHAPE, 4, 200)
+    lens = [(90, 300), (1, 500), (1, 20), (5, 444)]
+    T = sum(c for c, _ in lens)
+    for windows in ([(0, 0), (50, 4), (0, 0), (120, 0)], [(50, 4), (33, 17), (50, 4), (120, 0)], [(64, 2)] * 4):
+        dm = DeviceModel(SHAPE, mw, 128, T, 4)
+        gen = torch.Generator(device="cuda")
+        gen.manual_seed(7)
+        for p in [p for layer in dm.pools for p in layer]:
+            p.normal_(0.0, 1.0, generator=gen)
+        perm, at, reqs = np.random.default_rng(8).permutation(128).astype(np.int32), 0, []
+        for l, (w, s) in enumerate(windows):
+            H.hb_set_attention_window(dm.model.layer(l), w, s)
+        for c, x in lens:
+            n = -(-(c + x) // 16)
+            t = perm[at:at + n].copy()
+            if all(w for w, _ in windows):  # dead in every layer
+                dead = set.intersection(*[set(range(f, f + k)) for f, k in
+                                          (H.hb_window_dead_blocks(x, w, s) for w, s in windows)])
+                t[sorted(dead)] = -1
+            reqs.append((c, x, t))
+            at += n
+        ids = np.arange(T) * 7 % 200
+        hidden = torch.empty((4, T, SHAPE.hidden), dtype=torch.bfloat16, device="cuda")
+        nxt, logits = dm.run(reqs, ids, hidden_states=hidden)
+        torch.cuda.synchronize()
+        assert bool(torch.isfinite(logits).all())
+        x = dm.embed[torch.from_numpy(ids).cuda()].contiguous()
+        for l in range(4):
+            y = torch.empty((T, SHAPE.hidden), dtype=torch.bfloat16, device="cuda")
+            H.hb_run_iteration(dm.model.layer(l), reqs, x, y)
+            torch.cuda.synchronize()
+            assert torch.equal(y, hidden[l]), l
+            x = hidden[l].contiguous()
+        if (0, 0) in windows:  # a layer that sees everything needs every block
+            bad = [(c, x, np.where(np.arange(len(t)) == 0, -1, t)) for c, x, t in reqs]
+            with pytest.raises(H.HBError) as e:
+                dm.run(bad, ids)
+            assert e.value.status == H.HB_ERR_RANGE
+
+
+def test_window_of_a_layer(hb):
+    """The layer's attention under a window against 64 bits on its own q and cache, through every entry that runs it;
+    a window that hides nothing, and the window taken off again, give the unwindowed bits."""
+    import torch
+    from attnref import assert_close, reference
+    from paper_2503_22562_amd import hb as H
+    from paper_2503_22562_amd.harness import DeviceLayer, bf16_bits, k_by_slot, v_by_slot
+    from hb_workloads import bf16_bits_to_f32
+    lens = [(90, 300), (1, 500), (1, 0), (5, 444)]
+    T = sum(c for c, _ in lens)
+    dl = DeviceLayer(SHAPE, make_weights(SHAPE), 128, T, 4)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(9)
+    for p in (dl.k_pool, dl.v_pool):
+        p.normal_(0.0, 1.0, generator=gen)
+    perm, at, reqs = np.random.default_rng(10).permutation(128).astype(np.int32), 0, []
+    for c, x in lens:
+        n = -(-(c + x) // 16)
+        reqs.append((c, x, perm[at:at + n].copy()))
+        at += n
+    x = torch.randn(T, SHAPE.hidden, device="cuda", generator=gen).to(torch.bfloat16)
+    plain = dl.run(reqs, x).clone()
+    for window, sinks in ((64, 4), (7, 0), (400, 30)):
+        H.hb_set_attention_window(dl.layer, window, sinks)
+        y = dl.run(reqs, x).clone()
+        q, o = (dl.stage(s, T).float().cpu().numpy().astype(np.float64).reshape(T, 8, 64)
+                for s in (H.HB_STAGE_Q, H.HB_STAGE_ATTN))
+        k, v = k_by_slot(bf16_bits(dl.k_pool)), v_by_slot(bf16_bits(dl.v_pool))
+        at = 0
+        for c, ctx, t in reqs:
+            kk, vv = (bf16_bits_to_f32(p[t].transpose(0, 2, 1, 3).reshape(-1, 2, 64)[:ctx + c]).astype(np.float64)
+                      for p in (k, v))
+            ref, pv = reference(q[at:at + c], kk, vv, np.arange(ctx, ctx + c), window, sinks)
+            assert_close(o[at:at + c], ref, pv, f"window {window} request ({c}, {ctx})")
+            at += c
+        assert not torch.equal(y, plain)
+        y2 = torch.full_like(y, float("nan"))
+        H.hb_run_iteration_noalloc(dl.layer, reqs, x, y2)
+        torch.cuda.synchronize()
+        assert torch.equal(y, y2)
+        cells = H.hb_profile_batches(dl.layer, [(reqs, x, y2)], warmup=1, iters=3)
+        assert cells["median_ms"][0] > 0 and torch.equal(y, y2)
+    for window, sinks in ((505, 0), (400, 101), (0, 3)):  # position 500 is the last
+        H.hb_set_attention_window(dl.layer, window, sinks)
+        assert torch.equal(dl.run(reqs, x), plain)
+    H.hb_set_attention_window(dl.layer, 10, 0)
+    for w, s in ((-1, 0), (0, -1), ((1 << 30) + 1, 0)):
+        with pytest.raises(H.HBError) as e:
+            H.hb_set_attention_window(dl.layer, w, s)
+        assert e.value.status == H.HB_ERR_INVALID
+    assert H.load().hb_set_attention_window(None, 1, 0) == H.HB_ERR_INVALID
