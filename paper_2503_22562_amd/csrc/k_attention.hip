@@ -146,6 +146,21 @@ __device__ __forceinline__ int window_edge(const AttnArgs& a, const AttnItem& it
 // Whether the window hides key j from the row at position pos.
 __device__ __forceinline__ bool hidden(const AttnArgs& a, int j, int pos) { return j <= pos - a.window && j >= a.sinks; }
 
+// -inf for the scores of the lane's eight keys j .. j + 7 that the row at `pos`
+// does not see: later ones, those from kv_end on, hidden ones. (Plain selects:
+// no short circuits, which would become branches.)
+template <bool WIN>
+__device__ __forceinline__ void mask_scores(float (&sv)[8], const AttnArgs& a, int j, int pos, int kv_end) {
+  const int lim = min(pos, kv_end - 1) - j;
+  const int far = WIN ? pos - a.window - j : 0, sinks = WIN ? a.sinks - j : 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    bool off = i > lim;
+    if (WIN) off |= bool((i <= far) & (i >= sinks));
+    sv[i] = off ? -INFINITY : sv[i];
+  }
+}
+
 // Write the result of one column: normalised bf16 output, or fp32 partials.
 template <int HD>
 __device__ __forceinline__ void store_column(const AttnArgs& a, const AttnItem& it, int c, const f32x4 (&o)[HD / 16],
@@ -256,14 +271,7 @@ __device__ __forceinline__ void wave_compute(const AttnArgs& a, const WaveStep<H
     for (int i = 0; i < 4; ++i) sv[4 * b + i] = s[b][i];
   const bool edge = WIN && j0 < window_edge(a, it);              // the window's far edge (wave-uniform)
   if (j0 + WSTEP > it.kv_end || j0 + WSTEP > it.pos0 || edge) {  // causal / tail masking (wave-uniform)
-    const int lim = min(pos, it.kv_end - 1);
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int j = j0 + 8 * grp + 4 * b + i;
-        if (j > lim || (WIN && hidden(a, j, pos))) sv[4 * b + i] = -INFINITY;
-      }
+    mask_scores<WIN>(sv, a, j0 + 8 * grp, pos, it.kv_end);
   }
   float ps;
   bf16x8 pf;
@@ -340,13 +348,10 @@ __device__ __forceinline__ void wave_run(const AttnArgs& a, const AttnItem& it, 
     wave_compute<HD, WIN>(a, B, it.kv_begin + WSTEP * (s + 1), it, pos, grp, a.scale_log2, qf, o, m, l);
     __builtin_amdgcn_sched_barrier(0);
   }
-  if (s + 1 < nsteps) {
-    wave_load(B, a, ids[0], ids[1], g, col, grp);
-    wave_compute<HD, WIN>(a, A, it.kv_begin + WSTEP * s, it, pos, grp, a.scale_log2, qf, o, m, l);
-    wave_compute<HD, WIN>(a, B, it.kv_begin + WSTEP * (s + 1), it, pos, grp, a.scale_log2, qf, o, m, l);
-  } else {
-    wave_compute<HD, WIN>(a, A, it.kv_begin + WSTEP * s, it, pos, grp, a.scale_log2, qf, o, m, l);
-  }
+  const bool two = s + 1 < nsteps;
+  if (two) wave_load(B, a, ids[0], ids[1], g, col, grp);
+  wave_compute<HD, WIN>(a, A, it.kv_begin + WSTEP * s, it, pos, grp, a.scale_log2, qf, o, m, l);
+  if (two) wave_compute<HD, WIN>(a, B, it.kv_begin + WSTEP * (s + 1), it, pos, grp, a.scale_log2, qf, o, m, l);
   l = rows_sum(l);
 }
 
@@ -357,35 +362,19 @@ __device__ __forceinline__ UnitShift shift_of(const int32_t* shifts, int idx) {
   else return {0, 0};
 }
 
-template <int HD, bool WIN>
-__device__ __forceinline__ void wave_item(const AttnArgs& a, const AttnItem& it, UnitShift sh, int lane) {
-  f32x4 o[HD / 16];
-  float m, l;
-  wave_run<HD, WIN>(a, it, sh, lane, o, m, l);
-  store_column<HD>(a, it, lane & 15, o, m, l, lane >> 4);
-}
-
 // A merged unit: its four items are consecutive key ranges of one (request,
 // kv head, positions), one per wave (an empty range contributes nothing).
 // The waves' results are combined in LDS with the log-sum-exp rule: with
 // M = max_w m_w, O = sum_w O_w 2^(m_w - M) and l = sum_w l_w 2^(m_w - M).
 // Wave w then finishes dimension tiles w DT/4 .. (w + 1) DT/4 - 1 of every
 // column and writes them, normalised, or as a partial result (O, M, l).
-template <int HD, bool WIN>
-__device__ __forceinline__ void merged_unit(const AttnArgs& a, int v, uint8_t* smem) {
+template <int HD>
+__device__ __forceinline__ void merge_waves(const AttnArgs& a, const AttnItem& it, const f32x4 (&o)[HD / 16], float m,
+                                            float l, uint8_t* smem) {
   constexpr int DT = HD / 16, PER = DT / WAVES;
   static_assert(PER * WAVES == DT, "dimension tiles per wave");
   const int lane = threadIdx.x & 63, wave = wave_id();
   const int col = lane & 15, grp = lane >> 4;
-  const AttnItem it = const_load(reinterpret_cast<const AttnItem*>(a.items) + WAVES * v + wave);
-  f32x4 o[DT];
-  float m = NEG_BIG, l = 0.f;
-  if (it.kv_begin < it.kv_end) {
-    wave_run<HD, WIN>(a, it, shift_of<WIN>(a.item_shift, WAVES * v + wave), lane, o, m, l);
-  } else {
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
   float* ml = reinterpret_cast<float*>(smem);                       // [wave][column] (m, l)
   f32x4* os = reinterpret_cast<f32x4*>(smem + WAVES * 16 * 2 * 4);  // [wave][dt][lane]
   if (grp == 0) {
@@ -444,8 +433,27 @@ __device__ __forceinline__ void merged_unit(const AttnArgs& a, int v, uint8_t* s
   }
 }
 
+// Four items, one per wave: separate ones, or the key ranges of a merged unit.
+// (The waves of the last unit of separate items may have none.)
+template <int HD, bool WIN>
+__device__ __forceinline__ void item_unit(const AttnArgs& a, int code, uint8_t* smem) {
+  const bool merged = code & kUnitMerged;
+  const int idx = (code & ~kUnitMerged) * WAVES + wave_id(), lane = threadIdx.x & 63;
+  const AttnItem it = const_load(reinterpret_cast<const AttnItem*>(a.items) + idx);
+  f32x4 o[HD / 16];
+  float m = NEG_BIG, l = 0.f;
+  if (it.kv_begin < it.kv_end) {
+    wave_run<HD, WIN>(a, it, shift_of<WIN>(a.item_shift, idx), lane, o, m, l);
+    if (!merged) store_column<HD>(a, it, lane & 15, o, m, l, lane >> 4);
+  } else if (merged) {
+#pragma unroll
+    for (int dt = 0; dt < HD / 16; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  if (merged) merge_waves<HD>(a, it, o, m, l, smem);
+}
+
 // ---------------------------------------------------------------------------
-// chunk tile: 256 columns, K/V staged in an LDS ring by the DMA path
+// chunk tile: 128 columns, K/V staged in an LDS ring by the DMA path
 // ---------------------------------------------------------------------------
 constexpr int TSTEP = 32;    // keys per tile step = 2 pool blocks
 constexpr int TSTAGES = 4;   // LDS ring depth of the tile path
@@ -544,16 +552,7 @@ __device__ __forceinline__ bool tile_softmax(const AttnArgs& a, const f32x4 (&sc
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int i = 0; i < 4; ++i) sv[ct][4 * b + i] = sc[ct][b][i];
-    if (MASKED) {
-      const int lim = min(pos[ct], kv_end - 1);
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int j = j0 + 8 * grp + 4 * b + i;
-          if (j > lim || (WIN && hidden(a, j, pos[ct]))) sv[ct][4 * b + i] = -INFINITY;
-        }
-    }
+    if (MASKED) mask_scores<WIN>(sv[ct], a, j0 + 8 * grp, pos[ct], kv_end);
     rescale |= softmax_fast<8>(sv[ct], scale, m[ct], ps[ct], p[ct]);
   }
   return rescale;
@@ -570,7 +569,7 @@ __device__ __forceinline__ void tile_pv(f32x4 (&o)[CT][HD / 16], const u32x4 (&v
 // One key step of a tile. The scores of this step (sc_cur) were formed one
 // step earlier; while their softmax runs on the vector ALUs, the next step's
 // scores go to the matrix cores (sc_next), so the two overlap within the wave.
-template <int HD, int CT, bool WIN, bool MASKED, bool LAST>
+template <int HD, int CT, bool WIN, bool MASKED>
 __device__ __forceinline__ void tile_step(const AttnArgs& a, const AttnItem& it, uint8_t* smem, int kt, int nsteps,
                                           const BlockIds<WIN>& blocks, int kb0, int& next_id, int wave, int lane,
                                           int k_lane, int v_lane, const bf16x8 (&qf)[CT][HD / 32],
@@ -582,16 +581,16 @@ __device__ __forceinline__ void tile_step(const AttnArgs& a, const AttnItem& it,
   const int j0 = it.kv_begin + TSTEP * kt;
   u32x4 vf[HD / 16];
   tile_read_v<HD>(vf, smem + (kt % TSTAGES) * TG::STAGE, v_lane);
-  if (!LAST) {
-    // step kt + 1 complete (the one issued after it may stay in flight); the
-    // ring slot of step kt - 1 is free for step kt + TSTAGES - 1
-    if (kt + 2 < nsteps) wait_vmcnt<TG::LOADS>();
-    else wait_vmcnt<0>();
-    __builtin_amdgcn_s_barrier();
-    if (kt + TSTAGES - 1 < nsteps) {
-      tile_issue<HD>(smem + ((kt + TSTAGES - 1) % TSTAGES) * TG::STAGE, a, next_id, it.kv_head, wave, lane);
-      if (kt + TSTAGES < nsteps) next_id = blocks.at(kb0 + 2 * (kt + TSTAGES) + (wave & 1));
-    }
+  // step kt + 1 complete (the one issued after it may stay in flight); the
+  // ring slot of step kt - 1 is free for step kt + TSTAGES - 1
+  if (kt + 2 < nsteps) wait_vmcnt<TG::LOADS>();
+  else wait_vmcnt<0>();
+  __builtin_amdgcn_s_barrier();
+  if (kt + TSTAGES - 1 < nsteps) {
+    tile_issue<HD>(smem + ((kt + TSTAGES - 1) % TSTAGES) * TG::STAGE, a, next_id, it.kv_head, wave, lane);
+    if (kt + TSTAGES < nsteps) next_id = blocks.at(kb0 + 2 * (kt + TSTAGES) + (wave & 1));
+  }
+  {
     bf16x8 kf[2][HD / 32];
     tile_read_k<HD>(kf, smem + ((kt + 1) % TSTAGES) * TG::STAGE, k_lane);
     tile_scores<HD, CT>(sc_next, kf, qf);
@@ -686,36 +685,30 @@ __device__ __forceinline__ void tile_unit(const AttnArgs& a, const AttnItem& it,
     tile_read_k<HD>(kf, smem, k_lane);
     tile_scores<HD, CT>(sa, kf, qf);
   }
-  // steps alternate the two score buffers; the last step is peeled
-  auto step = [&](auto masked, auto last, int t, f32x4(&cur)[CT][2], f32x4(&next)[CT][2]) {
-    tile_step<HD, CT, WIN, decltype(masked)::value, decltype(last)::value>(
-        a, it, smem, t, nsteps, blocks, kb0, next_id, wave, lane, k_lane, v_lane, qf, pos, o, m, l, cur, next);
+  // Steps alternate the two score buffers. The last step forms the scores of a
+  // step that does not exist, from whatever its ring slot holds, and nobody
+  // reads them: a copy of the step's code without them costs more, in
+  // instructions that a short tile runs once and has to fetch.
+  auto step = [&](auto masked, int t, f32x4(&cur)[CT][2], f32x4(&next)[CT][2]) {
+    tile_step<HD, CT, WIN, decltype(masked)::value>(a, it, smem, t, nsteps, blocks, kb0, next_id, wave, lane, k_lane,
+                                                    v_lane, qf, pos, o, m, l, cur, next);
   };
   constexpr std::true_type yes{};
   constexpr std::false_type no{};
+  // first step with no key that the window hides from some row
+  const int near = WIN ? (window_edge(a, it) - it.kv_begin + TSTEP - 1) / TSTEP : 0;
   int kt = 0;
-  if (WIN) {
-    // steps with keys that the window hides from some row
-    const int far = (window_edge(a, it) - it.kv_begin + TSTEP - 1) / TSTEP;
-    for (; kt < far && kt + 2 < nsteps; kt += 2) {
-      step(yes, no, kt, sa, sb);
-      step(yes, no, kt + 1, sb, sa);
+  while (kt + 2 <= nsteps) {  // masked steps, unmasked ones, masked ones (each part may be empty)
+    for (; kt >= near && kt + 2 <= full; kt += 2) {
+      step(no, kt, sa, sb);
+      step(no, kt + 1, sb, sa);
+    }
+    for (; kt + 2 <= nsteps && !(kt >= near && kt + 2 <= full); kt += 2) {
+      step(yes, kt, sa, sb);
+      step(yes, kt + 1, sb, sa);
     }
   }
-  for (; kt + 2 <= full && kt + 2 < nsteps; kt += 2) {
-    step(no, no, kt, sa, sb);
-    step(no, no, kt + 1, sb, sa);
-  }
-  for (; kt + 2 < nsteps; kt += 2) {
-    step(yes, no, kt, sa, sb);
-    step(yes, no, kt + 1, sb, sa);
-  }
-  if (kt + 1 < nsteps) {
-    step(yes, no, kt, sa, sb);
-    step(yes, yes, kt + 1, sb, sa);
-  } else {
-    step(yes, yes, kt, sa, sb);
-  }
+  if (kt < nsteps) step(yes, kt, sa, sb);
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) store_column<HD>(a, it, 32 * wave + 16 * ct + col, o[ct], m[ct], rows_sum(l[ct]), grp);
 }
@@ -727,15 +720,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_kernel(AttnArgs a) {
   if (unit >= 0) {
     tile_unit<HD, WIN>(a, const_load(reinterpret_cast<const AttnItem*>(a.tiles) + unit),
                        shift_of<WIN>(a.tile_shift, unit), smem);
-  } else if ((-unit - 1) & kUnitMerged) {
-    merged_unit<HD, WIN>(a, (-unit - 1) & ~kUnitMerged, smem);
   } else {
-    const int idx = (-unit - 1) * WAVES + wave_id();
-    if (idx < a.n_items) {
-      const AttnItem it = const_load(reinterpret_cast<const AttnItem*>(a.items) + idx);
-      if (it.kv_begin < it.kv_end)
-        wave_item<HD, WIN>(a, it, shift_of<WIN>(a.item_shift, idx), threadIdx.x & 63);
-    }
+    item_unit<HD, WIN>(a, -unit - 1, smem);
   }
 }
 

@@ -8,10 +8,20 @@ namespace hb {
 namespace {
 
 // pool[dst] = pool[src], a block's n_kv heads at a time: one contiguous run of
-// 32 n_kv hd bytes in the K pool and one in the V pool. A workgroup copies up to
-// kCopyVecs 16-byte vectors per thread of one run, all of its loads in flight
-// before its first store. Bound by HBM: every byte is read once and written once.
-constexpr int kCopyThreads = 256, kCopyVecs = 8;
+// 32 n_kv hd bytes in the K pool and one in the V pool. A workgroup copies two
+// 16-byte vectors per thread, 8 KB, of one run; its neighbours take the rest of
+// the run, the block's other runs (V, then the other layers), then the next
+// pair. Bound by HBM: every byte is read once and written once. Bytes moved per
+// second (read + write; torch's copy of 4 GiB: 5.4 TB/s):
+//   9000 pairs of 2 x 32 KB         6.0 TB/s, 195 us
+//   48 pairs in 32 layers           6.6 TB/s, 30.5 us
+//   4000 pairs of 2 x 4 KB          6.5 TB/s, 10.1 us
+// Eight vectors per thread leave too few workgroups in flight (4.0, 3.6 and 2.7
+// TB/s); four are as fast on large lists and slower on short ones (300 pairs 5.7
+// against 4.8 us). Stores are non-temporal, as they displace the next pairs'
+// lines otherwise (5.5 -> 6.0 TB/s); non-temporal loads cost up to a third on
+// lists that fit the caches.
+constexpr int kCopyThreads = 256, kCopyVecs = 2;
 
 struct InlinePairs {
   int32_t s[kCopyInlinePairs], d[kCopyInlinePairs];
@@ -25,10 +35,11 @@ struct ListedPairs {
 };
 
 template <typename Pairs>
-__global__ __launch_bounds__(kCopyThreads) void copy_blocks_kernel(CopyPools pools, Pairs pairs, int vecs, int parts) {
-  const int pair = blockIdx.x / parts, part = blockIdx.x - pair * parts;
-  const int layer = blockIdx.y >> 1;
-  u32x4* pool = static_cast<u32x4*>((blockIdx.y & 1) ? pools.v[layer] : pools.k[layer]);
+__global__ __launch_bounds__(kCopyThreads) void copy_blocks_kernel(CopyPools pools, int n_pools, Pairs pairs, int vecs,
+                                                                   int parts) {
+  const int run = blockIdx.x / parts, part = blockIdx.x - run * parts;
+  const int pair = run / (2 * n_pools), side = run - pair * 2 * n_pools;  // K and V of layer 0, of layer 1, ...
+  u32x4* pool = static_cast<u32x4*>((side & 1) ? pools.v[side >> 1] : pools.k[side >> 1]);
   const u32x4* s = pool + (size_t)pairs.src(pair) * vecs;
   u32x4* d = pool + (size_t)pairs.dst(pair) * vecs;
   const int i0 = part * kCopyThreads * kCopyVecs + threadIdx.x;
@@ -38,35 +49,34 @@ __global__ __launch_bounds__(kCopyThreads) void copy_blocks_kernel(CopyPools poo
     if (i0 + k * kCopyThreads < vecs) v[k] = s[i0 + k * kCopyThreads];
 #pragma unroll
   for (int k = 0; k < kCopyVecs; ++k)
-    if (i0 + k * kCopyThreads < vecs) d[i0 + k * kCopyThreads] = v[k];
+    if (i0 + k * kCopyThreads < vecs) __builtin_nontemporal_store(v[k], d + i0 + k * kCopyThreads);
 }
 
-// Launches of at most 2^20 workgroups along the pairs (a grid holds fewer than 2^32 threads).
+// Launches of at most 2^20 workgroups (a grid holds fewer than 2^32 threads).
 template <typename F>
-void for_pairs(int n, int nkv, int hd, F&& launch) {
+void for_pairs(int n, int n_pools, int nkv, int hd, F&& launch) {
   const int vecs = nkv * hd * 2, parts = (vecs + kCopyThreads * kCopyVecs - 1) / (kCopyThreads * kCopyVecs);
-  const int most = std::max(1, (1 << 20) / parts);
-  for (int i = 0; i < n; i += most) launch(i, std::min(most, n - i) * parts, vecs, parts);
+  const int per_pair = 2 * n_pools * parts, most = std::max(1, (1 << 20) / per_pair);
+  for (int i = 0; i < n; i += most) launch(i, std::min(most, n - i) * per_pair, vecs, parts);
 }
 
 }  // namespace
 
 void launch_copy_blocks(hipStream_t s, const CopyPools& pools, int n_pools, const int32_t* src, const int32_t* dst,
                         int n, int nkv, int hd) {
-  for_pairs(n, nkv, hd, [&](int i, int groups, int vecs, int parts) {
-    copy_blocks_kernel<<<dim3(groups, 2 * n_pools), kCopyThreads, 0, s>>>(pools, ListedPairs{src + i, dst + i}, vecs,
-                                                                         parts);
+  for_pairs(n, n_pools, nkv, hd, [&](int i, int groups, int vecs, int parts) {
+    copy_blocks_kernel<<<groups, kCopyThreads, 0, s>>>(pools, n_pools, ListedPairs{src + i, dst + i}, vecs, parts);
   });
 }
 
 void launch_copy_blocks_inline(hipStream_t s, const CopyPools& pools, int n_pools, const int32_t* src,
                                const int32_t* dst, int n, int nkv, int hd) {
-  InlinePairs p{};
-  std::copy(src, src + n, p.s);
-  std::copy(dst, dst + n, p.d);
-  for_pairs(n, nkv, hd, [&](int i, int groups, int vecs, int parts) {
-    (void)i;  // n <= kCopyInlinePairs: one launch
-    copy_blocks_kernel<<<dim3(groups, 2 * n_pools), kCopyThreads, 0, s>>>(pools, p, vecs, parts);
+  for_pairs(n, n_pools, nkv, hd, [&](int i, int groups, int vecs, int parts) {
+    InlinePairs p{};
+    const int m = groups / (2 * n_pools * parts);
+    std::copy(src + i, src + i + m, p.s);
+    std::copy(dst + i, dst + i + m, p.d);
+    copy_blocks_kernel<<<groups, kCopyThreads, 0, s>>>(pools, n_pools, p, vecs, parts);
   });
 }
 

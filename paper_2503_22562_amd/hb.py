@@ -389,6 +389,8 @@ class Attention:
         self.handle = handle
         self.cfg = cfg
         self.num_blocks = num_blocks
+        self.row = cfg.n_q_heads * cfg.head_dim             # values of a row of q
+        self.block_values = cfg.n_kv_heads * 16 * cfg.head_dim  # values of a block of one pool
         self.n_tokens = 0
 
     def __del__(self):
@@ -421,33 +423,39 @@ def hb_plan_attention(attention: Attention, requests: Sequence[Tuple[int, int, I
     attention.n_tokens = sum(int(r[0]) for r in requests)
 
 
-def _rows(name: str, t, n: int, row: int) -> int:
+def _rows(name: str, t, n: int, row: int, bf16) -> int:
     """Row stride of n rows of `row` contiguous bf16 values ([n][heads][head_dim] or [n][heads * head_dim])."""
-    import torch
-    if t.dtype != torch.bfloat16 or not t.is_cuda:
+    if t.dtype != bf16 or not t.is_cuda:
         raise ValueError(f"{name}: a bf16 tensor on the GPU, not {t.dtype} on {t.device}")
-    if t.dim() < 2 or t.shape[0] != n or t.numel() != n * row:
+    if t.numel() != n * row or t.dim() < 2 or t.shape[0] != n:
         raise ValueError(f"{name}: {n} rows of {row} values, not {tuple(t.shape)}")
-    if n and not t[0].is_contiguous():
-        raise ValueError(f"{name}: the values of a row must be contiguous, strides {t.stride()}")
-    return int(t.stride(0)) if n > 1 else row
+    if t.is_contiguous():
+        return row
+    shape, stride = t.shape, t.stride()
+    run = 1
+    for size, step in zip(shape[:0:-1], stride[:0:-1]):
+        if size != 1 and step != run:
+            raise ValueError(f"{name}: the values of a row must be contiguous, strides {stride}")
+        run *= size
+    return stride[0] if n > 1 else row
 
 
 def hb_run_attention(attention: Attention, q, k_pool, v_pool, out) -> None:
     """q, out: bf16 [T][n_q_heads][head_dim] (or [T][n_q_heads * head_dim]), rows any multiple of 8 elements apart."""
-    import torch
-    c = attention.cfg
+    from torch import bfloat16
+    blocks = attention.num_blocks
     for name, p in (("k_pool", k_pool), ("v_pool", v_pool)):
-        if p.dtype != torch.bfloat16 or not p.is_cuda or not p.is_contiguous():
+        if p.dtype != bfloat16 or not p.is_cuda or not p.is_contiguous():
             raise ValueError(f"{name}: a contiguous bf16 tensor on the GPU")
-        if p.shape[0] < attention.num_blocks or p.numel() != p.shape[0] * c.n_kv_heads * 16 * c.head_dim:
-            raise ValueError(f"{name}: at least {attention.num_blocks} blocks of {c.n_kv_heads} kv heads, "
-                             f"16 slots and {c.head_dim} dimensions, not {tuple(p.shape)}")
-    row = c.n_q_heads * c.head_dim
-    qs, os_ = (_rows(n, t, attention.n_tokens, row) for n, t in (("q", q), ("out", out)))
-    pool = hb_kv_pool(_ptr(k_pool), _ptr(v_pool), min(int(k_pool.shape[0]), int(v_pool.shape[0])))
-    _check(load().hb_run_attention(attention.handle, C.byref(pool), C.c_void_p(_ptr(q)), qs, C.c_void_p(_ptr(out)),
-                                   os_))
+        have = p.shape[0]
+        if have < blocks or p.numel() != have * attention.block_values:
+            raise ValueError(f"{name}: at least {blocks} blocks of {attention.block_values} values, not {tuple(p.shape)}")
+    n, row = attention.n_tokens, attention.row
+    qs, os_ = _rows("q", q, n, row, bfloat16), _rows("out", out, n, row, bfloat16)
+    status = load().hb_run_attention(attention.handle, hb_kv_pool(k_pool.data_ptr(), v_pool.data_ptr(), blocks),
+                                     q.data_ptr(), qs, out.data_ptr(), os_)
+    if status:
+        _check(status)
 
 
 def _block_pairs(src, dst):
