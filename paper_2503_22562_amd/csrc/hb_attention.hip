@@ -34,6 +34,7 @@ struct hb_attention {
   hipStream_t stream = nullptr;
   PlanOptions opt;
   Plan plan, next;  // the current plan, and the one being built
+  RecordPlan records, next_records;
   bool planned = false;
   int32_t* meta = nullptr;  // the current plan's metadata; in stream order with the runs that read it
   size_t meta_cap = 0;      // int32
@@ -88,7 +89,8 @@ hb_status plan_attention(hb_attention* a, int n, const hb_request* requests, int
   if (st != HB_OK) return st;
   const hb_batch_desc desc{n, requests, nullptr, nullptr, HB_OUT_BF16};
   build_plan(a->d, &desc, a->cu_count, &a->next, opt);
-  const size_t words = a->next.meta.size();
+  build_records(a->next, &a->next_records);
+  const size_t words = a->next_records.meta.size();
   PlanStage& s = a->stage[a->stage_next];
   if (s.pending) {
     if (hipEventSynchronize(s.copied) != hipSuccess) return fail(HB_ERR_HIP, "plan staging wait failed");
@@ -121,7 +123,7 @@ hb_status plan_attention(hb_attention* a, int n, const hb_request* requests, int
     if (!regrow(a, (void**)&a->meta, cap * sizeof(int32_t))) return fail(HB_ERR_OOM, "plan of %zu B", cap * 4);
     a->meta_cap = cap;
   }
-  std::memcpy(s.host, a->next.meta.data(), words * sizeof(int32_t));
+  std::memcpy(s.host, a->next_records.meta.data(), words * sizeof(int32_t));
   a->planned = false;
   if (words > 0) {
     launch_copy_words(a->stream, s.host, a->meta, words);
@@ -132,6 +134,7 @@ hb_status plan_attention(hb_attention* a, int n, const hb_request* requests, int
     a->stage_next = (a->stage_next + 1) % kPlanStages;
   }
   std::swap(a->plan, a->next);
+  std::swap(a->records, a->next_records);
   a->planned = true;
   return HB_OK;
 }
@@ -152,6 +155,7 @@ hb_status hb_create_attention(const hb_layer_config* cfg, int32_t num_blocks, vo
     auto bail = [&](hb_status s) { free_attention(a); return s; };
     a->d = d;
     a->num_blocks = num_blocks;
+    a->opt.fit_items = true;
     a->stream = static_cast<hipStream_t>(hip_stream);
     if (hipGetDevice(&a->device) != hipSuccess ||
         hipDeviceGetAttribute(&a->cu_count, hipDeviceAttributeMultiprocessorCount, a->device) != hipSuccess)
@@ -196,7 +200,7 @@ hb_status hb_run_attention(hb_attention* a, const hb_kv_pool* pool, const void* 
   const DeviceGuard on(a->device);
   const hb_status st = refuse_capture(a->stream);
   if (st != HB_OK) return st;
-  AttnArgs at = attention_args(a->d, p, a->meta, pool->k_pool, pool->v_pool, a->part_o, a->part_ml);
+  AttnArgs at = attention_args(a->d, p, a->meta, pool->k_pool, pool->v_pool, a->part_o, a->part_ml, &a->records);
   at.q = static_cast<const uint16_t*>(q);
   at.o = static_cast<uint16_t*>(out);
   at.q_stride = q_stride;

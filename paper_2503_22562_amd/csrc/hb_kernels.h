@@ -157,11 +157,14 @@ struct AttnArgs {
   int window, sinks, sink_blocks;
   const int32_t* tile_shift;
   const int32_t* item_shift;
+  // the units as records (UnitRec), in place of tiles, items, units, req_bt and the shifts; or null
+  const int32_t* records;
 };
-// The arguments of a plan's attention: its uploaded metadata, the pools and the
-// split partials. q, o and their strides are left to the caller.
+// The arguments of a plan's attention: its uploaded metadata (records: as
+// build_records lays it out, else the plan's own), the pools and the split
+// partials. q, o and their strides are left to the caller.
 AttnArgs attention_args(const Dims& d, const Plan& p, const int32_t* meta, const void* k_pool, const void* v_pool,
-                        float* part_o, float* part_ml);
+                        float* part_o, float* part_ml, const RecordPlan* records = nullptr);
 void launch_attention(hipStream_t s, const AttnArgs& a);
 void launch_attn_merge(hipStream_t s, const AttnArgs& a);
 

@@ -2,6 +2,7 @@
 #include "hb_plan.h"
 
 #include <algorithm>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -235,6 +236,30 @@ void iteration_work(const Dims& d, const hb_request* reqs, int n, double* flops,
 
 static int round_up(int64_t x, int m) { return (int)((x + m - 1) / m * m); }
 
+// Split length of a launch of item ranges (lengths, each in nkv kv heads) that
+// fits one round of workgroups, one per CU; 0 where it does not.
+// A range of at most 576 keys stays one unit: its four waves, of up to 192 keys,
+// are done before a merge kernel would be (cold caches, 300 keys 12.2 -> 9.3 us,
+// 8 decodes behind a 500-key window 13.3 -> 11.8; at 1000 keys a unit takes 15.6
+// and the split 13.0). Longer ones are split as finely as one round allows (4
+// decodes of 3000 keys, 192 instead of 128 units 18.8 -> 17.4 us; a second
+// round costs more than it divides: 1 x 20000 keys on eight heads, 320 units of
+// 128 keys a wave 28.5, 216 of 192 23.1), but no finer than sqrt(keys): parts
+// cost the merge about as much as a wave's keys cost it (1 x 30000 keys on one
+// head, 64 keys a wave and 118 parts 25.0 us, 192 and 40 20.8).
+static int fit_item_split(const std::vector<int>& lengths, int nkv, int cus) {
+  int longest = 0;
+  for (int n : lengths) longest = std::max(longest, n);
+  if ((int64_t)lengths.size() * nkv > cus || longest == 0) return 0;
+  if (longest <= 576) return round_up((longest + kItemsPerUnit - 1) / kItemsPerUnit, 64);
+  for (int S = round_up((int64_t)std::ceil(std::sqrt((double)longest)), 64); S <= 1024; S += 64) {
+    int64_t units = 0;
+    for (int n : lengths) units += (n + (int64_t)S * kItemsPerUnit - 1) / (S * kItemsPerUnit);
+    if (units * nkv <= cus) return S;
+  }
+  return 0;
+}
+
 void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p, const PlanOptions& opt) {
   const int R = desc->n_requests;
   const hb_request* rq = desc->requests;
@@ -259,11 +284,14 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   // path; decodes and short chunks become 16-column wave items.
   auto is_tile = [&](int r) { return (int64_t)rq[r].chunk_len * d.G >= kTileCols / 2; };
   double tile_keys = 0, item_keys = 0;
+  std::vector<int> item_lengths;  // of one kv head
   for (int r = 0; r < R; ++r) {
     const int c = rq[r].chunk_len, x = rq[r].context_len, w = is_tile(r) ? d.BQ : d.P;
-    for (int i0 = 0; i0 < c; i0 += w)
-      (is_tile(r) ? tile_keys : item_keys) +=
-          (double)d.nkv * (x + std::min(c, i0 + w) - 16 * dead_blocks(win, x + i0).count);
+    for (int i0 = 0; i0 < c; i0 += w) {
+      const int len = x + std::min(c, i0 + w) - 16 * dead_blocks(win, x + i0).count;
+      (is_tile(r) ? tile_keys : item_keys) += (double)d.nkv * len;
+      if (opt.fit_items && !is_tile(r)) item_lengths.push_back(len);
+    }
   }
   // split lengths (multiples of 64 keys): about one round of tile workgroups
   // (each split also writes kTileCols columns of fp32 partials). Items: a
@@ -296,7 +324,9 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   const int S_t_auto = std::max(1024, round_up((int64_t)std::min(s_t, 1.0e9) + 1, 64));
   const int S_t = opt.split_tile > 0 ? round_up(opt.split_tile, 64) : S_t_auto;
   const int S_i_fill = std::min(1024, std::max(opt.min_item, round_up((int64_t)(item_keys * d.hd / 128 / (2.8 * cus)), 64)));
+  const int S_i_fit = tile_keys > 0 ? 0 : fit_item_split(item_lengths, d.nkv, cus);
   const int S_i = opt.split_item > 0 ? round_up(opt.split_item, 64)
+                  : S_i_fit > 0      ? S_i_fit
                                      : std::max(S_i_fill, round_up((int64_t)(item_keys / (16.0 * cus)) + 1, 64));
   p->split_tile = S_t;
   p->split_item = S_i;
@@ -503,6 +533,47 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   if (!groups.empty()) std::memcpy(m + p->off_groups, groups.data(), sizeof(MergeGroup) * groups.size());
   if (!merge.empty()) std::memcpy(m + p->off_merge, merge.data(), sizeof(int32_t) * merge.size());
   iteration_work(d, rq, R, &p->flops, &p->bytes, win);
+}
+
+void build_records(const Plan& p, RecordPlan* out) {
+  const int32_t* m = p.meta.data();
+  const int n_bt = p.off_tiles - p.off_bt;  // with its padding
+  int off = 16 * 4 * p.n_units;
+  out->off_bt = off;      off += n_bt;
+  out->off_groups = off;  off += align16(8 * p.n_groups);
+  out->off_merge = off;   off += align16(p.n_merge_units);
+  out->meta.assign(off, 0);
+  if (off == 0) return;
+  int32_t* o = out->meta.data();
+  std::memcpy(o + out->off_bt, m + p.off_bt, sizeof(int32_t) * n_bt);
+  std::memcpy(o + out->off_groups, m + p.off_groups, sizeof(MergeGroup) * p.n_groups);
+  std::memcpy(o + out->off_merge, m + p.off_merge, sizeof(int32_t) * p.n_merge_units);
+  UnitRec* rec = reinterpret_cast<UnitRec*>(o);
+  const AttnItem* tiles = reinterpret_cast<const AttnItem*>(m + p.off_tiles);
+  const AttnItem* items = reinterpret_cast<const AttnItem*>(m + p.off_items);
+  for (int u = 0; u < p.n_units; ++u) {
+    const int code = m[p.off_units + u];
+    const bool tile = code >= 0;
+    const int unit = tile ? code : (-1 - code) & ~kUnitMerged;
+    for (int w = 0; w < kItemsPerUnit; ++w) {
+      UnitRec& r = rec[kItemsPerUnit * u + w];
+      const int i = tile ? unit : kItemsPerUnit * unit + w;
+      r.item = tile ? tiles[i] : items[i];
+      r.kind = tile ? kRecTile : ((-1 - code) & kUnitMerged) ? kRecMerged : kRecSingle;
+      r.sink = r.window = m[p.off_req_bt + r.item.req];
+      if (p.windowed) {
+        const int32_t* s = m + (tile ? p.off_tile_shift : p.off_item_shift) + 2 * i;
+        r.sink += s[0];
+        r.window += s[1];
+      }
+      if (r.item.kv_begin >= r.item.kv_end) continue;  // an empty item reads nothing
+      const int first = r.item.kv_begin / 16, last = (r.item.kv_end - 1) / 16;
+      for (int k = 0; k < 4; ++k) {
+        const int b = std::min(last, first + (tile ? 2 * k + (w & 1) : k));
+        r.ids[k] = m[p.off_bt + b + (b < p.sink_blocks ? r.sink : r.window)];
+      }
+    }
+  }
 }
 
 }  // namespace hb

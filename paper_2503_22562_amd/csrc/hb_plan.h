@@ -85,6 +85,22 @@ constexpr int kBtPad = 3;
 // a workgroup (one per wave): the attention workgroup has 4 waves.
 constexpr int kTileCols = 128;
 constexpr int kItemsPerUnit = 4;
+// One wave's work in one record, as hb_attention uploads it: four per
+// workgroup, in launch order, so that a wave has all it needs for its first
+// loads after one scalar load (units -> items -> req_bt -> bt otherwise).
+enum { kRecTile = 0, kRecSingle = 1, kRecMerged = 2 };
+struct UnitRec {
+  AttnItem item;  // of the tile, or the wave's own
+  int32_t kind;
+  // axis block i stands at bt[sink + i] below Plan.sink_blocks (windowed plans)
+  // and at bt[window + i] from there on
+  int32_t sink, window, pad;
+  // a tile's wave w: the blocks it copies in steps 0 .. 3 (block w % 2 of each);
+  // an item's: both blocks of steps 0 and 1 (past the range: its last block)
+  int32_t ids[4];
+};
+static_assert(sizeof(UnitRec) == 64, "packed as 16 int32");
+
 // Work unit encoding: u >= 0 is tile u; -1 - v runs items 4 w .. 4 w + 3 with
 // w = v & ~kUnitMerged, one per wave. Without kUnitMerged the four items are
 // independent. With it they are consecutive key ranges of one (request, kv
@@ -133,11 +149,22 @@ struct PlanOptions {
   int min_item = 64;   // least item split the planner chooses by itself
   int unit_block = 0;  // runs of tiles / item groups in the unit order (0: one per CU; < 0: fine interleave)
   Window window;
+  // split lengths of item-only launches that need one round of workgroups at
+  // most are chosen for that round (fit_item_split)
+  bool fit_items = false;
 };
 
 // Build the plan of a validated batch for a GPU with cu_count compute units.
 void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
                 const PlanOptions& opt = PlanOptions());
+
+// A plan as hb_attention uploads it: 4 n_units records, then the plan's block
+// ids, merge groups and merge units, at these offsets (int32).
+struct RecordPlan {
+  int off_bt = 0, off_groups = 0, off_merge = 0;
+  std::vector<int32_t> meta;
+};
+void build_records(const Plan& p, RecordPlan* out);
 
 // Algorithmic flops and HBM bytes of one iteration (what the method must
 // compute and move, not what an implementation happens to do).

@@ -132,9 +132,26 @@ struct BlockIds {
     return const_load(tab + i);
   }
 };
+// What a wave starts from: its item, where its block ids are, and (RECORDS)
+// the first four ids it needs.
+template <bool WIN, bool RECORDS>
+struct WaveStart {
+  AttnItem it;
+  BlockIds<WIN> blocks;
+  int32_t ids[4];
+};
 template <bool WIN>
-__device__ __forceinline__ BlockIds<WIN> block_ids(const AttnArgs& a, const AttnItem& it, UnitShift sh) {
-  return {a.bt + const_load(a.req_bt + it.req), (it.kv_end - 1) >> 4, a.sink_blocks, sh.sink, sh.window};
+__device__ __forceinline__ WaveStart<WIN, true> start_of(const AttnArgs& a, const UnitRec& r) {
+  return {r.item, {a.bt + (WIN ? 0 : r.window), (r.item.kv_end - 1) >> 4, a.sink_blocks, r.sink, r.window},
+          {r.ids[0], r.ids[1], r.ids[2], r.ids[3]}};
+}
+template <bool WIN>
+__device__ __forceinline__ WaveStart<WIN, false> start_of(const AttnArgs& a, const int32_t* items, const int32_t* shifts,
+                                                          int idx) {
+  const AttnItem it = const_load(reinterpret_cast<const AttnItem*>(items) + idx);
+  UnitShift sh = {0, 0};
+  if (WIN) sh = const_load(reinterpret_cast<const UnitShift*>(shifts) + idx);
+  return {it, {a.bt + const_load(a.req_bt + it.req), (it.kv_end - 1) >> 4, a.sink_blocks, sh.sink, sh.window}, {}};
 }
 
 // First key of the axis that the window hides from no row of the unit, sinks aside.
@@ -296,9 +313,11 @@ __device__ __forceinline__ void wave_compute(const AttnArgs& a, const WaveStep<H
 // One wave item's 16 columns over its key range: the unnormalised O^T, the
 // running maximum m and the weight sum l of the lane's column (l summed over
 // the column's four lanes; m is the same on all four).
-template <int HD, bool WIN>
-__device__ __forceinline__ void wave_run(const AttnArgs& a, const AttnItem& it, UnitShift sh, int lane,
+template <int HD, bool WIN, bool RECORDS>
+__device__ __forceinline__ void wave_run(const AttnArgs& a, const WaveStart<WIN, RECORDS>& start, int lane,
                                          f32x4 (&o)[HD / 16], float& m, float& l) {
+  const AttnItem& it = start.it;
+  const BlockIds<WIN>& blocks = start.blocks;
   const int G = a.nq / a.nkv;
   const int col = lane & 15, grp = lane >> 4;
   const int pi = col / G;
@@ -312,7 +331,6 @@ __device__ __forceinline__ void wave_run(const AttnArgs& a, const AttnItem& it, 
     if (valid) v = ld16(a.q + (int64_t)(it.tok0 + pi) * a.q_stride + h * HD + 32 * kc + 8 * grp);
     qf[kc] = as_bf16x8(v);
   }
-  const BlockIds<WIN> blocks = block_ids<WIN>(a, it, sh);
 #pragma unroll
   for (int dt = 0; dt < HD / 16; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
   m = NEG_BIG;
@@ -332,9 +350,9 @@ __device__ __forceinline__ void wave_run(const AttnArgs& a, const AttnItem& it, 
   // step's registers while the next step's loads stay in flight; the last
   // one or two steps are peeled off.
   WaveStep<HD> A, B;
-  i32x2 ids = ids_of(0);
+  i32x2 ids = RECORDS ? i32x2{start.ids[0], start.ids[1]} : ids_of(0);
   wave_load(A, a, ids[0], ids[1], g, col, grp);
-  ids = ids_of(1);
+  ids = RECORDS ? i32x2{start.ids[2], start.ids[3]} : ids_of(1);
   int s = 0;
   for (; s + 2 < nsteps; s += 2) {
     wave_load(B, a, ids[0], ids[1], g, col, grp);
@@ -348,18 +366,14 @@ __device__ __forceinline__ void wave_run(const AttnArgs& a, const AttnItem& it, 
     wave_compute<HD, WIN>(a, B, it.kv_begin + WSTEP * (s + 1), it, pos, grp, a.scale_log2, qf, o, m, l);
     __builtin_amdgcn_sched_barrier(0);
   }
-  const bool two = s + 1 < nsteps;
-  if (two) wave_load(B, a, ids[0], ids[1], g, col, grp);
-  wave_compute<HD, WIN>(a, A, it.kv_begin + WSTEP * s, it, pos, grp, a.scale_log2, qf, o, m, l);
-  if (two) wave_compute<HD, WIN>(a, B, it.kv_begin + WSTEP * (s + 1), it, pos, grp, a.scale_log2, qf, o, m, l);
+  if (s + 1 < nsteps) {
+    wave_load(B, a, ids[0], ids[1], g, col, grp);
+    wave_compute<HD, WIN>(a, A, it.kv_begin + WSTEP * s, it, pos, grp, a.scale_log2, qf, o, m, l);
+    wave_compute<HD, WIN>(a, B, it.kv_begin + WSTEP * (s + 1), it, pos, grp, a.scale_log2, qf, o, m, l);
+  } else {
+    wave_compute<HD, WIN>(a, A, it.kv_begin + WSTEP * s, it, pos, grp, a.scale_log2, qf, o, m, l);
+  }
   l = rows_sum(l);
-}
-
-// Shift of item idx / tile idx (none without a window).
-template <bool WIN>
-__device__ __forceinline__ UnitShift shift_of(const int32_t* shifts, int idx) {
-  if constexpr (WIN) return const_load(reinterpret_cast<const UnitShift*>(shifts) + idx);
-  else return {0, 0};
 }
 
 // A merged unit: its four items are consecutive key ranges of one (request,
@@ -435,15 +449,15 @@ __device__ __forceinline__ void merge_waves(const AttnArgs& a, const AttnItem& i
 
 // Four items, one per wave: separate ones, or the key ranges of a merged unit.
 // (The waves of the last unit of separate items may have none.)
-template <int HD, bool WIN>
-__device__ __forceinline__ void item_unit(const AttnArgs& a, int code, uint8_t* smem) {
-  const bool merged = code & kUnitMerged;
-  const int idx = (code & ~kUnitMerged) * WAVES + wave_id(), lane = threadIdx.x & 63;
-  const AttnItem it = const_load(reinterpret_cast<const AttnItem*>(a.items) + idx);
+template <int HD, bool WIN, bool RECORDS>
+__device__ __forceinline__ void item_unit(const AttnArgs& a, const WaveStart<WIN, RECORDS>& start, bool merged,
+                                          uint8_t* smem) {
+  const int lane = threadIdx.x & 63;
+  const AttnItem& it = start.it;
   f32x4 o[HD / 16];
   float m = NEG_BIG, l = 0.f;
   if (it.kv_begin < it.kv_end) {
-    wave_run<HD, WIN>(a, it, shift_of<WIN>(a.item_shift, idx), lane, o, m, l);
+    wave_run<HD, WIN, RECORDS>(a, start, lane, o, m, l);
     if (!merged) store_column<HD>(a, it, lane & 15, o, m, l, lane >> 4);
   } else if (merged) {
 #pragma unroll
@@ -569,7 +583,7 @@ __device__ __forceinline__ void tile_pv(f32x4 (&o)[CT][HD / 16], const u32x4 (&v
 // One key step of a tile. The scores of this step (sc_cur) were formed one
 // step earlier; while their softmax runs on the vector ALUs, the next step's
 // scores go to the matrix cores (sc_next), so the two overlap within the wave.
-template <int HD, int CT, bool WIN, bool MASKED>
+template <int HD, int CT, bool WIN, bool MASKED, bool LAST>
 __device__ __forceinline__ void tile_step(const AttnArgs& a, const AttnItem& it, uint8_t* smem, int kt, int nsteps,
                                           const BlockIds<WIN>& blocks, int kb0, int& next_id, int wave, int lane,
                                           int k_lane, int v_lane, const bf16x8 (&qf)[CT][HD / 32],
@@ -581,16 +595,16 @@ __device__ __forceinline__ void tile_step(const AttnArgs& a, const AttnItem& it,
   const int j0 = it.kv_begin + TSTEP * kt;
   u32x4 vf[HD / 16];
   tile_read_v<HD>(vf, smem + (kt % TSTAGES) * TG::STAGE, v_lane);
-  // step kt + 1 complete (the one issued after it may stay in flight); the
-  // ring slot of step kt - 1 is free for step kt + TSTAGES - 1
-  if (kt + 2 < nsteps) wait_vmcnt<TG::LOADS>();
-  else wait_vmcnt<0>();
-  __builtin_amdgcn_s_barrier();
-  if (kt + TSTAGES - 1 < nsteps) {
-    tile_issue<HD>(smem + ((kt + TSTAGES - 1) % TSTAGES) * TG::STAGE, a, next_id, it.kv_head, wave, lane);
-    if (kt + TSTAGES < nsteps) next_id = blocks.at(kb0 + 2 * (kt + TSTAGES) + (wave & 1));
-  }
-  {
+  if (!LAST) {
+    // step kt + 1 complete (the one issued after it may stay in flight); the
+    // ring slot of step kt - 1 is free for step kt + TSTAGES - 1
+    if (kt + 2 < nsteps) wait_vmcnt<TG::LOADS>();
+    else wait_vmcnt<0>();
+    __builtin_amdgcn_s_barrier();
+    if (kt + TSTAGES - 1 < nsteps) {
+      tile_issue<HD>(smem + ((kt + TSTAGES - 1) % TSTAGES) * TG::STAGE, a, next_id, it.kv_head, wave, lane);
+      if (kt + TSTAGES < nsteps) next_id = blocks.at(kb0 + 2 * (kt + TSTAGES) + (wave & 1));
+    }
     bf16x8 kf[2][HD / 32];
     tile_read_k<HD>(kf, smem + ((kt + 1) % TSTAGES) * TG::STAGE, k_lane);
     tile_scores<HD, CT>(sc_next, kf, qf);
@@ -626,8 +640,10 @@ __device__ __forceinline__ void tile_step(const AttnArgs& a, const AttnItem& it,
   tile_pv<HD, CT>(o, vf, pf);
 }
 
-template <int HD, bool WIN>
-__device__ __forceinline__ void tile_unit(const AttnArgs& a, const AttnItem& it, UnitShift sh, uint8_t* smem) {
+template <int HD, bool WIN, bool RECORDS>
+__device__ __forceinline__ void tile_unit(const AttnArgs& a, const WaveStart<WIN, RECORDS>& start, uint8_t* smem) {
+  const AttnItem& it = start.it;
+  const BlockIds<WIN>& blocks = start.blocks;
   using TG = TileGeom<HD>;
   constexpr int KC = HD / 32, DT = HD / 16;
   constexpr int CT = 2;  // 16-column tiles per wave (4 waves x 32 columns)
@@ -651,7 +667,6 @@ __device__ __forceinline__ void tile_unit(const AttnArgs& a, const AttnItem& it,
       qf[ct][kc] = as_bf16x8(v);
     }
   }
-  const BlockIds<WIN> blocks = block_ids<WIN>(a, it, sh);
   const int kb0 = it.kv_begin >> 4;
   const int nsteps = (it.kv_end - it.kv_begin + TSTEP - 1) / TSTEP;
   // steps whose keys all lie below the tile's first position and kv_end need no mask
@@ -669,11 +684,12 @@ __device__ __forceinline__ void tile_unit(const AttnArgs& a, const AttnItem& it,
   const int k_lane = TG::off(col >> 3) + (8 * grp + (col & 7)) * 16;
   const int v_lane = grp * HD * 16 + col * 16;
   // prologue: steps 0..TSTAGES-2 in flight, scores of step 0
-  int next_id = blocks.at(kb0 + (wave & 1));
+  static_assert(TSTAGES == 4, "a record holds the ids of the prologue's steps and the next one");
+  int next_id = RECORDS ? start.ids[0] : blocks.at(kb0 + (wave & 1));
 #pragma unroll
   for (int s0 = 0; s0 < TSTAGES - 1; ++s0) {
     if (s0 < nsteps) tile_issue<HD>(smem + s0 * TG::STAGE, a, next_id, g, wave, lane);
-    if (s0 + 1 < nsteps) next_id = blocks.at(kb0 + 2 * (s0 + 1) + (wave & 1));
+    if (s0 + 1 < nsteps) next_id = RECORDS ? start.ids[s0 + 1] : blocks.at(kb0 + 2 * (s0 + 1) + (wave & 1));
   }
   if (nsteps >= 3) wait_vmcnt<2 * TG::LOADS>();
   else if (nsteps == 2) wait_vmcnt<TG::LOADS>();
@@ -685,43 +701,56 @@ __device__ __forceinline__ void tile_unit(const AttnArgs& a, const AttnItem& it,
     tile_read_k<HD>(kf, smem, k_lane);
     tile_scores<HD, CT>(sa, kf, qf);
   }
-  // Steps alternate the two score buffers. The last step forms the scores of a
-  // step that does not exist, from whatever its ring slot holds, and nobody
-  // reads them: a copy of the step's code without them costs more, in
-  // instructions that a short tile runs once and has to fetch.
-  auto step = [&](auto masked, int t, f32x4(&cur)[CT][2], f32x4(&next)[CT][2]) {
-    tile_step<HD, CT, WIN, decltype(masked)::value>(a, it, smem, t, nsteps, blocks, kb0, next_id, wave, lane, k_lane,
-                                                    v_lane, qf, pos, o, m, l, cur, next);
+  // steps alternate the two score buffers; the last step is peeled
+  auto step = [&](auto masked, auto last, int t, f32x4(&cur)[CT][2], f32x4(&next)[CT][2]) {
+    tile_step<HD, CT, WIN, decltype(masked)::value, decltype(last)::value>(
+        a, it, smem, t, nsteps, blocks, kb0, next_id, wave, lane, k_lane, v_lane, qf, pos, o, m, l, cur, next);
   };
   constexpr std::true_type yes{};
   constexpr std::false_type no{};
-  // first step with no key that the window hides from some row
-  const int near = WIN ? (window_edge(a, it) - it.kv_begin + TSTEP - 1) / TSTEP : 0;
   int kt = 0;
-  while (kt + 2 <= nsteps) {  // masked steps, unmasked ones, masked ones (each part may be empty)
-    for (; kt >= near && kt + 2 <= full; kt += 2) {
-      step(no, kt, sa, sb);
-      step(no, kt + 1, sb, sa);
-    }
-    for (; kt + 2 <= nsteps && !(kt >= near && kt + 2 <= full); kt += 2) {
-      step(yes, kt, sa, sb);
-      step(yes, kt + 1, sb, sa);
+  if (WIN) {
+    // steps with keys that the window hides from some row
+    const int far = (window_edge(a, it) - it.kv_begin + TSTEP - 1) / TSTEP;
+    for (; kt < far && kt + 2 < nsteps; kt += 2) {
+      step(yes, no, kt, sa, sb);
+      step(yes, no, kt + 1, sb, sa);
     }
   }
-  if (kt < nsteps) step(yes, kt, sa, sb);
+  for (; kt + 2 <= full && kt + 2 < nsteps; kt += 2) {
+    step(no, no, kt, sa, sb);
+    step(no, no, kt + 1, sb, sa);
+  }
+  for (; kt + 2 < nsteps; kt += 2) {
+    step(yes, no, kt, sa, sb);
+    step(yes, no, kt + 1, sb, sa);
+  }
+  if (kt + 1 < nsteps) {
+    step(yes, no, kt, sa, sb);
+    step(yes, yes, kt + 1, sb, sa);
+  } else {
+    step(yes, yes, kt, sa, sb);
+  }
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) store_column<HD>(a, it, 32 * wave + 16 * ct + col, o[ct], m[ct], rows_sum(l[ct]), grp);
 }
 
-template <int HD, bool WIN>
+template <int HD, bool WIN, bool RECORDS>
 __global__ __launch_bounds__(64 * WAVES, 2) void attn_kernel(AttnArgs a) {
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
-  const int unit = const_load(a.units + blockIdx.x);
-  if (unit >= 0) {
-    tile_unit<HD, WIN>(a, const_load(reinterpret_cast<const AttnItem*>(a.tiles) + unit),
-                       shift_of<WIN>(a.tile_shift, unit), smem);
+  if constexpr (RECORDS) {
+    const UnitRec r = const_load(reinterpret_cast<const UnitRec*>(a.records) + WAVES * blockIdx.x + wave_id());
+    const WaveStart<WIN, true> start = start_of<WIN>(a, r);
+    if (r.kind == kRecTile) tile_unit<HD, WIN, true>(a, start, smem);
+    else item_unit<HD, WIN, true>(a, start, r.kind == kRecMerged, smem);
   } else {
-    item_unit<HD, WIN>(a, -unit - 1, smem);
+    const int unit = const_load(a.units + blockIdx.x);
+    if (unit >= 0) {
+      tile_unit<HD, WIN, false>(a, start_of<WIN>(a, a.tiles, a.tile_shift, unit), smem);
+    } else {
+      const int code = -unit - 1, idx = (code & ~kUnitMerged) * WAVES + wave_id();
+      item_unit<HD, WIN, false>(a, start_of<WIN>(a, a.items, a.item_shift, idx), code & kUnitMerged, smem);
+    }
   }
 }
 
@@ -813,19 +842,19 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a) {
 // stay far faster.
 constexpr int kItemOnlyLds = 96 * 1024;
 
-template <int HD, bool WIN>
+template <int HD, bool WIN, bool RECORDS>
 void launch(hipStream_t s, const AttnArgs& a) {
   constexpr int lds = TSTAGES * TileGeom<HD>::STAGE;
   static_assert(2 * lds <= 160 * 1024 && 2 * kItemOnlyLds > 160 * 1024 && kItemOnlyLds <= 160 * 1024, "occupancy");
   static std::atomic<uint64_t> lds_raised{0};
-  raise_dynamic_lds(reinterpret_cast<const void*>(&attn_kernel<HD, WIN>), kItemOnlyLds, lds_raised);
-  attn_kernel<HD, WIN><<<a.n_units, 64 * WAVES, a.n_tiles > 0 ? lds : kItemOnlyLds, s>>>(a);
+  raise_dynamic_lds(reinterpret_cast<const void*>(&attn_kernel<HD, WIN, RECORDS>), kItemOnlyLds, lds_raised);
+  attn_kernel<HD, WIN, RECORDS><<<a.n_units, 64 * WAVES, a.n_tiles > 0 ? lds : kItemOnlyLds, s>>>(a);
 }
 
 }  // namespace attn_detail
 
 AttnArgs attention_args(const Dims& d, const Plan& p, const int32_t* meta, const void* k_pool, const void* v_pool,
-                        float* part_o, float* part_ml) {
+                        float* part_o, float* part_ml, const RecordPlan* records) {
   AttnArgs at{};
   at.k_pool = static_cast<const uint16_t*>(k_pool); at.v_pool = static_cast<const uint16_t*>(v_pool);
   at.tiles = meta + p.off_tiles; at.n_tiles = p.n_tiles;
@@ -841,13 +870,25 @@ AttnArgs attention_args(const Dims& d, const Plan& p, const int32_t* meta, const
   at.window = p.window.window; at.sinks = p.window.sinks; at.sink_blocks = p.sink_blocks;
   at.tile_shift = meta + p.off_tile_shift;
   at.item_shift = meta + p.off_item_shift;
+  if (records) {
+    at.records = meta;
+    at.bt = meta + records->off_bt;
+    at.groups = meta + records->off_groups;
+    at.merge_units = meta + records->off_merge;
+    at.tiles = at.items = at.units = at.req_bt = at.tile_shift = at.item_shift = nullptr;
+  }
   return at;
 }
 
 void launch_attention(hipStream_t s, const AttnArgs& a) {
   if (a.n_units <= 0) return;
-  if (a.hd == 128) a.windowed ? attn_detail::launch<128, true>(s, a) : attn_detail::launch<128, false>(s, a);
-  else a.windowed ? attn_detail::launch<64, true>(s, a) : attn_detail::launch<64, false>(s, a);
+  auto go = [&](auto windowed, auto records) {
+    constexpr bool W = decltype(windowed)::value, R = decltype(records)::value;
+    if (a.hd == 128) attn_detail::launch<128, W, R>(s, a);
+    else attn_detail::launch<64, W, R>(s, a);
+  };
+  if (a.records) a.windowed ? go(std::true_type{}, std::true_type{}) : go(std::false_type{}, std::true_type{});
+  else a.windowed ? go(std::true_type{}, std::false_type{}) : go(std::false_type{}, std::false_type{});
 }
 
 void launch_attn_merge(hipStream_t s, const AttnArgs& a) {

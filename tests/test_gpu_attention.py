@@ -118,8 +118,10 @@ def test_strided_rows_and_untouched_memory(hb):
     assert bool((wide[keep] == 7.0).all())
 
 
-def test_same_bits_as_the_layer(hb):
-    """The layer's attention over the same cache and the layer's own q, with and without a window."""
+def test_same_bits_as_the_layer(hb, monkeypatch):
+    """The layer's attention over the same cache and the layer's own q, with and without a window. (With one split
+    length for both: their planners choose it differently, and partial sums then add in another order.)"""
+    monkeypatch.setenv("HB_ATTN_SPLIT_ITEM", "256")
     import torch
     from paper_2503_22562_amd import hb as H
     from paper_2503_22562_amd.harness import DeviceLayer

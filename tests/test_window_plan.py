@@ -67,6 +67,7 @@ def check(plan, where, shape, reqs, window, sinks):
     tile_cols, per_unit, windowed, sink_blocks = (int(v) for v in plan["geom"][0])
     assert windowed == any(window and x + c - window > sinks for c, x in reqs)
     assert all(int(o) % 16 == 0 and int(o) <= int(n) for o, n in plan["off"])
+    assert plan["records"] == [["1"]]  # what hb_attention uploads says the same
     seen = defaultdict(list)
     for kind in ("tile", "item"):
         for v in plan[kind]:
@@ -127,6 +128,20 @@ def test_random_windows(driver, seed):
     plan, where = run(driver, shape, int(rng.choice([1, 16, 256])), reqs, window, sinks,
                       int(rng.choice([0, 64, 256])), int(rng.choice([0, 64, 128])))
     check(plan, where, shape, reqs, window, sinks)
+
+
+@pytest.mark.parametrize("name,reqs,window,units", [
+    ("tp8", [(1, 300)], 0, 1),                  # short ranges: one unit each
+    ("g1", [(1, 9000)] * 8, 500, 32),
+    ("tp8", [(1, 1000)], 0, 4),                 # longer ones in 64-key pieces a wave
+    ("g1", [(1, 3000)] * 8, 0, 8 * 4 * 6),      # as finely as 256 workgroups allow: 128 keys a wave
+    ("tp8", [(1, 30000)], 0, 40),               # no finer than sqrt(keys): 192
+])
+def test_small_launches_fit_one_round(driver, name, reqs, window, units):
+    plan, where = run(driver, SHAPES[name], 256, reqs, window, 0)
+    assert len(plan["unit"]) == units <= 256
+    if max(x for _, x in reqs) < 5000:
+        check(plan, where, SHAPES[name], reqs, window, 0)
 
 
 def test_entries_of_dead_blocks_are_not_looked_at(driver):

@@ -1,6 +1,8 @@
 // Prints the plan of one batch under a sliding window as text, its block ids
 // looked up the way the kernels look them up.
+#include <algorithm>
 #include <cstdio>
+#include <cstring>
 #include <vector>
 
 #include "hb_plan.h"
@@ -33,6 +35,7 @@ int main() {
   opt.split_tile = split_tile;
   opt.split_item = split_item;
   opt.window = {window, sinks};
+  opt.fit_items = true;
   int64_t T = 0;
   const hb_status st = check_requests(d, 1 << 24, reqs.data(), n, opt.window, &T);
   printf("status %d\n", (int)st);
@@ -67,6 +70,39 @@ int main() {
   for (int i = 0; i < p.n_tiles; ++i) unit("tile", p.off_tiles, p.off_tile_shift, i);
   for (int i = 0; i < p.n_items; ++i) unit("item", p.off_items, p.off_item_shift, i);
   for (int i = 0; i < p.n_units; ++i) printf("unit %d\n", m[p.off_units + i]);
+  // the records: the same units, in launch order, one per wave, with the same
+  // block at every place of their ranges and the first of them at hand
+  RecordPlan rp;
+  build_records(p, &rp);
+  const int32_t* o = rp.meta.data();
+  bool same = (int)rp.meta.size() >= 64 * p.n_units && rp.off_bt == 64 * p.n_units;
+  auto block = [&](const AttnItem& it, const UnitShift& sh, int b) {
+    return m[p.off_bt + m[p.off_req_bt + it.req] + b + (p.windowed ? (b < p.sink_blocks ? sh.sink : sh.window) : 0)];
+  };
+  for (int u = 0; u < p.n_units; ++u) {
+    const int code = m[p.off_units + u];
+    const int unit = code >= 0 ? code : (-1 - code) & ~kUnitMerged;
+    for (int w = 0; w < 4; ++w) {
+      const UnitRec& r = reinterpret_cast<const UnitRec*>(o)[4 * u + w];
+      const int i = code >= 0 ? unit : 4 * unit + w;
+      const AttnItem& it = reinterpret_cast<const AttnItem*>(m + (code >= 0 ? p.off_tiles : p.off_items))[i];
+      UnitShift sh{0, 0};
+      if (p.windowed) sh = reinterpret_cast<const UnitShift*>(m + (code >= 0 ? p.off_tile_shift : p.off_item_shift))[i];
+      same &= r.kind == (code >= 0 ? kRecTile : ((-1 - code) & kUnitMerged) ? kRecMerged : kRecSingle);
+      same &= std::memcmp(&r.item, &it, sizeof it) == 0;
+      if (it.kv_begin >= it.kv_end) continue;
+      const int first = it.kv_begin / 16, last = (it.kv_end - 1) / 16;
+      for (int b = first; b <= last; ++b) {
+        const int at = rp.off_bt + b + (b < p.sink_blocks ? r.sink : r.window);
+        same &= at >= rp.off_bt && at < rp.off_groups && o[at] == block(it, sh, b);
+      }
+      for (int k = 0; k < 4; ++k)
+        same &= r.ids[k] == block(it, sh, std::min(last, first + (code >= 0 ? 2 * k + (w & 1) : k)));
+    }
+  }
+  same &= std::memcmp(o + rp.off_groups, m + p.off_groups, sizeof(MergeGroup) * p.n_groups) == 0;
+  same &= std::memcmp(o + rp.off_merge, m + p.off_merge, sizeof(int32_t) * p.n_merge_units) == 0;
+  printf("records %d\n", (int)same);
   for (int r = 0; r < n; ++r)  // the block a request's first new token goes to
     printf("slot %d\n", m[p.off_bt + m[p.off_req_bt + r] + reqs[r].context_len / 16]);
   return 0;
