@@ -328,6 +328,15 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   const int S_i = opt.split_item > 0 ? round_up(opt.split_item, 64)
                   : S_i_fit > 0      ? S_i_fit
                                      : std::max(S_i_fill, round_up((int64_t)(item_keys / (16.0 * cus)) + 1, 64));
+  // Longest range that one wave takes alone. With few item groups a lone wave of
+  // S_i keys is what the launch ends on, so ranges above 256 keys are cut over a
+  // unit's four waves already (beside a 512-token chunk, 64 decodes behind a
+  // 1024-key window 55.8 -> 49.4 us; 300 + 100 decodes of 50-800 keys 34.4 ->
+  // 29.5; 64 decodes behind 4096 138 -> 134.7). From four groups per CU on others
+  // fill in behind it, and the merge in LDS is only a cost (128 decodes of 600
+  // keys on eight heads 49.4 -> 52.0, 256 of 50-1000 82.4 -> 84.4).
+  const bool few_items = opt.fit_items && item_lengths.size() * (size_t)d.nkv < 4 * (size_t)cus;
+  const int S_1 = few_items ? std::min(S_i, 256) : S_i;
   p->split_tile = S_t;
   p->split_item = S_i;
 
@@ -376,7 +385,7 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
                              nspl > 1 ? part0 + s * kTileCols : -1});
           continue;
         }
-        if (nspl == 1) {
+        if (kv_len <= S_1) {
           singles.push_back({r, g, tok_start[r] + i0, pos0, npos, 0, kv_len, -1});
           continue;
         }
