@@ -468,13 +468,13 @@ def _block_pairs(src, dst):
 def hb_copy_blocks(layer: Layer, src, dst) -> None:
     """Block dst[i] of the layer's pool takes the contents of block src[i]."""
     s, d = _block_pairs(src, dst)
-    _check(load().hb_copy_blocks(layer.handle, s.ctypes.data, d.ctypes.data, len(s)))
+    _check(load().hb_copy_blocks(layer.handle, s.tobytes(), d.tobytes(), len(s)))
 
 
 def hb_copy_model_blocks(model: Model, src, dst) -> None:
     """hb_copy_blocks in the pools of every layer."""
     s, d = _block_pairs(src, dst)
-    _check(load().hb_copy_model_blocks(model.handle, s.ctypes.data, d.ctypes.data, len(s)))
+    _check(load().hb_copy_model_blocks(model.handle, s.tobytes(), d.tobytes(), len(s)))
 
 
 def hb_plan_compaction(num_blocks: int, tables: Sequence[Iterable[int]]):
