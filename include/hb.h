@@ -244,7 +244,10 @@ hb_status hb_run_iteration_noalloc(hb_layer* layer, const hb_batch_desc* desc);
  * query row and head, K and V read from a pool in the layouts above, keys
  * visible as in hb_run_iteration or under a sliding window with sinks
  * (hb_set_attention_window). Softmax statistics and sums are fp32; the
- * probabilities enter the product with V as bf16.
+ * probabilities enter the product with V as bf16. Long key ranges are split and
+ * their parts joined in the order of the keys, so a plan's results do not depend
+ * on timing; the splits may differ from hb_run_iteration's, and with them the
+ * last bits.
  *
  * A handle holds the plan of one batch, which every layer's call runs: an
  * iteration plans once and calls hb_run_attention per layer, each with its own
@@ -271,10 +274,10 @@ void hb_destroy_attention(hb_attention* attention);
  * runs enqueued earlier keep theirs. Allocates device memory only where a plan
  * needs more than every one before it. n_requests == 0 plans nothing: runs are
  * no-ops.
- * Errors: HB_ERR_INVALID and HB_ERR_RANGE as hb_validate_batch for the requests,
- * and a window or sinks outside [0, 2^30] (the plan before stays); HB_ERR_OOM,
- * HB_ERR_HIP (the handle holds no plan afterwards, except that a stream under
- * graph capture, which is refused, leaves the plan before). */
+ * Errors: HB_ERR_INVALID and HB_ERR_RANGE as hb_validate_batch for the requests
+ * and a window or sinks outside [0, 2^30], HB_ERR_UNSUPPORTED for block tables of
+ * more than 2^30 entries, HB_ERR_HIP for a stream under graph capture: the plan
+ * before stays. HB_ERR_OOM and other HB_ERR_HIP: the handle holds no plan. */
 hb_status hb_plan_attention(hb_attention* attention, int32_t n_requests, const hb_request* requests, int32_t window,
                             int32_t sinks);
 
@@ -301,7 +304,8 @@ hb_status hb_run_attention(hb_attention* attention, const hb_kv_pool* pool, cons
  * chunk_len < 1, context_len < 0, short block table, T > max_batch_tokens,
  * n_requests > max_requests or < 0, bad out_dtype, overlapping x_in/x_out,
  * two requests writing one slot), HB_ERR_RANGE (a used block id outside
- * [0, num_blocks)), HB_ERR_UNSUPPORTED (config outside the limits). */
+ * [0, num_blocks)), HB_ERR_UNSUPPORTED (config outside the limits, block tables
+ * of more than 2^30 entries together). */
 hb_status hb_validate_batch(const hb_layer_config* cfg, int32_t num_blocks, const hb_batch_desc* desc);
 
 /* Decode load of one profile row: n_decode decodes with the given contexts

@@ -60,7 +60,7 @@ void free_attention(hb_attention* a) {
 }
 
 // Replace a device array by one of `bytes` (its contents are not kept) once no
-// enqueued work uses it. The old one stays where the new one cannot be had.
+// enqueued work uses it. Where the new one cannot be had the old one stays.
 bool regrow(hb_attention* a, void** p, size_t bytes) {
   void* q = nullptr;
   if (hipMalloc(&q, bytes) != hipSuccess) {
@@ -87,6 +87,7 @@ hb_status plan_attention(hb_attention* a, int n, const hb_request* requests, int
   const DeviceGuard on(a->device);
   st = refuse_capture(a->stream);
   if (st != HB_OK) return st;
+  a->planned = false;  // until the new one stands
   const hb_batch_desc desc{n, requests, nullptr, nullptr, HB_OUT_BF16};
   build_plan(a->d, &desc, a->cu_count, &a->next, opt);
   build_records(a->next, &a->next_records);
@@ -108,10 +109,8 @@ hb_status plan_attention(hb_attention* a, int n, const hb_request* requests, int
     }
     s.cap = cap;
   }
-  // the array a plan in use reads goes only when its successor can have one
   if (a->next.n_slots > a->part_cap) {
     const int slots = std::max(a->next.n_slots, 2 * a->part_cap);
-    a->planned = false;
     a->part_cap = 0;
     if (!regrow(a, (void**)&a->part_o, (size_t)slots * a->d.hd * sizeof(float)) ||
         !regrow(a, (void**)&a->part_ml, (size_t)slots * 2 * sizeof(float)))
@@ -119,13 +118,11 @@ hb_status plan_attention(hb_attention* a, int n, const hb_request* requests, int
     a->part_cap = slots;
   }
   if (words > a->meta_cap) {
-    a->planned = false;
     if (!regrow(a, (void**)&a->meta, cap * sizeof(int32_t))) return fail(HB_ERR_OOM, "plan of %zu B", cap * 4);
     a->meta_cap = cap;
   }
-  std::memcpy(s.host, a->next_records.meta.data(), words * sizeof(int32_t));
-  a->planned = false;
   if (words > 0) {
+    std::memcpy(s.host, a->next_records.meta.data(), words * sizeof(int32_t));
     launch_copy_words(a->stream, s.host, a->meta, words);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || hipEventRecord(s.copied, a->stream) != hipSuccess)

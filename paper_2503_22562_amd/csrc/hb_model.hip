@@ -126,7 +126,7 @@ hb_status hb_run_model(hb_model* m, const hb_model_batch* b) {
   const int H = c.hidden, R = b->n_requests;
   // all layers share shape and pool size; their windows may differ
   hb_batch_desc desc{b->n_requests, b->requests, m->x[0], m->x[1], HB_OUT_BF16};
-  hb_status st = check_layer_stack(m->layers.data(), (int)m->layers.size(), &desc);
+  hb_status st = guarded([&] { return check_layer_stack(m->layers.data(), (int)m->layers.size(), &desc); });
   if (st == HB_OK) st = refuse_capture(m->stream);
   if (st != HB_OK) return st;
   int T = 0;
@@ -160,7 +160,7 @@ hb_status hb_run_model(hb_model* m, const hb_model_batch* b) {
     xout[l] = next;
     cur = next;
   }
-  st = run_layer_stack(m->layers.data(), (int)nl, &desc, xin.data(), xout.data());
+  st = guarded([&] { return run_layer_stack(m->layers.data(), (int)nl, &desc, xin.data(), xout.data()); });
   if (st != HB_OK) return st;
   launch_gather_rows(m->stream, cur, T, m->rows_dev, R, H, m->last);
   launch_rmsnorm(m->stream, m->last, false, m->g_final, m->normed, R, H, c.rms_eps);

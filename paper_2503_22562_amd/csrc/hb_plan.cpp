@@ -103,7 +103,7 @@ hb_status check_requests(const Dims& d, int num_blocks, const hb_request* reques
   if (n > d.max_R) return fail(HB_ERR_INVALID, "n_requests %d exceeds max_requests %d", n, d.max_R);
   if (n > 0 && !requests) return fail(HB_ERR_INVALID, "null request array");
   if (num_blocks <= 0) return fail(HB_ERR_INVALID, "pool has no blocks");
-  int64_t T = 0;
+  int64_t T = 0, entries = 0;
   for (int r = 0; r < n; ++r) {
     const hb_request& q = requests[r];
     if (q.chunk_len < 1) return fail(HB_ERR_INVALID, "request %d: chunk_len %d < 1", r, q.chunk_len);
@@ -122,8 +122,11 @@ hb_status check_requests(const Dims& d, int num_blocks, const hb_request* reques
         return fail(HB_ERR_RANGE, "request %d: block_table[%lld] = %d outside [0, %d)", r, (long long)i, b, num_blocks);
     }
     T += q.chunk_len;
+    entries += blocks_for(kv) - dead.count + kBtPad;
   }
   if (T > d.max_T) return fail(HB_ERR_INVALID, "batch has %lld tokens, max_batch_tokens is %d", (long long)T, d.max_T);
+  if (entries > (int64_t)1 << 30)  // the plan counts its words in 32 bits
+    return fail(HB_ERR_UNSUPPORTED, "block tables of %lld entries in one batch", (long long)entries);
   *n_tokens = T;
   return HB_OK;
 }

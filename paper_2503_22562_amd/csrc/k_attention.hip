@@ -857,26 +857,24 @@ AttnArgs attention_args(const Dims& d, const Plan& p, const int32_t* meta, const
                         float* part_o, float* part_ml, const RecordPlan* records) {
   AttnArgs at{};
   at.k_pool = static_cast<const uint16_t*>(k_pool); at.v_pool = static_cast<const uint16_t*>(v_pool);
-  at.tiles = meta + p.off_tiles; at.n_tiles = p.n_tiles;
-  at.items = meta + p.off_items; at.n_items = p.n_items;
-  at.units = meta + p.off_units; at.n_units = p.n_units;
-  at.groups = meta + p.off_groups; at.n_groups = p.n_groups;
-  at.merge_units = meta + p.off_merge; at.n_merge_units = p.n_merge_units;
-  at.req_bt = meta + p.off_req_bt; at.bt = meta + p.off_bt;
-  at.part_o = part_o; at.part_ml = part_ml;
-  at.nq = d.nq; at.nkv = d.nkv; at.hd = d.hd;
-  at.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)d.hd));
-  at.windowed = p.windowed;
-  at.window = p.window.window; at.sinks = p.window.sinks; at.sink_blocks = p.sink_blocks;
-  at.tile_shift = meta + p.off_tile_shift;
-  at.item_shift = meta + p.off_item_shift;
+  at.n_tiles = p.n_tiles; at.n_items = p.n_items; at.n_units = p.n_units;
+  at.n_groups = p.n_groups; at.n_merge_units = p.n_merge_units;
   if (records) {
     at.records = meta;
     at.bt = meta + records->off_bt;
     at.groups = meta + records->off_groups;
     at.merge_units = meta + records->off_merge;
-    at.tiles = at.items = at.units = at.req_bt = at.tile_shift = at.item_shift = nullptr;
+  } else {
+    at.tiles = meta + p.off_tiles; at.items = meta + p.off_items; at.units = meta + p.off_units;
+    at.groups = meta + p.off_groups; at.merge_units = meta + p.off_merge;
+    at.req_bt = meta + p.off_req_bt; at.bt = meta + p.off_bt;
+    at.tile_shift = meta + p.off_tile_shift; at.item_shift = meta + p.off_item_shift;
   }
+  at.part_o = part_o; at.part_ml = part_ml;
+  at.nq = d.nq; at.nkv = d.nkv; at.hd = d.hd;
+  at.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)d.hd));
+  at.windowed = p.windowed;
+  at.window = p.window.window; at.sinks = p.window.sinks; at.sink_blocks = p.sink_blocks;
   return at;
 }
 

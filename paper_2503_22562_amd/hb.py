@@ -385,8 +385,9 @@ def hb_window_dead_blocks(context_len: int, window: int, sinks: int = 0) -> Tupl
 class Attention:
     """Owns an hb_attention handle; n_tokens: rows of the current plan."""
 
-    def __init__(self, handle: C.c_void_p, cfg: hb_layer_config, num_blocks: int):
+    def __init__(self, handle: C.c_void_p, cfg: hb_layer_config, num_blocks: int, device: int):
         self.handle = handle
+        self.device = device
         self.cfg = cfg
         self.num_blocks = num_blocks
         self.row = cfg.n_q_heads * cfg.head_dim             # values of a row of q
@@ -401,12 +402,12 @@ class Attention:
 
 
 def hb_create_attention(cfg: hb_layer_config, num_blocks: int, stream: Optional[int] = None) -> Attention:
+    import torch
     if stream is None:
-        import torch
         stream = torch.cuda.current_stream().cuda_stream
     h = C.c_void_p()
     _check(load().hb_create_attention(C.byref(cfg), int(num_blocks), C.c_void_p(stream), C.byref(h)))
-    return Attention(h, cfg, int(num_blocks))
+    return Attention(h, cfg, int(num_blocks), torch.cuda.current_device())
 
 
 def hb_destroy_attention(attention: Attention) -> None:
@@ -423,10 +424,10 @@ def hb_plan_attention(attention: Attention, requests: Sequence[Tuple[int, int, I
     attention.n_tokens = sum(int(r[0]) for r in requests)
 
 
-def _rows(name: str, t, n: int, row: int, bf16) -> int:
+def _rows(name: str, t, n: int, row: int, bf16, device: int) -> int:
     """Row stride of n rows of `row` contiguous bf16 values ([n][heads][head_dim] or [n][heads * head_dim])."""
-    if t.dtype != bf16 or not t.is_cuda:
-        raise ValueError(f"{name}: a bf16 tensor on the GPU, not {t.dtype} on {t.device}")
+    if t.dtype != bf16 or t.get_device() != device:
+        raise ValueError(f"{name}: a bf16 tensor on GPU {device}, not {t.dtype} on {t.device}")
     if t.numel() != n * row or t.dim() < 2 or t.shape[0] != n:
         raise ValueError(f"{name}: {n} rows of {row} values, not {tuple(t.shape)}")
     if t.is_contiguous():
@@ -443,15 +444,15 @@ def _rows(name: str, t, n: int, row: int, bf16) -> int:
 def hb_run_attention(attention: Attention, q, k_pool, v_pool, out) -> None:
     """q, out: bf16 [T][n_q_heads][head_dim] (or [T][n_q_heads * head_dim]), rows any multiple of 8 elements apart."""
     from torch import bfloat16
-    blocks = attention.num_blocks
+    blocks, device = attention.num_blocks, attention.device
     for name, p in (("k_pool", k_pool), ("v_pool", v_pool)):
-        if p.dtype != bfloat16 or not p.is_cuda or not p.is_contiguous():
-            raise ValueError(f"{name}: a contiguous bf16 tensor on the GPU")
+        if p.dtype != bfloat16 or p.get_device() != device or not p.is_contiguous():
+            raise ValueError(f"{name}: a contiguous bf16 tensor on GPU {device}")
         have = p.shape[0]
         if have < blocks or p.numel() != have * attention.block_values:
             raise ValueError(f"{name}: at least {blocks} blocks of {attention.block_values} values, not {tuple(p.shape)}")
     n, row = attention.n_tokens, attention.row
-    qs, os_ = _rows("q", q, n, row, bfloat16), _rows("out", out, n, row, bfloat16)
+    qs, os_ = _rows("q", q, n, row, bfloat16, device), _rows("out", out, n, row, bfloat16, device)
     status = load().hb_run_attention(attention.handle, hb_kv_pool(k_pool.data_ptr(), v_pool.data_ptr(), blocks),
                                      q.data_ptr(), qs, out.data_ptr(), os_)
     if status:

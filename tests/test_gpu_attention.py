@@ -187,6 +187,43 @@ def test_plans_in_a_row(hb):
                 at += c
 
 
+def test_two_handles_on_two_streams(hb):
+    """Two plans of one cache at once, each on its own stream with its own split buffers; requests that share blocks."""
+    import torch
+    from paper_2503_22562_amd import hb as H
+    from paper_2503_22562_amd.harness import to_device_bf16
+    shape = heads(8, 1, 128)
+    cache = Cache(shape, 700, 512, 64, seed=13)
+    made = [cache.request(1, 9000, 0, 0), cache.request(120, 1500, 0, 0)]
+    (_, _, t0), (_, _, t1) = made[0][0], made[1][0]
+    # the same blocks under several requests: shorter contexts of the same sequences
+    batches = [[(1, 9000, t0), (1, 4000, t0), (1, 0, t1)], [(120, 1500, t1), (3, 700, t1), (2, 8999, t0)]]
+    kv = [(made[0][1:], made[0][1:], made[1][1:]), (made[1][1:], made[1][1:], made[0][1:])]
+    torch.cuda.synchronize()
+    streams, work = [torch.cuda.Stream() for _ in range(2)], []
+    for s, b in zip(streams, batches):
+        with torch.cuda.stream(s):
+            q = cache.bits(sum(r[0] for r in b), 8, 128)
+            qd = to_device_bf16(q)
+            outs = [torch.full_like(qd, float("nan")) for _ in range(6)]
+            att = H.hb_create_attention(cache.dl.cfg, 700)
+            H.hb_plan_attention(att, b)
+            work.append((att, q, qd, outs))
+    torch.cuda.synchronize()
+    for i in range(6):
+        for att, _, qd, outs in work:
+            H.hb_run_attention(att, qd, cache.dl.k_pool, cache.dl.v_pool, outs[i])
+    torch.cuda.synchronize()
+    for (att, q, _, outs), b, kvs in zip(work, batches, kv):
+        assert all(torch.equal(outs[0], o) for o in outs[1:])
+        got, at = outs[0].float().cpu().numpy().astype(np.float64), 0
+        qf = bf16_bits_to_f32(q).astype(np.float64)
+        for (c, x, _), (k, v) in zip(b, kvs):
+            o, pv = reference(qf[at:at + c], k[:x + c], v[:x + c], np.arange(x, x + c), 0, 0)
+            assert_close(got[at:at + c], o, pv, f"request ({c}, {x})")
+            at += c
+
+
 def test_offsets_past_32_bits(hb):
     """Blocks beyond 2^32 elements (8 GiB) of a pool, read and copied."""
     import torch

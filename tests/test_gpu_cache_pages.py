@@ -57,6 +57,26 @@ def test_copy_in_every_layer_of_a_model(hb):
                 assert np.array_equal(_bits(p), w)
 
 
+def test_copy_of_a_long_list(hb):
+    """More pairs than the staging ring uploads in-stream, and more workgroups than one launch takes."""
+    import torch
+    from paper_2503_22562_amd import hb as H
+    from paper_2503_22562_amd.harness import DeviceLayer
+    shape = LayerShape("copy", 64, 8, 8, 128, 16, weight_seed=3)
+    n, nb = 132000, 264100
+    dl = DeviceLayer(shape, make_weights(shape), nb, 16, 4, pool_fill_bits=None)
+    for p in (dl.k_pool, dl.v_pool):
+        p.view(torch.int16).random_(-(1 << 15), 1 << 15)
+    ids = np.random.default_rng(5).permutation(nb).astype(np.int32)
+    origin = np.arange(nb)
+    origin[ids[n:2 * n]] = ids[:n]
+    origin = torch.from_numpy(origin).cuda()
+    want = [p.view(torch.int16)[origin] for p in (dl.k_pool, dl.v_pool)]
+    H.hb_copy_blocks(dl.layer, ids[:n], ids[n:2 * n])
+    torch.cuda.synchronize()
+    assert all(torch.equal(p.view(torch.int16), w) for p, w in zip((dl.k_pool, dl.v_pool), want))
+
+
 def test_copy_refusals(hb):
     import torch
     from paper_2503_22562_amd import hb as H

@@ -252,3 +252,48 @@ def test_compaction_refusals(H):
     assert lib.hb_plan_compaction(4, None, None, 1, src.ctypes.data, dst.ctypes.data, C.byref(m), C.byref(u)) \
         == H.HB_ERR_INVALID
     assert lib.hb_plan_compaction(4, None, None, 0, None, dst.ctypes.data, C.byref(m), C.byref(u)) == H.HB_ERR_INVALID
+
+
+def test_calls_refused_before_any_device_work(H):
+    """Null handles and configurations outside the limits: no HIP call is made, so this runs without a GPU."""
+    import ctypes as C
+    lib = H.load()
+
+    class Shape:
+        hidden, n_q_heads, n_kv_heads, head_dim, ffn_dim = 256, 4, 2, 64, 688
+        rope_theta, rms_eps, kv_block = 5e5, 1e-5, 16
+
+    def create(cfg, nb, out=True):
+        h = C.c_void_p(7)
+        st = lib.hb_create_attention(C.byref(cfg) if cfg is not None else None, nb, None, C.byref(h) if out else None)
+        assert not out or h.value is None
+        return st
+
+    good = H.make_config(Shape, 16, 4)
+    assert create(good, 4, out=False) == H.HB_ERR_INVALID
+    assert create(good, 0) == create(good, -1) == create(None, 4) == H.HB_ERR_INVALID
+    for field, value, status in (("head_dim", 96, "UNSUPPORTED"), ("kv_block", 32, "UNSUPPORTED"),
+                                 ("n_kv_heads", 3, "UNSUPPORTED"), ("hidden", 0, "INVALID")):
+        assert create(H.make_config(type("S", (Shape,), {field: value}), 16, 4), 4) == getattr(H, "HB_ERR_" + status)
+    lib.hb_destroy_attention(None)
+    ids = np.arange(2, dtype=np.int32).tobytes()
+    pool = H.hb_kv_pool(0x1000, 0x1000, 4)
+    for st in (lib.hb_plan_attention(None, 0, None, 0, 0), lib.hb_run_attention(None, pool, 0x1000, 256, 0x9000, 256),
+               lib.hb_copy_blocks(None, ids, ids, 2), lib.hb_copy_model_blocks(None, ids, ids, 2),
+               lib.hb_set_attention_window(None, 1, 0)):
+        assert st == H.HB_ERR_INVALID
+        assert "null" in H.hb_last_error()
+
+
+def test_the_copy_kernel_does_not_spill(tmp_path):
+    import re
+    import shutil
+    from paper_2503_22562_amd import build as B
+    if not os.path.exists(B.HIPCC) and shutil.which("hipcc") is None:
+        pytest.skip("no hipcc")
+    cmd = [B.HIPCC, *B.COMMON, *B.HIP_FLAGS, "--cuda-device-only", "-Rpass-analysis=kernel-resource-usage", "-c",
+           os.path.join(B.CSRC, "k_blocks.hip"), "-o", str(tmp_path / "k.o")]
+    r = subprocess.run(cmd, capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0, r.stderr[-2000:]
+    spills = [int(v) for v in re.findall(r"VGPRs Spill: (\d+)", r.stderr)]
+    assert spills and not any(spills)
