@@ -117,10 +117,10 @@ void launch_append_kv_inline(hipStream_t s, const uint16_t* k, const uint16_t* v
 
 // Copy whole blocks, all kv heads of K and V, inside each of n_pools pools: block
 // dst[i] becomes block src[i]. No block of dst occurs again in src or dst. The ids
-// are in device memory or (inline) in host memory, at most kCopyInlinePairs, and
-// travel with the launch.
-constexpr int kCopyPools = 64;          // pools of one launch
-constexpr int kCopyInlinePairs = 320;   // with the pools' addresses within the 4 KB of a launch's arguments
+// are in device memory or (inline) in host memory and travel with the launches.
+constexpr int kCopyPools = 64;         // pools of one launch
+constexpr int kCopyInlinePairs = 320;  // pairs of one launch, within the 4 KB its arguments may take
+constexpr int kCopyInlineOne = 496;    // pairs of one launch over one pool
 struct CopyPools {
   void* k[kCopyPools];
   void* v[kCopyPools];

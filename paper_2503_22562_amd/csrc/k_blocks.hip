@@ -23,8 +23,9 @@ namespace {
 // lists that fit the caches.
 constexpr int kCopyThreads = 256, kCopyVecs = 2;
 
+template <int N>
 struct InlinePairs {
-  int32_t s[kCopyInlinePairs], d[kCopyInlinePairs];
+  int32_t s[N], d[N];
   __device__ __forceinline__ int src(int i) const { return s[i]; }
   __device__ __forceinline__ int dst(int i) const { return d[i]; }
 };
@@ -34,8 +35,14 @@ struct ListedPairs {
   __device__ __forceinline__ int dst(int i) const { return const_load(d + i); }
 };
 
-template <typename Pairs>
-__global__ __launch_bounds__(kCopyThreads) void copy_blocks_kernel(CopyPools pools, int n_pools, Pairs pairs, int vecs,
+struct OnePool {
+  void *k[1], *v[1];
+};
+static_assert(sizeof(CopyPools) + sizeof(InlinePairs<kCopyInlinePairs>) + 12 <= 4096, "launch arguments");
+static_assert(sizeof(OnePool) + sizeof(InlinePairs<kCopyInlineOne>) + 12 <= 4096, "launch arguments");
+
+template <typename Pools, typename Pairs>
+__global__ __launch_bounds__(kCopyThreads) void copy_blocks_kernel(Pools pools, int n_pools, Pairs pairs, int vecs,
                                                                    int parts) {
   const int run = blockIdx.x / parts, part = blockIdx.x - run * parts;
   const int pair = run / (2 * n_pools), side = run - pair * 2 * n_pools;  // K and V of layer 0, of layer 1, ...
@@ -52,32 +59,37 @@ __global__ __launch_bounds__(kCopyThreads) void copy_blocks_kernel(CopyPools poo
     if (i0 + k * kCopyThreads < vecs) __builtin_nontemporal_store(v[k], d + i0 + k * kCopyThreads);
 }
 
-// Launches of at most 2^20 workgroups (a grid holds fewer than 2^32 threads).
+// Launches of at most `pairs` pairs and 2^20 workgroups (a grid holds fewer than 2^32 threads).
 template <typename F>
-void for_pairs(int n, int n_pools, int nkv, int hd, F&& launch) {
+void for_pairs(int n, int pairs, int n_pools, int nkv, int hd, F&& launch) {
   const int vecs = nkv * hd * 2, parts = (vecs + kCopyThreads * kCopyVecs - 1) / (kCopyThreads * kCopyVecs);
-  const int per_pair = 2 * n_pools * parts, most = std::max(1, (1 << 20) / per_pair);
-  for (int i = 0; i < n; i += most) launch(i, std::min(most, n - i) * per_pair, vecs, parts);
+  const int per_pair = 2 * n_pools * parts, most = std::max(1, std::min(pairs, (1 << 20) / per_pair));
+  for (int i = 0; i < n; i += most) {
+    const int m = std::min(most, n - i);
+    launch(i, m, m * per_pair, vecs, parts);
+  }
 }
 
 }  // namespace
 
 void launch_copy_blocks(hipStream_t s, const CopyPools& pools, int n_pools, const int32_t* src, const int32_t* dst,
                         int n, int nkv, int hd) {
-  for_pairs(n, n_pools, nkv, hd, [&](int i, int groups, int vecs, int parts) {
+  for_pairs(n, n, n_pools, nkv, hd, [&](int i, int, int groups, int vecs, int parts) {
     copy_blocks_kernel<<<groups, kCopyThreads, 0, s>>>(pools, n_pools, ListedPairs{src + i, dst + i}, vecs, parts);
   });
 }
 
 void launch_copy_blocks_inline(hipStream_t s, const CopyPools& pools, int n_pools, const int32_t* src,
                                const int32_t* dst, int n, int nkv, int hd) {
-  for_pairs(n, n_pools, nkv, hd, [&](int i, int groups, int vecs, int parts) {
-    InlinePairs p{};
-    const int m = groups / (2 * n_pools * parts);
-    std::copy(src + i, src + i + m, p.s);
-    std::copy(dst + i, dst + i + m, p.d);
-    copy_blocks_kernel<<<groups, kCopyThreads, 0, s>>>(pools, n_pools, p, vecs, parts);
-  });
+  auto go = [&](const auto& to, auto pairs, int most) {
+    for_pairs(n, most, n_pools, nkv, hd, [&](int i, int m, int groups, int vecs, int parts) {
+      std::copy(src + i, src + i + m, pairs.s);
+      std::copy(dst + i, dst + i + m, pairs.d);
+      copy_blocks_kernel<<<groups, kCopyThreads, 0, s>>>(to, n_pools, pairs, vecs, parts);
+    });
+  };
+  if (n_pools == 1) go(OnePool{{pools.k[0]}, {pools.v[0]}}, InlinePairs<kCopyInlineOne>{}, kCopyInlineOne);
+  else go(pools, InlinePairs<kCopyInlinePairs>{}, kCopyInlinePairs);
 }
 
 }  // namespace hb

@@ -15,7 +15,7 @@ def _bits(t):
 
 
 @pytest.mark.parametrize("nq,nkv,hd", [(1, 1, 64), (4, 2, 64), (6, 3, 128), (8, 8, 128), (40, 40, 128)])
-@pytest.mark.parametrize("n", [0, 1, 7, 320, 321, 1500])
+@pytest.mark.parametrize("n", [0, 1, 7, 320, 321, 496, 497, 992, 993, 1500])
 def test_copy(hb, nq, nkv, hd, n):
     import torch
     from paper_2503_22562_amd import hb as H
@@ -47,7 +47,7 @@ def test_copy_in_every_layer_of_a_model(hb):
     for p in [p for layer in dm.pools for p in layer]:
         p.view(torch.int16).random_(-(1 << 15), 1 << 15)
     rng = np.random.default_rng(1)
-    for n in (3, 400):
+    for n in (3, 320, 321, 400):
         want = [[_bits(p).copy() for p in layer] for layer in dm.pools]
         ids = rng.permutation(900).astype(np.int32)
         H.hb_copy_model_blocks(dm.model, ids[:n], ids[n:2 * n])
