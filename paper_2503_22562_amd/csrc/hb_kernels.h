@@ -139,11 +139,9 @@ struct AttnArgs {
   const int32_t* tiles;   // workgroup tiles (AttnItem)
   int n_tiles;
   const int32_t* items;   // wave items (AttnItem)
-  int n_items;
   const int32_t* units;   // per workgroup: tile index, or -1 - (group of 4 items)
   int n_units;
   const int32_t* groups;
-  int n_groups;
   const int32_t* merge_units;  // per merge workgroup: group * 16 + 16-column block
   int n_merge_units;
   const int32_t* req_bt;

@@ -857,8 +857,7 @@ AttnArgs attention_args(const Dims& d, const Plan& p, const int32_t* meta, const
                         float* part_o, float* part_ml, const RecordPlan* records) {
   AttnArgs at{};
   at.k_pool = static_cast<const uint16_t*>(k_pool); at.v_pool = static_cast<const uint16_t*>(v_pool);
-  at.n_tiles = p.n_tiles; at.n_items = p.n_items; at.n_units = p.n_units;
-  at.n_groups = p.n_groups; at.n_merge_units = p.n_merge_units;
+  at.n_tiles = p.n_tiles; at.n_units = p.n_units; at.n_merge_units = p.n_merge_units;
   if (records) {
     at.records = meta;
     at.bt = meta + records->off_bt;

@@ -316,6 +316,23 @@ def _i32(a) -> np.ndarray:
     return np.ascontiguousarray(a, dtype=np.int32)
 
 
+def _int32(v) -> int:
+    """An argument of the C interface: ctypes would keep its low 32 bits without a word."""
+    v = int(v)
+    if not -(1 << 31) <= v < 1 << 31:
+        raise ValueError(f"{v} does not fit 32 bits")
+    return v
+
+
+def _ids(a) -> np.ndarray:
+    """Block ids as a new or the caller's int32 array. (NumPy checks Python integers by itself, not those of arrays.)"""
+    if getattr(a, "dtype", np.int32) != np.int32:
+        a = np.asarray(a)
+        if a.size and (a.dtype.kind not in "iu" or a.min() < -(1 << 31) or a.max() >= 1 << 31):
+            raise ValueError(f"block ids are 32-bit integers, not these of {a.dtype}")
+    return _i32(a)
+
+
 def hb_append_kv(layer: Layer, block_table, context_len: int, k, v) -> None:
     bt = _i32(block_table)
     n = 0 if k is None else int(k.shape[0])
@@ -372,13 +389,13 @@ def hb_run_iteration_noalloc(layer: Layer, requests: Sequence[Tuple[int, int, It
 
 def hb_set_attention_window(layer: Layer, window: int, sinks: int = 0) -> None:
     """Sliding window of the layer's later iterations (0: every earlier key)."""
-    _check(load().hb_set_attention_window(layer.handle, int(window), int(sinks)))
+    _check(load().hb_set_attention_window(layer.handle, _int32(window), _int32(sinks)))
 
 
 def hb_window_dead_blocks(context_len: int, window: int, sinks: int = 0) -> Tuple[int, int]:
     """(first, count): the block-table entries that no row at a position >= context_len sees."""
     first, count = C.c_int32(), C.c_int32()
-    _check(load().hb_window_dead_blocks(int(context_len), int(window), int(sinks), C.byref(first), C.byref(count)))
+    _check(load().hb_window_dead_blocks(_int32(context_len), _int32(window), _int32(sinks), C.byref(first), C.byref(count)))
     return first.value, count.value
 
 
@@ -406,7 +423,7 @@ def hb_create_attention(cfg: hb_layer_config, num_blocks: int, stream: Optional[
     if stream is None:
         stream = torch.cuda.current_stream().cuda_stream
     h = C.c_void_p()
-    _check(load().hb_create_attention(C.byref(cfg), int(num_blocks), C.c_void_p(stream), C.byref(h)))
+    _check(load().hb_create_attention(C.byref(cfg), _int32(num_blocks), C.c_void_p(stream), C.byref(h)))
     return Attention(h, cfg, int(num_blocks), torch.cuda.current_device())
 
 
@@ -420,7 +437,7 @@ def hb_plan_attention(attention: Attention, requests: Sequence[Tuple[int, int, I
                       sinks: int = 0) -> None:
     """requests: (chunk_len, context_len, block_table) per request, in row order."""
     d, keep = _desc(requests, 0, 0, HB_OUT_BF16)
-    _check(load().hb_plan_attention(attention.handle, d.n_requests, d.requests, int(window), int(sinks)))
+    _check(load().hb_plan_attention(attention.handle, d.n_requests, d.requests, _int32(window), _int32(sinks)))
     attention.n_tokens = sum(int(r[0]) for r in requests)
 
 
@@ -460,7 +477,7 @@ def hb_run_attention(attention: Attention, q, k_pool, v_pool, out) -> None:
 
 
 def _block_pairs(src, dst):
-    s, d = _i32(src), _i32(dst)
+    s, d = _ids(src), _ids(dst)
     if s.ndim != 1 or s.shape != d.shape:
         raise ValueError(f"src and dst: one list of block ids each, of equal length, not {s.shape} and {d.shape}")
     return s, d
@@ -480,12 +497,12 @@ def hb_copy_model_blocks(model: Model, src, dst) -> None:
 
 def hb_plan_compaction(num_blocks: int, tables: Sequence[Iterable[int]]):
     """(tables, src, dst, n_used): the tables over blocks [0, n_used), and the moves that make them true."""
-    ts = [np.array(t, dtype=np.int32).reshape(-1) for t in tables]
+    ts = [_ids(t).reshape(-1).copy() for t in tables]
     ptrs = (C.c_void_p * max(1, len(ts)))(*[t.ctypes.data for t in ts])
     lens = _i32([len(t) for t in ts] or [0])
     src, dst = (np.zeros(max(1, int(num_blocks) // 2), np.int32) for _ in range(2))
     moves, used = C.c_int32(), C.c_int32()
-    _check(load().hb_plan_compaction(int(num_blocks), ptrs, lens.ctypes.data_as(C.POINTER(C.c_int32)), len(ts),
+    _check(load().hb_plan_compaction(_int32(num_blocks), ptrs, lens.ctypes.data_as(C.POINTER(C.c_int32)), len(ts),
                                      src.ctypes.data, dst.ctypes.data, C.byref(moves), C.byref(used)))
     return ts, src[:moves.value], dst[:moves.value], used.value
 

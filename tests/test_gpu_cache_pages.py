@@ -314,3 +314,47 @@ def test_window_of_a_layer(hb):
             H.hb_set_attention_window(dl.layer, w, s)
         assert e.value.status == H.HB_ERR_INVALID
     assert H.load().hb_set_attention_window(None, 1, 0) == H.HB_ERR_INVALID
+
+
+def test_a_captured_iteration_keeps_its_window(hb):
+    """A replay runs the window, the tables and the dead entries of its capture, whatever window and batch the layer
+    runs in between."""
+    import torch
+    from paper_2503_22562_amd import hb as H
+    from paper_2503_22562_amd.harness import DeviceLayer
+    rng = np.random.default_rng(21)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        lens = [(90, 300)] + [(1, 190 + i) for i in range(20)] + [(1, 1500)]
+        T = sum(c for c, _ in lens)
+        dl = DeviceLayer(SHAPE, make_weights(SHAPE), 512, T, len(lens))
+        gen = torch.Generator(device="cuda")
+        gen.manual_seed(22)
+        for p in (dl.k_pool, dl.v_pool):
+            p.normal_(0.0, 1.0, generator=gen)
+        perm, at, reqs = rng.permutation(512).astype(np.int32), 0, []
+        for c, x in lens:
+            n = -(-(c + x) // 16)
+            table = perm[at:at + n].copy()
+            first, count = H.hb_window_dead_blocks(x, 150, 20)
+            table[first:first + count] = -1
+            reqs.append((c, x, table))
+            at += n
+        x = torch.randn(T, SHAPE.hidden, device="cuda", generator=gen).to(torch.bfloat16)
+        other, xo = reqs[1:5], x[90:94].contiguous()
+        H.hb_set_attention_window(dl.layer, 150, 20)
+        want, want_other = dl.run(reqs, x).clone(), dl.run(other, xo).clone()
+        y = torch.empty_like(want)
+        side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        H.hb_run_iteration_noalloc(dl.layer, reqs, x, y)
+    with torch.cuda.stream(side):
+        for i in range(5):
+            H.hb_set_attention_window(dl.layer, (40, 150, 97)[i % 3], 20)
+            mid = dl.run(other, xo).clone()
+            y.fill_(float("nan"))
+            graph.replay()
+            side.synchronize()
+            assert torch.equal(y, want), i
+            assert torch.equal(mid, want_other) == (i % 3 == 1), i

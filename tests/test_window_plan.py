@@ -285,6 +285,27 @@ def test_calls_refused_before_any_device_work(H):
         assert "null" in H.hb_last_error()
 
 
+def test_arguments_that_do_not_fit_32_bits(H):
+    """Values whose low 32 bits would be a valid argument are refused by the binding, not shortened."""
+    wide, ids = (1 << 32) + 1, np.arange(2)
+
+    class Handle:
+        handle, layer = None, None
+
+    for call in (lambda: H.hb_set_attention_window(Handle, wide), lambda: H.hb_set_attention_window(Handle, 1, wide),
+                 lambda: H.hb_window_dead_blocks(wide, 1), lambda: H.hb_window_dead_blocks(1, wide),
+                 lambda: H.hb_plan_attention(Handle, [], wide), lambda: H.hb_plan_attention(Handle, [], 1, wide),
+                 lambda: H.hb_copy_blocks(Handle, ids + wide, ids), lambda: H.hb_copy_blocks(Handle, ids, ids + 0.5),
+                 lambda: H.hb_copy_model_blocks(Handle, ids, ids - wide),
+                 lambda: H.hb_plan_compaction(4, [ids + wide])):
+        with pytest.raises(ValueError):
+            call()
+    table = np.array([5, 3], np.int32)
+    moved = H.hb_plan_compaction(6, [table, [5, -1]])
+    assert [t.tolist() for t in moved[0]] == [[1, 0], [1, -1]] and moved[3] == 2
+    assert table.tolist() == [5, 3]  # the caller's table is not rewritten
+
+
 def test_the_copy_kernel_does_not_spill(tmp_path):
     import re
     import shutil
