@@ -155,7 +155,8 @@ struct AttnArgs {
   int window, sinks, sink_blocks;
   const int32_t* tile_shift;
   const int32_t* item_shift;
-  // the units as records (UnitRec), in place of tiles, items, units, req_bt and the shifts; or null
+  // the units as records (UnitRec), in place of tiles, items, units, req_bt and the shifts; or null.
+  // With records, groups are merge records, one per merge workgroup, in place of merge_units.
   const int32_t* records;
 };
 // The arguments of a plan's attention: its uploaded metadata (records: as

@@ -551,15 +551,19 @@ void build_records(const Plan& p, RecordPlan* out) {
   const int32_t* m = p.meta.data();
   const int n_bt = p.off_tiles - p.off_bt;  // with its padding
   int off = 16 * 4 * p.n_units;
-  out->off_bt = off;      off += n_bt;
-  out->off_groups = off;  off += align16(8 * p.n_groups);
-  out->off_merge = off;   off += align16(p.n_merge_units);
+  out->off_bt = off;     off += n_bt;
+  out->off_merge = off;  off += align16(8 * p.n_merge_units);
   out->meta.assign(off, 0);
   if (off == 0) return;
   int32_t* o = out->meta.data();
   std::memcpy(o + out->off_bt, m + p.off_bt, sizeof(int32_t) * n_bt);
-  std::memcpy(o + out->off_groups, m + p.off_groups, sizeof(MergeGroup) * p.n_groups);
-  std::memcpy(o + out->off_merge, m + p.off_merge, sizeof(int32_t) * p.n_merge_units);
+  const MergeGroup* groups = reinterpret_cast<const MergeGroup*>(m + p.off_groups);
+  MergeGroup* merge = reinterpret_cast<MergeGroup*>(o + out->off_merge);
+  for (int i = 0; i < p.n_merge_units; ++i) {
+    const int mu = m[p.off_merge + i];
+    merge[i] = groups[mu >> 4];
+    merge[i].cols = mu & 15;
+  }
   UnitRec* rec = reinterpret_cast<UnitRec*>(o);
   const AttnItem* tiles = reinterpret_cast<const AttnItem*>(m + p.off_tiles);
   const AttnItem* items = reinterpret_cast<const AttnItem*>(m + p.off_items);

@@ -73,7 +73,9 @@ struct UnitShift {
 // Columns whose key range was split: part s of column c sits in slot
 // part0 + s * stride + c.
 struct MergeGroup {
-  int32_t part0, nparts, stride, tok0, npos, kv_head, pad0, pad1;
+  int32_t part0, nparts, stride, tok0, npos, kv_head;
+  int32_t cols;  // a merge record's: its block of 16 of the columns
+  int32_t pad;
 };
 static_assert(sizeof(AttnItem) == 32 && sizeof(MergeGroup) == 32, "packed as 8 int32");
 static_assert(sizeof(UnitShift) == 8, "packed as 2 int32");
@@ -160,9 +162,10 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
                 const PlanOptions& opt = PlanOptions());
 
 // A plan as hb_attention uploads it: 4 n_units records, then the plan's block
-// ids, merge groups and merge units, at these offsets (int32).
+// ids and a merge record (the group, with its block of columns) per merge unit,
+// at these offsets (int32).
 struct RecordPlan {
-  int off_bt = 0, off_groups = 0, off_merge = 0;
+  int off_bt = 0, off_merge = 0;
   std::vector<int32_t> meta;
 };
 void build_records(const Plan& p, RecordPlan* out);

@@ -762,19 +762,28 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attn_kernel(AttnArgs a) {
 // (a decode has G of 16), the parts are dealt to the idle column slots and
 // the slots' results combined, in slot order, through LDS: 8 decodes of one
 // kv head, up to 29 parts each, 8.5 -> 4.6 us.
-template <int HD>
+// RECORDS: one record per workgroup in place of the merge unit and its group, one
+// scalar load less before the parts' (8 decodes of one kv head, cold caches, the
+// whole call 15.2 -> 14.6 us; a decode at 3000 keys 12.7 -> 12.1).
+template <int HD, bool RECORDS>
 __global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a) {
   constexpr int TPC = HD / 8, SLOTS = 256 / TPC;  // threads per column, column slots
   __shared__ float sacc[SLOTS][TPC][8];
   __shared__ float sml[SLOTS][2];
-  const int mu = const_load(a.merge_units + blockIdx.x);
-  const MergeGroup gr = const_load(reinterpret_cast<const MergeGroup*>(a.groups) + (mu >> 4));
+  int gi = blockIdx.x, cb = 0;
+  if (!RECORDS) {
+    const int mu = const_load(a.merge_units + blockIdx.x);
+    gi = mu >> 4;
+    cb = mu & 15;
+  }
+  const MergeGroup gr = const_load(reinterpret_cast<const MergeGroup*>(a.groups) + gi);
+  if (RECORDS) cb = gr.cols;
   const int G = a.nq / a.nkv;
-  const int cols = min(16, gr.npos * G - (mu & 15) * 16);
+  const int cols = min(16, gr.npos * G - cb * 16);
   int width = 1;  // column slots of one pass over the columns: a power of two
   while (width < cols) width *= 2;
   const int slot = threadIdx.x / TPC, t = threadIdx.x % TPC, d = t * 8;
-  const int ci = slot & (width - 1), c = (mu & 15) * 16 + min(ci, cols - 1);
+  const int ci = slot & (width - 1), c = cb * 16 + min(ci, cols - 1);
   const int step = SLOTS / width, first = slot / width;  // parts first, first + step, ...
   float M = NEG_BIG, L = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   // parts are folded four at a time so their loads are in flight together
@@ -861,8 +870,7 @@ AttnArgs attention_args(const Dims& d, const Plan& p, const int32_t* meta, const
   if (records) {
     at.records = meta;
     at.bt = meta + records->off_bt;
-    at.groups = meta + records->off_groups;
-    at.merge_units = meta + records->off_merge;
+    at.groups = meta + records->off_merge;
   } else {
     at.tiles = meta + p.off_tiles; at.items = meta + p.off_items; at.units = meta + p.off_units;
     at.groups = meta + p.off_groups; at.merge_units = meta + p.off_merge;
@@ -890,8 +898,12 @@ void launch_attention(hipStream_t s, const AttnArgs& a) {
 
 void launch_attn_merge(hipStream_t s, const AttnArgs& a) {
   if (a.n_merge_units <= 0) return;
-  if (a.hd == 128) attn_detail::attn_merge_kernel<128><<<a.n_merge_units, 256, 0, s>>>(a);
-  else attn_detail::attn_merge_kernel<64><<<a.n_merge_units, 256, 0, s>>>(a);
+  auto go = [&](auto records) {
+    constexpr bool R = decltype(records)::value;
+    if (a.hd == 128) attn_detail::attn_merge_kernel<128, R><<<a.n_merge_units, 256, 0, s>>>(a);
+    else attn_detail::attn_merge_kernel<64, R><<<a.n_merge_units, 256, 0, s>>>(a);
+  };
+  a.records ? go(std::true_type{}) : go(std::false_type{});
 }
 
 }  // namespace hb

@@ -94,14 +94,18 @@ int main() {
       const int first = it.kv_begin / 16, last = (it.kv_end - 1) / 16;
       for (int b = first; b <= last; ++b) {
         const int at = rp.off_bt + b + (b < p.sink_blocks ? r.sink : r.window);
-        same &= at >= rp.off_bt && at < rp.off_groups && o[at] == block(it, sh, b);
+        same &= at >= rp.off_bt && at < rp.off_merge && o[at] == block(it, sh, b);
       }
       for (int k = 0; k < 4; ++k)
         same &= r.ids[k] == block(it, sh, std::min(last, first + (code >= 0 ? 2 * k + (w & 1) : k)));
     }
   }
-  same &= std::memcmp(o + rp.off_groups, m + p.off_groups, sizeof(MergeGroup) * p.n_groups) == 0;
-  same &= std::memcmp(o + rp.off_merge, m + p.off_merge, sizeof(int32_t) * p.n_merge_units) == 0;
+  for (int i = 0; i < p.n_merge_units; ++i) {
+    const int mu = m[p.off_merge + i];
+    MergeGroup want = reinterpret_cast<const MergeGroup*>(m + p.off_groups)[mu >> 4];
+    want.cols = mu & 15;
+    same &= std::memcmp(o + rp.off_merge + 8 * i, &want, sizeof want) == 0;
+  }
   printf("records %d\n", (int)same);
   for (int r = 0; r < n; ++r)  // the block a request's first new token goes to
     printf("slot %d\n", m[p.off_bt + m[p.off_req_bt + r] + reqs[r].context_len / 16]);
