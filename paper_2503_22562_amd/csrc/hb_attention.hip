@@ -152,7 +152,7 @@ hb_status hb_create_attention(const hb_layer_config* cfg, int32_t num_blocks, vo
     auto bail = [&](hb_status s) { free_attention(a); return s; };
     a->d = d;
     a->num_blocks = num_blocks;
-    a->opt.fit_items = true;
+    a->opt.fit_round = true;
     a->stream = static_cast<hipStream_t>(hip_stream);
     if (hipGetDevice(&a->device) != hipSuccess ||
         hipDeviceGetAttribute(&a->cu_count, hipDeviceAttributeMultiprocessorCount, a->device) != hipSuccess)

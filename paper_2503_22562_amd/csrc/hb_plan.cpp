@@ -239,6 +239,18 @@ void iteration_work(const Dims& d, const hb_request* reqs, int n, double* flops,
 
 static int round_up(int64_t x, int m) { return (int)((x + m - 1) / m * m); }
 
+// Smallest split length from `finest` on (multiples of 64 keys, at most 1024) at
+// which key ranges of these lengths, each in nkv kv heads, take `slots`
+// workgroups at most, a workgroup taking `waves` splits; 0 where none does.
+static int one_round_split(const std::vector<int>& lengths, int nkv, int64_t slots, double finest, int waves) {
+  for (int S = std::max(64, round_up((int64_t)std::ceil(finest), 64)); S <= 1024; S += 64) {
+    int64_t units = 0;
+    for (int n : lengths) units += (n + (int64_t)S * waves - 1) / (S * waves);
+    if (units * nkv <= slots) return S;
+  }
+  return 0;
+}
+
 // Split length of a launch of item ranges (lengths, each in nkv kv heads) that
 // fits one round of workgroups, one per CU; 0 where it does not.
 // A range of at most 576 keys stays one unit: its four waves, of up to 192 keys,
@@ -255,12 +267,20 @@ static int fit_item_split(const std::vector<int>& lengths, int nkv, int cus) {
   for (int n : lengths) longest = std::max(longest, n);
   if ((int64_t)lengths.size() * nkv > cus || longest == 0) return 0;
   if (longest <= 576) return round_up((longest + kItemsPerUnit - 1) / kItemsPerUnit, 64);
-  for (int S = round_up((int64_t)std::ceil(std::sqrt((double)longest)), 64); S <= 1024; S += 64) {
-    int64_t units = 0;
-    for (int n : lengths) units += (n + (int64_t)S * kItemsPerUnit - 1) / (S * kItemsPerUnit);
-    if (units * nkv <= cus) return S;
-  }
-  return 0;
+  return one_round_split(lengths, nkv, cus, std::sqrt((double)longest), kItemsPerUnit);
+}
+
+// The same for tiles that share the CUs with item units: `slots` workgroups are
+// theirs. A tile step costs a third of an item's, and a part that the merge
+// reads holds eight times an item's columns, so no finer than 3 sqrt(keys) (one
+// kv head, cold caches: one tile of 2000 keys 29.2 -> 16.7 us, 4 of 16000 32.8 ->
+// 27.5 at 384 and 28.7 at 256 keys; eight heads, 32 tiles of 2100: 30.9 -> 22.1
+// at 384, one round, 24.4 at 256), and ranges of at most 576 keys stay whole
+// (128 tiles of 544 keys, halved, 22.5 -> 24.2; 128 of 1000 28.2 -> 25.9).
+static int fit_tile_split(const std::vector<int>& lengths, int nkv, int64_t slots) {
+  int longest = 0;
+  for (int n : lengths) longest = std::max(longest, n);
+  return longest > 576 ? one_round_split(lengths, nkv, slots, 3.0 * std::sqrt((double)longest), 1) : 0;
 }
 
 void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p, const PlanOptions& opt) {
@@ -283,17 +303,43 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   p->T = T;
   p->R = R;
 
-  // A chunk that fills at least half a workgroup tile goes to the workgroup
-  // path; decodes and short chunks become 16-column wave items.
-  auto is_tile = [&](int r) { return (int64_t)rq[r].chunk_len * d.G >= kTileCols / 2; };
+  const int cus = std::max(1, cu_count);
+  // keys of the w rows from i0 on of request r
+  auto range_len = [&](int r, int i0, int w) {
+    const int x = rq[r].context_len;
+    return x + std::min(rq[r].chunk_len, i0 + w) - 16 * dead_blocks(win, x + i0).count;
+  };
+  // A small launch is latency: a wave item starts sooner than a tile (its K and V
+  // go straight to registers, no ring and barrier) and its four waves share the
+  // key range, so a batch whose chunks, cut into items as well, make one round of
+  // workgroups of at most 256 keys a wave takes no tiles. Eight kv heads, cold
+  // caches: a fresh 100-token chunk 10.3 -> 8.4 us, 64 tokens behind 500 cached
+  // 19.1 -> 13.0 (finer tiles 16), behind 900 26.6 -> 14.7; one head, 512 behind
+  // 500 26.4 -> 14.3 (17.7). At 320 keys a wave the tiles are ahead (128 tokens
+  // behind 2000, four heads: 22.7, tiles 19.4).
+  bool items_only = false;
+  if (opt.fit_round && opt.split_tile <= 0 && opt.split_item <= 0) {
+    int64_t n = 0;
+    for (int r = 0; r < R; ++r) n += (rq[r].chunk_len + d.P - 1) / d.P;
+    if (n * d.nkv <= cus) {
+      std::vector<int> all;
+      for (int r = 0; r < R; ++r)
+        for (int i0 = 0; i0 < rq[r].chunk_len; i0 += d.P) all.push_back(range_len(r, i0, d.P));
+      const int S = fit_item_split(all, d.nkv, cus);
+      items_only = S > 0 && S <= 256;
+    }
+  }
+  // Otherwise a chunk that fills at least half a workgroup tile goes to the
+  // workgroup path; decodes and short chunks become 16-column wave items.
+  auto is_tile = [&](int r) { return !items_only && (int64_t)rq[r].chunk_len * d.G >= kTileCols / 2; };
   double tile_keys = 0, item_keys = 0;
-  std::vector<int> item_lengths;  // of one kv head
+  std::vector<int> item_lengths, tile_lengths;  // of one kv head
   for (int r = 0; r < R; ++r) {
-    const int c = rq[r].chunk_len, x = rq[r].context_len, w = is_tile(r) ? d.BQ : d.P;
-    for (int i0 = 0; i0 < c; i0 += w) {
-      const int len = x + std::min(c, i0 + w) - 16 * dead_blocks(win, x + i0).count;
+    const int w = is_tile(r) ? d.BQ : d.P;
+    for (int i0 = 0; i0 < rq[r].chunk_len; i0 += w) {
+      const int len = range_len(r, i0, w);
       (is_tile(r) ? tile_keys : item_keys) += (double)d.nkv * len;
-      if (opt.fit_items && !is_tile(r)) item_lengths.push_back(len);
+      if (opt.fit_round) (is_tile(r) ? tile_lengths : item_lengths).push_back(len);
     }
   }
   // split lengths (multiples of 64 keys): about one round of tile workgroups
@@ -316,7 +362,6 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   // over chunk/decode mixes of the 8B and 70B layers and of their
   // tensor-parallel shards (item split 256 .. 4096, tile split 1024 .. 16384).
   constexpr double kMixedStepUs = 0.6, kItemBytesPerUs = 6.0e6;
-  const int cus = std::max(1, cu_count);
   const bool mixed = tile_keys > 0 && item_keys > 0;
   double s_t = tile_keys / (1.0 * cus);
   if (mixed) {
@@ -325,7 +370,6 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
     s_t = launch_us / kMixedStepUs * 32.0;
   }
   const int S_t_auto = std::max(1024, round_up((int64_t)std::min(s_t, 1.0e9) + 1, 64));
-  const int S_t = opt.split_tile > 0 ? round_up(opt.split_tile, 64) : S_t_auto;
   const int S_i_fill = std::min(1024, std::max(opt.min_item, round_up((int64_t)(item_keys * d.hd / 128 / (2.8 * cus)), 64)));
   const int S_i_fit = tile_keys > 0 ? 0 : fit_item_split(item_lengths, d.nkv, cus);
   const int S_i = opt.split_item > 0 ? round_up(opt.split_item, 64)
@@ -338,8 +382,17 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   // 29.5; 64 decodes behind 4096 138 -> 134.7). From four groups per CU on others
   // fill in behind it, and the merge in LDS is only a cost (128 decodes of 600
   // keys on eight heads 49.4 -> 52.0, 256 of 50-1000 82.4 -> 84.4).
-  const bool few_items = opt.fit_items && item_lengths.size() * (size_t)d.nkv < 4 * (size_t)cus;
+  const bool few_items = opt.fit_round && item_lengths.size() * (size_t)d.nkv < 4 * (size_t)cus;
   const int S_1 = few_items ? std::min(S_i, 256) : S_i;
+  // Tiles that leave CUs idle are split for one round too, beside the item units.
+  int S_t_fit = 0;
+  if (opt.fit_round) {
+    int64_t quarters = 0;  // of item units
+    for (int n : item_lengths)
+      quarters += n <= S_1 ? 1 : ((n + S_i - 1) / S_i + kItemsPerUnit - 1) / kItemsPerUnit * kItemsPerUnit;
+    S_t_fit = fit_tile_split(tile_lengths, d.nkv, cus - quarters * d.nkv / kItemsPerUnit);
+  }
+  const int S_t = opt.split_tile > 0 ? round_up(opt.split_tile, 64) : S_t_fit > 0 ? S_t_fit : S_t_auto;
   p->split_tile = S_t;
   p->split_item = S_i;
 

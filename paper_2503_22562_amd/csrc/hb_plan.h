@@ -151,10 +151,10 @@ struct PlanOptions {
   int min_item = 64;   // least item split the planner chooses by itself
   int unit_block = 0;  // runs of tiles / item groups in the unit order (0: one per CU; < 0: fine interleave)
   Window window;
-  // as hb_attention plans: split lengths of item-only launches that need one
-  // round of workgroups at most are chosen for that round (fit_item_split), and
+  // as hb_attention plans: launches that need one round of workgroups at most are
+  // cut for that round, chunks into items too where that is sooner done, and
   // where items are few no wave takes more than 256 keys alone
-  bool fit_items = false;
+  bool fit_round = false;
 };
 
 // Build the plan of a validated batch for a GPU with cu_count compute units.

@@ -71,6 +71,23 @@ def test_chunks(hb, nq, nkv, hd, window, sinks):
     r.check(r.run())
 
 
+@pytest.mark.parametrize("nq,nkv,hd", [(4, 2, 64), (2, 2, 128), (8, 2, 128), (8, 1, 128), (16, 1, 128)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 2), (31, 0), (64, 64), (200, 5), (257, 300)])
+def test_chunks_as_tiles(hb, monkeypatch, nq, nkv, hd, window, sinks):
+    """A forced tile split keeps the planner from cutting these small launches into wave items."""
+    monkeypatch.setenv("HB_ATTN_SPLIT_TILE", "4096")
+    r = Run(heads(nq, nkv, hd), [(130, 0), (64, 333), (200, 900), (1, 640)], window, sinks, seed=nq + window + 1)
+    r.check(r.run())
+
+
+@pytest.mark.parametrize("lens", [[(64, 9000)], [(16, 7001), (1, 9), (33, 4000)], [(300, 2500), (1, 2500)], [(700, 0)]])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1999, 40)])
+def test_chunks_that_leave_compute_units_idle(hb, lens, window, sinks):
+    """Tiles and items split to fill one round of workgroups, joined over tens of parts."""
+    r = Run(heads(16, 2, 128), lens, window, sinks, seed=31)
+    r.check(r.run())
+
+
 @pytest.mark.parametrize("split_tile,split_item", [(64, 64), (128, 64), (512, 256)])
 @pytest.mark.parametrize("window,sinks", [(0, 0), (333, 20), (900, 0)])
 def test_split_over_the_length(hb, monkeypatch, split_tile, split_item, window, sinks):

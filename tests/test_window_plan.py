@@ -144,6 +144,23 @@ def test_small_launches_fit_one_round(driver, name, reqs, window, units):
         check(plan, where, SHAPES[name], reqs, window, 0)
 
 
+@pytest.mark.parametrize("name,reqs,window,tiles,units", [
+    # 256 item groups of two rows, 256 keys a wave: no tile
+    ("tp8", [(512, 500)], 0, 0, 256),
+    ("g1", [(512, 4000)], 512, 0, 128),
+    # a wave would have more: 32 tiles, 2016 to 2512 keys in pieces of 320
+    ("tp8", [(512, 2000)], 0, sum(-(-n // 320) for n in range(2016, 2513, 16)), None),
+    ("tp8", [(64, 16000)], 0, 4 * 42, None),  # no finer than 3 sqrt(keys): 384
+    ("tp8", [(550, 0)], 0, 35, 35),           # 275 item groups are more than one round; up to 576 keys stay whole
+    ("tp8", [(64, 16000), (1, 100), (1, 100)], 0, 4 * 42, 4 * 42 + 2),  # (items are cut at 64 keys: a unit each)
+])
+def test_small_launches_with_chunks_fit_one_round(driver, name, reqs, window, tiles, units):
+    plan, where = run(driver, SHAPES[name], 256, reqs, window, 0)
+    assert len(plan["tile"]) == tiles and len(plan["unit"]) == (units or tiles) <= 256
+    if max(x for _, x in reqs) < 5000:
+        check(plan, where, SHAPES[name], reqs, window, 0)
+
+
 def test_entries_of_dead_blocks_are_not_looked_at(driver):
     for dead_id in (-1, 1 << 30, -(1 << 31)):
         plan, where = run(driver, SHAPES["tp8"], 64, [(1, 5000), (40, 4000)], 300, 20, dead_id=dead_id)

@@ -35,7 +35,7 @@ int main() {
   opt.split_tile = split_tile;
   opt.split_item = split_item;
   opt.window = {window, sinks};
-  opt.fit_items = true;
+  opt.fit_round = true;
   int64_t T = 0;
   const hb_status st = check_requests(d, 1 << 24, reqs.data(), n, opt.window, &T);
   printf("status %d\n", (int)st);
