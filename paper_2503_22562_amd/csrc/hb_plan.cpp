@@ -6,7 +6,9 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <map>
 #include <new>
+#include <tuple>
 
 namespace hb {
 
@@ -283,6 +285,48 @@ static int fit_tile_split(const std::vector<int>& lengths, int nkv, int64_t slot
   return longest > 576 ? one_round_split(lengths, nkv, slots, 3.0 * std::sqrt((double)longest), 1) : 0;
 }
 
+// Item units of one round in an order that gives those that read the same keys to
+// one die: workgroups go to the kDies dies in turn, each with an L2 of its own,
+// and every die would fetch all of K and V otherwise (cold caches, 64 tokens
+// behind 500 cached, eight kv heads, 128 units 13.1 -> 10.0 us; 70B heads behind
+// 900 17.4 -> 12.6). Larger groups first, each to the die with the most room, the
+// rest of it to the next. (Tiles share a key range four times less often: even
+// with cold caches, 19.8 -> 23.2 us with warm ones, 64 tiles of 1000 keys.)
+constexpr int kDies = 8;
+template <typename F>
+static std::vector<int32_t> by_die(const std::vector<int32_t>& units, F&& item_of) {
+  const int n = (int)units.size();
+  std::map<std::tuple<int, int, int>, int> known;
+  std::vector<std::vector<int32_t>> groups;
+  for (const int32_t u : units) {
+    const AttnItem it = item_of(u);
+    const auto at = known.insert({{it.req, it.kv_head, it.kv_begin}, (int)groups.size()}).first;
+    if (at->second == (int)groups.size()) groups.emplace_back();
+    groups[at->second].push_back(u);
+  }
+  std::stable_sort(groups.begin(), groups.end(), [](const auto& a, const auto& b) { return a.size() > b.size(); });
+  int next[kDies], room[kDies];
+  for (int x = 0; x < kDies; ++x) {
+    next[x] = x;
+    room[x] = (n - x + kDies - 1) / kDies;
+  }
+  std::vector<int32_t> order(n);
+  for (const auto& group : groups) {
+    int x = 0, left = 0;
+    for (const int32_t u : group) {
+      if (left == 0) {
+        x = (int)(std::max_element(room, room + kDies) - room);
+        left = room[x];
+      }
+      order[next[x]] = u;
+      next[x] += kDies;
+      --room[x];
+      --left;
+    }
+  }
+  return order;
+}
+
 void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p, const PlanOptions& opt) {
   const int R = desc->n_requests;
   const hb_request* rq = desc->requests;
@@ -312,11 +356,11 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   // A small launch is latency: a wave item starts sooner than a tile (its K and V
   // go straight to registers, no ring and barrier) and its four waves share the
   // key range, so a batch whose chunks, cut into items as well, make one round of
-  // workgroups of at most 256 keys a wave takes no tiles. Eight kv heads, cold
-  // caches: a fresh 100-token chunk 10.3 -> 8.4 us, 64 tokens behind 500 cached
-  // 19.1 -> 13.0 (finer tiles 16), behind 900 26.6 -> 14.7; one head, 512 behind
-  // 500 26.4 -> 14.3 (17.7). At 320 keys a wave the tiles are ahead (128 tokens
-  // behind 2000, four heads: 22.7, tiles 19.4).
+  // workgroups of at most 320 keys a wave takes no tiles. Eight kv heads, cold
+  // caches: a fresh 100-token chunk 10.3 -> 8.2 us, 64 tokens behind 500 cached
+  // 19.1 -> 10.0, behind 900 26.6 -> 13.2, 128 behind 1000 18.7 (split tiles) ->
+  // 13.7. From 384 keys a wave on it depends (64 behind 2500 20.2 -> 20.5; sixteen
+  // heads, 64 behind 2000 with 4 decodes of 3000 28.0 -> 30.9).
   bool items_only = false;
   if (opt.fit_round && opt.split_tile <= 0 && opt.split_item <= 0) {
     int64_t n = 0;
@@ -326,7 +370,7 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
       for (int r = 0; r < R; ++r)
         for (int i0 = 0; i0 < rq[r].chunk_len; i0 += d.P) all.push_back(range_len(r, i0, d.P));
       const int S = fit_item_split(all, d.nkv, cus);
-      items_only = S > 0 && S <= 256;
+      items_only = S > 0 && S <= 320;
     }
   }
   // Otherwise a chunk that fills at least half a workgroup tile goes to the
@@ -539,6 +583,8 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
       else units.push_back(item_unit_codes[b++]);
     }
   }
+  if (items_only && ni_units <= cus)
+    units = by_die(units, [&](int32_t u) { return items[((-1 - u) & ~kUnitMerged) * kItemsPerUnit]; });
   p->n_tiles = nt;
   p->n_items = (int)items.size();
   p->n_units = (int)units.size();
