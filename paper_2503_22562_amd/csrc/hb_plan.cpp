@@ -360,22 +360,37 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   // caches: a fresh 100-token chunk 10.3 -> 8.2 us, 64 tokens behind 500 cached
   // 19.1 -> 10.0, behind 900 26.6 -> 13.2, 128 behind 1000 18.7 (split tiles) ->
   // 13.7. From 384 keys a wave on it depends (64 behind 2500 20.2 -> 20.5; sixteen
-  // heads, 64 behind 2000 with 4 decodes of 3000 28.0 -> 30.9).
+  // heads, 64 behind 2000 with 4 decodes of 3000 28.0 -> 30.9). With more items
+  // than CUs, one round of two workgroups per CU, a unit to a range, does as well
+  // up to 256 keys a wave (256 behind 200 17.8 -> 12.0, a fresh 256 13.3 -> 10.4; at
+  // 320 128 behind 1000 beside 8 decodes of 1000 21.5 -> 23.8; with ranges split 128
+  // behind 2000 22.3 -> 25.1; a second round 512 behind 300 23.4 -> 32.8).
+  auto fills_tile = [&](int r) { return (int64_t)rq[r].chunk_len * d.G >= kTileCols / 2; };
   bool items_only = false;
+  int S_items = 0;
+  p->paired = false;
   if (opt.fit_round && opt.split_tile <= 0 && opt.split_item <= 0) {
     int64_t n = 0;
-    for (int r = 0; r < R; ++r) n += (rq[r].chunk_len + d.P - 1) / d.P;
-    if (n * d.nkv <= cus) {
+    bool chunks = false;
+    for (int r = 0; r < R; ++r) {
+      n += (rq[r].chunk_len + d.P - 1) / d.P;
+      chunks |= fills_tile(r);
+    }
+    if (chunks && n * d.nkv <= 2 * cus) {
       std::vector<int> all;
       for (int r = 0; r < R; ++r)
         for (int i0 = 0; i0 < rq[r].chunk_len; i0 += d.P) all.push_back(range_len(r, i0, d.P));
-      const int S = fit_item_split(all, d.nkv, cus);
-      items_only = S > 0 && S <= 320;
+      const int longest = *std::max_element(all.begin(), all.end());
+      p->paired = n * d.nkv > cus;
+      S_items = p->paired ? round_up(((int64_t)longest + kItemsPerUnit - 1) / kItemsPerUnit, 64)
+                          : fit_item_split(all, d.nkv, cus);
+      items_only = S_items > 0 && S_items <= (p->paired ? 256 : 320);
+      p->paired &= items_only;
     }
   }
   // Otherwise a chunk that fills at least half a workgroup tile goes to the
   // workgroup path; decodes and short chunks become 16-column wave items.
-  auto is_tile = [&](int r) { return !items_only && (int64_t)rq[r].chunk_len * d.G >= kTileCols / 2; };
+  auto is_tile = [&](int r) { return !items_only && fills_tile(r); };
   double tile_keys = 0, item_keys = 0;
   std::vector<int> item_lengths, tile_lengths;  // of one kv head
   for (int r = 0; r < R; ++r) {
@@ -415,7 +430,9 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   }
   const int S_t_auto = std::max(1024, round_up((int64_t)std::min(s_t, 1.0e9) + 1, 64));
   const int S_i_fill = std::min(1024, std::max(opt.min_item, round_up((int64_t)(item_keys * d.hd / 128 / (2.8 * cus)), 64)));
-  const int S_i_fit = tile_keys > 0 ? 0 : fit_item_split(item_lengths, d.nkv, cus);
+  const int S_i_fit = items_only      ? S_items
+                      : tile_keys > 0 ? 0
+                                      : fit_item_split(item_lengths, d.nkv, cus);
   const int S_i = opt.split_item > 0 ? round_up(opt.split_item, 64)
                   : S_i_fit > 0      ? S_i_fit
                                      : std::max(S_i_fill, round_up((int64_t)(item_keys / (16.0 * cus)) + 1, 64));
@@ -583,7 +600,7 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
       else units.push_back(item_unit_codes[b++]);
     }
   }
-  if (items_only && ni_units <= cus)
+  if (items_only)
     units = by_die(units, [&](int32_t u) { return items[((-1 - u) & ~kUnitMerged) * kItemsPerUnit]; });
   p->n_tiles = nt;
   p->n_items = (int)items.size();

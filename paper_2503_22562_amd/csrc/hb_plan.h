@@ -119,6 +119,7 @@ struct Plan {
   // some row's window hides a key from it: the units have shifts, and the
   // kernels that apply `window` run
   bool windowed = false;
+  bool paired = false;  // item units alone, but for one round of two workgroups per CU
   Window window;
   int sink_blocks = 0;
   // offsets (int32 units) of each section inside meta

@@ -848,7 +848,8 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a) {
 // 109 -> 103 us; larger decode batches 0-1 % faster, none slower): such a
 // launch asks for more LDS than half a CU holds, so one workgroup fits per CU.
 // With tiles, two workgroups per CU (a tile beside a tile or an item group)
-// stay far faster.
+// stay far faster, and the planner asks for two where that makes one round
+// (Plan.paired).
 constexpr int kItemOnlyLds = 96 * 1024;
 
 template <int HD, bool WIN, bool RECORDS>
@@ -857,7 +858,7 @@ void launch(hipStream_t s, const AttnArgs& a) {
   static_assert(2 * lds <= 160 * 1024 && 2 * kItemOnlyLds > 160 * 1024 && kItemOnlyLds <= 160 * 1024, "occupancy");
   static std::atomic<uint64_t> lds_raised{0};
   raise_dynamic_lds(reinterpret_cast<const void*>(&attn_kernel<HD, WIN, RECORDS>), kItemOnlyLds, lds_raised);
-  attn_kernel<HD, WIN, RECORDS><<<a.n_units, 64 * WAVES, a.n_tiles > 0 ? lds : kItemOnlyLds, s>>>(a);
+  attn_kernel<HD, WIN, RECORDS><<<a.n_units, 64 * WAVES, a.n_tiles > 0 || a.paired ? lds : kItemOnlyLds, s>>>(a);
 }
 
 }  // namespace attn_detail
@@ -866,7 +867,7 @@ AttnArgs attention_args(const Dims& d, const Plan& p, const int32_t* meta, const
                         float* part_o, float* part_ml, const RecordPlan* records) {
   AttnArgs at{};
   at.k_pool = static_cast<const uint16_t*>(k_pool); at.v_pool = static_cast<const uint16_t*>(v_pool);
-  at.n_tiles = p.n_tiles; at.n_units = p.n_units; at.n_merge_units = p.n_merge_units;
+  at.n_tiles = p.n_tiles; at.paired = p.paired; at.n_units = p.n_units; at.n_merge_units = p.n_merge_units;
   if (records) {
     at.records = meta;
     at.bt = meta + records->off_bt;

@@ -80,10 +80,11 @@ def test_chunks_as_tiles(hb, monkeypatch, nq, nkv, hd, window, sinks):
     r.check(r.run())
 
 
-@pytest.mark.parametrize("lens", [[(64, 9000)], [(16, 7001), (1, 9), (33, 4000)], [(300, 2500), (1, 2500)], [(700, 0)]])
+@pytest.mark.parametrize("lens", [[(64, 9000)], [(16, 7001), (1, 9), (33, 4000)], [(300, 2500), (1, 2500)], [(700, 0)],
+                                  [(450, 300), (1, 5)]])
 @pytest.mark.parametrize("window,sinks", [(0, 0), (1999, 40)])
 def test_chunks_that_leave_compute_units_idle(hb, lens, window, sinks):
-    """Tiles and items split to fill one round of workgroups, joined over tens of parts."""
+    """Tiles and items cut to fill one round of workgroups (of one or two per CU), joined over tens of parts."""
     r = Run(heads(16, 2, 128), lens, window, sinks, seed=31)
     r.check(r.run())
 
