@@ -137,7 +137,7 @@ struct AttnArgs {
   const uint16_t* k_pool;
   const uint16_t* v_pool;
   const int32_t* tiles;   // workgroup tiles (AttnItem)
-  int n_tiles, paired;  // (paired: see Plan)
+  int n_tiles, paired, half_tiles;  // (the latter two: see Plan)
   const int32_t* items;   // wave items (AttnItem)
   const int32_t* units;   // per workgroup: tile index, or -1 - (group of 4 items)
   int n_units;

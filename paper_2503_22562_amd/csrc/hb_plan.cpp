@@ -445,13 +445,25 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   // keys on eight heads 49.4 -> 52.0, 256 of 50-1000 82.4 -> 84.4).
   const bool few_items = opt.fit_round && item_lengths.size() * (size_t)d.nkv < 4 * (size_t)cus;
   const int S_1 = few_items ? std::min(S_i, 256) : S_i;
-  // Tiles that leave CUs idle are split for one round too, beside the item units.
+  // Tiles that leave CUs idle are split for one round too, beside the item units,
+  // or, where that is sooner done, halved: one round of two half tiles per CU,
+  // which hide each other's latencies (0.57 us a step of 32 keys; a tile alone
+  // 0.61), with nothing to merge. Of t tiles a split spreads the keys over all
+  // CUs, so halves win while (CUs - t) keys are few: eight kv heads, cold caches,
+  // 128 tiles of 512 keys 17.9 -> 14.9 us, of 1000 25.9 -> 22.3, 2500 even; 192
+  // of 1800 39.5 -> 33.8, of 2800 even; 256 of 9000 172 -> 161; 64 of 1250 lose.
+  constexpr int64_t kHalfTileKeys = 160 * 1024;
   int S_t_fit = 0;
+  p->half_tiles = false;
   if (opt.fit_round) {
     int64_t quarters = 0;  // of item units
     for (int n : item_lengths)
       quarters += n <= S_1 ? 1 : ((n + S_i - 1) / S_i + kItemsPerUnit - 1) / kItemsPerUnit * kItemsPerUnit;
-    S_t_fit = fit_tile_split(tile_lengths, d.nkv, cus - quarters * d.nkv / kItemsPerUnit);
+    const int64_t item_groups = quarters * d.nkv / kItemsPerUnit, t = (int64_t)tile_lengths.size() * d.nkv;
+    const int longest = tile_lengths.empty() ? 0 : *std::max_element(tile_lengths.begin(), tile_lengths.end());
+    p->half_tiles = opt.split_tile <= 0 && t > 0 && t <= cus && (cus - t) * longest <= kHalfTileKeys &&
+                    2 * t + item_groups <= 2 * cus;
+    S_t_fit = p->half_tiles ? round_up(longest, 64) : fit_tile_split(tile_lengths, d.nkv, cus - item_groups);
   }
   const int S_t = opt.split_tile > 0 ? round_up(opt.split_tile, 64) : S_t_fit > 0 ? S_t_fit : S_t_auto;
   p->split_tile = S_t;
@@ -482,7 +494,7 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   for (int r = 0; r < R; ++r) {
     const int c = rq[r].chunk_len, x = rq[r].context_len;
     const bool tile = is_tile(r);
-    const int w = tile ? d.BQ : d.P, S = tile ? S_t : S_i;
+    const int w = !tile ? d.P : p->half_tiles ? d.BQ / 2 : d.BQ, S = tile ? S_t : S_i;
     for (int g = 0; g < d.nkv; ++g) {
       for (int i0 = 0; i0 < c; i0 += w) {
         const int npos = std::min(w, c - i0);

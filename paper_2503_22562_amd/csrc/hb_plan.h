@@ -120,6 +120,7 @@ struct Plan {
   // kernels that apply `window` run
   bool windowed = false;
   bool paired = false;  // item units alone, but for one round of two workgroups per CU
+  bool half_tiles = false;  // tiles of kTileCols / 2 columns (a plan of records)
   Window window;
   int sink_blocks = 0;
   // offsets (int32 units) of each section inside meta

@@ -640,13 +640,13 @@ __device__ __forceinline__ void tile_step(const AttnArgs& a, const AttnItem& it,
   tile_pv<HD, CT>(o, vf, pf);
 }
 
-template <int HD, bool WIN, bool RECORDS>
+// CT: 16-column tiles per wave, two, or one in a plan of half tiles.
+template <int HD, int CT, bool WIN, bool RECORDS>
 __device__ __forceinline__ void tile_unit(const AttnArgs& a, const WaveStart<WIN, RECORDS>& start, uint8_t* smem) {
   const AttnItem& it = start.it;
   const BlockIds<WIN>& blocks = start.blocks;
   using TG = TileGeom<HD>;
   constexpr int KC = HD / 32, DT = HD / 16;
-  constexpr int CT = 2;  // 16-column tiles per wave (4 waves x 32 columns)
   const int lane = threadIdx.x & 63, wave = wave_id();
   const int G = a.nq / a.nkv;
   const int col = lane & 15, grp = lane >> 4;
@@ -655,7 +655,7 @@ __device__ __forceinline__ void tile_unit(const AttnArgs& a, const WaveStart<WIN
   int pos[CT];
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
-    const int c = 32 * wave + 16 * ct + col;
+    const int c = 16 * (CT * wave + ct) + col;
     const int pi = c / G;
     const bool valid = pi < it.npos;
     pos[ct] = it.pos0 + pi;
@@ -732,21 +732,21 @@ __device__ __forceinline__ void tile_unit(const AttnArgs& a, const WaveStart<WIN
     step(yes, yes, kt, sa, sb);
   }
 #pragma unroll
-  for (int ct = 0; ct < CT; ++ct) store_column<HD>(a, it, 32 * wave + 16 * ct + col, o[ct], m[ct], rows_sum(l[ct]), grp);
+  for (int ct = 0; ct < CT; ++ct) store_column<HD>(a, it, 16 * (CT * wave + ct) + col, o[ct], m[ct], rows_sum(l[ct]), grp);
 }
 
-template <int HD, bool WIN, bool RECORDS>
+template <int HD, bool WIN, bool RECORDS, bool HALF>
 __global__ __launch_bounds__(64 * WAVES, 2) void attn_kernel(AttnArgs a) {
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
   if constexpr (RECORDS) {
     const UnitRec r = const_load(reinterpret_cast<const UnitRec*>(a.records) + WAVES * blockIdx.x + wave_id());
     const WaveStart<WIN, true> start = start_of<WIN>(a, r);
-    if (r.kind == kRecTile) tile_unit<HD, WIN, true>(a, start, smem);
+    if (r.kind == kRecTile) tile_unit<HD, HALF ? 1 : 2, WIN, true>(a, start, smem);
     else item_unit<HD, WIN, true>(a, start, r.kind == kRecMerged, smem);
   } else {
     const int unit = const_load(a.units + blockIdx.x);
     if (unit >= 0) {
-      tile_unit<HD, WIN, false>(a, start_of<WIN>(a, a.tiles, a.tile_shift, unit), smem);
+      tile_unit<HD, 2, WIN, false>(a, start_of<WIN>(a, a.tiles, a.tile_shift, unit), smem);
     } else {
       const int code = -unit - 1, idx = (code & ~kUnitMerged) * WAVES + wave_id();
       item_unit<HD, WIN, false>(a, start_of<WIN>(a, a.items, a.item_shift, idx), code & kUnitMerged, smem);
@@ -852,13 +852,13 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a) {
 // (Plan.paired).
 constexpr int kItemOnlyLds = 96 * 1024;
 
-template <int HD, bool WIN, bool RECORDS>
+template <int HD, bool WIN, bool RECORDS, bool HALF>
 void launch(hipStream_t s, const AttnArgs& a) {
   constexpr int lds = TSTAGES * TileGeom<HD>::STAGE;
   static_assert(2 * lds <= 160 * 1024 && 2 * kItemOnlyLds > 160 * 1024 && kItemOnlyLds <= 160 * 1024, "occupancy");
   static std::atomic<uint64_t> lds_raised{0};
-  raise_dynamic_lds(reinterpret_cast<const void*>(&attn_kernel<HD, WIN, RECORDS>), kItemOnlyLds, lds_raised);
-  attn_kernel<HD, WIN, RECORDS><<<a.n_units, 64 * WAVES, a.n_tiles > 0 || a.paired ? lds : kItemOnlyLds, s>>>(a);
+  raise_dynamic_lds(reinterpret_cast<const void*>(&attn_kernel<HD, WIN, RECORDS, HALF>), kItemOnlyLds, lds_raised);
+  attn_kernel<HD, WIN, RECORDS, HALF><<<a.n_units, 64 * WAVES, a.n_tiles > 0 || a.paired ? lds : kItemOnlyLds, s>>>(a);
 }
 
 }  // namespace attn_detail
@@ -867,7 +867,8 @@ AttnArgs attention_args(const Dims& d, const Plan& p, const int32_t* meta, const
                         float* part_o, float* part_ml, const RecordPlan* records) {
   AttnArgs at{};
   at.k_pool = static_cast<const uint16_t*>(k_pool); at.v_pool = static_cast<const uint16_t*>(v_pool);
-  at.n_tiles = p.n_tiles; at.paired = p.paired; at.n_units = p.n_units; at.n_merge_units = p.n_merge_units;
+  at.n_tiles = p.n_tiles; at.paired = p.paired; at.half_tiles = p.half_tiles;
+  at.n_units = p.n_units; at.n_merge_units = p.n_merge_units;
   if (records) {
     at.records = meta;
     at.bt = meta + records->off_bt;
@@ -888,13 +889,16 @@ AttnArgs attention_args(const Dims& d, const Plan& p, const int32_t* meta, const
 
 void launch_attention(hipStream_t s, const AttnArgs& a) {
   if (a.n_units <= 0) return;
-  auto go = [&](auto windowed, auto records) {
-    constexpr bool W = decltype(windowed)::value, R = decltype(records)::value;
-    if (a.hd == 128) attn_detail::launch<128, W, R>(s, a);
-    else attn_detail::launch<64, W, R>(s, a);
+  constexpr std::true_type yes{};
+  constexpr std::false_type no{};
+  auto go = [&](auto windowed, auto records, auto half) {
+    constexpr bool W = decltype(windowed)::value, R = decltype(records)::value, H = decltype(half)::value;
+    if (a.hd == 128) attn_detail::launch<128, W, R, H>(s, a);
+    else attn_detail::launch<64, W, R, H>(s, a);
   };
-  if (a.records) a.windowed ? go(std::true_type{}, std::true_type{}) : go(std::false_type{}, std::true_type{});
-  else a.windowed ? go(std::true_type{}, std::false_type{}) : go(std::false_type{}, std::false_type{});
+  if (!a.records) a.windowed ? go(yes, no, no) : go(no, no, no);
+  else if (a.half_tiles) a.windowed ? go(yes, yes, yes) : go(no, yes, yes);
+  else a.windowed ? go(yes, yes, no) : go(no, yes, no);
 }
 
 void launch_attn_merge(hipStream_t s, const AttnArgs& a) {

@@ -89,6 +89,15 @@ def test_chunks_that_leave_compute_units_idle(hb, lens, window, sinks):
     r.check(r.run())
 
 
+@pytest.mark.parametrize("nq,nkv,hd,lens", [(4, 2, 64, [(800, 0)] * 3), (16, 1, 64, [(600, 0), (1, 77)]),
+                                            (8, 8, 128, [(400, 10)] * 3), (32, 8, 128, [(301, 222), (1, 600)])])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (100, 3), (450, 70)])
+def test_half_tiles(hb, nq, nkv, hd, lens, window, sinks):
+    """More wave items than two rounds take, and few enough keys for two half tiles per CU."""
+    r = Run(heads(nq, nkv, hd), lens, window, sinks, seed=32)
+    r.check(r.run())
+
+
 @pytest.mark.parametrize("split_tile,split_item", [(64, 64), (128, 64), (512, 256)])
 @pytest.mark.parametrize("window,sinks", [(0, 0), (333, 20), (900, 0)])
 def test_split_over_the_length(hb, monkeypatch, split_tile, split_item, window, sinks):

@@ -152,7 +152,8 @@ def test_small_launches_fit_one_round(driver, name, reqs, window, units):
     ("tp8", [(512, 2000)], 0, sum(-(-n // 320) for n in range(2016, 2513, 16)), None),
     ("tp8", [(64, 16000)], 0, 4 * 42, None),  # no finer than 3 sqrt(keys): 384
     ("tp8", [(550, 0)], 0, 0, 96 // 4 + 179),  # 275 groups, two workgroups per CU: 96 of up to 192 keys, a wave each
-    ("tp8", [(576, 0)] * 2, 0, 72, 72),        # 576 groups are too many; up to 576 keys a tile stays whole
+    ("tp8", [(576, 0)] * 2, 0, 144, 144),      # 576 groups are too many: two half tiles per CU, (256 - 72) 576 keys
+    ("tp8", [(576, 1500)] * 2, 1480, 72 * 3, None),  # 1496 to 1511 keys of the window: in three
     ("tp8", [(64, 16000), (1, 100), (1, 100)], 0, 4 * 42, 4 * 42 + 2),  # (items are cut at 64 keys: a unit each)
 ])
 def test_small_launches_with_chunks_fit_one_round(driver, name, reqs, window, tiles, units):
