@@ -369,7 +369,8 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   bool items_only = false;
   int S_items = 0;
   p->paired = false;
-  if (opt.fit_round && opt.split_tile <= 0 && opt.split_item <= 0) {
+  const bool fit_chunks = opt.fit_round && opt.split_tile <= 0 && opt.split_item <= 0;
+  if (fit_chunks) {
     int64_t n = 0;
     bool chunks = false;
     for (int r = 0; r < R; ++r) {
@@ -455,13 +456,13 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   constexpr int64_t kHalfTileKeys = 160 * 1024;
   int S_t_fit = 0;
   p->half_tiles = false;
-  if (opt.fit_round) {
+  if (fit_chunks) {
     int64_t quarters = 0;  // of item units
     for (int n : item_lengths)
       quarters += n <= S_1 ? 1 : ((n + S_i - 1) / S_i + kItemsPerUnit - 1) / kItemsPerUnit * kItemsPerUnit;
     const int64_t item_groups = quarters * d.nkv / kItemsPerUnit, t = (int64_t)tile_lengths.size() * d.nkv;
     const int longest = tile_lengths.empty() ? 0 : *std::max_element(tile_lengths.begin(), tile_lengths.end());
-    p->half_tiles = opt.split_tile <= 0 && t > 0 && t <= cus && (cus - t) * longest <= kHalfTileKeys &&
+    p->half_tiles = t > 0 && t <= cus && (cus - t) * longest <= kHalfTileKeys &&
                     2 * t + item_groups <= 2 * cus;
     S_t_fit = p->half_tiles ? round_up(longest, 64) : fit_tile_split(tile_lengths, d.nkv, cus - item_groups);
   }
