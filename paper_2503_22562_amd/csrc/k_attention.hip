@@ -15,14 +15,15 @@
 // Two kinds of work share the launch, one per 256-thread workgroup (4 waves;
 // two workgroups per CU, so a compute-bound tile and a bandwidth-bound item
 // group can run side by side on one CU; one per CU when the launch holds no
-// tiles):
+// tiles, but for the planner's paired launches):
 //  * chunk tiles: 128 columns (4 waves x 32) of one request and kv head over a
 //    key range; 32-key K/V steps (two pool blocks) are copied as stored into
 //    a 4-stage LDS ring by global-to-LDS loads and every wave reads them from
 //    there (the pool's K layout puts a fragment read's 8 keys of one
 //    dimension chunk in one 128-byte line; the second block sits 128 bytes
 //    off, so reads do not collide in banks). Compute-bound: 32 MFMAs per wave
-//    per step.
+//    per step. In launches of at most one such tile per CU the planner may ask
+//    for tiles of 64 columns (4 waves x 16), two per CU.
 //  * wave items: 16 columns (decodes, short chunks) per wave, four per
 //    workgroup; each wave streams its K/V straight into registers, the next
 //    32-key step loading while the current one is multiplied. HBM-bound.
