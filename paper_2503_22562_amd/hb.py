@@ -410,6 +410,7 @@ class Attention:
         self.row = cfg.n_q_heads * cfg.head_dim             # values of a row of q
         self.block_values = cfg.n_kv_heads * 16 * cfg.head_dim  # values of a block of one pool
         self.n_tokens = 0
+        self.pool = hb_kv_pool(0, 0, num_blocks)            # of the call at hand
 
     def __del__(self):
         try:
@@ -420,6 +421,8 @@ class Attention:
 
 def hb_create_attention(cfg: hb_layer_config, num_blocks: int, stream: Optional[int] = None) -> Attention:
     import torch
+    global _bf16
+    _bf16 = torch.bfloat16
     if stream is None:
         stream = torch.cuda.current_stream().cuda_stream
     h = C.c_void_p()
@@ -441,11 +444,14 @@ def hb_plan_attention(attention: Attention, requests: Sequence[Tuple[int, int, I
     attention.n_tokens = sum(int(r[0]) for r in requests)
 
 
-def _rows(name: str, t, n: int, row: int, bf16, device: int) -> int:
+_bf16 = None  # torch.bfloat16, once torch is there
+
+
+def _rows(name: str, t, n: int, row: int, device: int) -> int:
     """Row stride of n rows of `row` contiguous bf16 values ([n][heads][head_dim] or [n][heads * head_dim])."""
-    if t.dtype != bf16 or t.get_device() != device:
+    if t.dtype is not _bf16 or t.get_device() != device:
         raise ValueError(f"{name}: a bf16 tensor on GPU {device}, not {t.dtype} on {t.device}")
-    if t.numel() != n * row or t.dim() < 2 or t.shape[0] != n:
+    if t.numel() != n * row or t.dim() < 2 or t.size(0) != n:
         raise ValueError(f"{name}: {n} rows of {row} values, not {tuple(t.shape)}")
     if t.is_contiguous():
         return row
@@ -460,18 +466,19 @@ def _rows(name: str, t, n: int, row: int, bf16, device: int) -> int:
 
 def hb_run_attention(attention: Attention, q, k_pool, v_pool, out) -> None:
     """q, out: bf16 [T][n_q_heads][head_dim] (or [T][n_q_heads * head_dim]), rows any multiple of 8 elements apart."""
-    from torch import bfloat16
+    # (written for few calls of few attributes: beside a small launch they are most of the time)
     blocks, device = attention.num_blocks, attention.device
-    for name, p in (("k_pool", k_pool), ("v_pool", v_pool)):
-        if p.dtype != bfloat16 or p.get_device() != device or not p.is_contiguous():
-            raise ValueError(f"{name}: a contiguous bf16 tensor on GPU {device}")
-        have = p.shape[0]
-        if have < blocks or p.numel() != have * attention.block_values:
-            raise ValueError(f"{name}: at least {blocks} blocks of {attention.block_values} values, not {tuple(p.shape)}")
-    n, row = attention.n_tokens, attention.row
-    qs, os_ = _rows("q", q, n, row, bfloat16, device), _rows("out", out, n, row, bfloat16, device)
-    status = load().hb_run_attention(attention.handle, hb_kv_pool(k_pool.data_ptr(), v_pool.data_ptr(), blocks),
-                                     q.data_ptr(), qs, out.data_ptr(), os_)
+    for p in (k_pool, v_pool):
+        if p.dtype is not _bf16 or p.get_device() != device or not p.is_contiguous():
+            raise ValueError(f"{'k_pool' if p is k_pool else 'v_pool'}: a contiguous bf16 tensor on GPU {device}")
+        have = p.numel()
+        if have < blocks * attention.block_values or have % attention.block_values:
+            raise ValueError(f"{'k_pool' if p is k_pool else 'v_pool'}: at least {blocks} blocks of "
+                             f"{attention.block_values} values, not {tuple(p.shape)}")
+    n, row, pool = attention.n_tokens, attention.row, attention.pool
+    pool.k_pool, pool.v_pool = k_pool.data_ptr(), v_pool.data_ptr()
+    status = load().hb_run_attention(attention.handle, pool, q.data_ptr(), _rows("q", q, n, row, device),
+                                     out.data_ptr(), _rows("out", out, n, row, device))
     if status:
         _check(status)
 
