@@ -312,8 +312,23 @@ def hb_destroy_layer(layer: Layer) -> None:
         layer.handle = None
 
 
+_INT32 = np.dtype(np.int32)
+
+
 def _i32(a) -> np.ndarray:
-    return np.ascontiguousarray(a, dtype=np.int32)
+    """The values of `a` as int32, or a ValueError: NumPy checks Python integers by itself, but keeps the low 32 bits
+    of an array's wider ones."""
+    if getattr(a, "dtype", _INT32) is _INT32:
+        try:
+            return np.ascontiguousarray(a, dtype=np.int32)
+        except OverflowError as e:
+            raise ValueError(str(e)) from None
+    a = np.asarray(a)
+    with np.errstate(invalid="ignore"):
+        b = np.ascontiguousarray(a, dtype=np.int32)
+    if (a != b).any():
+        raise ValueError(f"values of {a.dtype} that are no 32-bit integers")
+    return b
 
 
 def _int32(v) -> int:
@@ -325,18 +340,18 @@ def _int32(v) -> int:
 
 
 def _ids(a) -> np.ndarray:
-    """Block ids as a new or the caller's int32 array. (NumPy checks Python integers by itself, not those of arrays.)"""
-    if getattr(a, "dtype", np.int32) != np.int32:
+    """Block ids as a new or the caller's int32 array."""
+    if getattr(a, "dtype", _INT32) is not _INT32:
         a = np.asarray(a)
-        if a.size and (a.dtype.kind not in "iu" or a.min() < -(1 << 31) or a.max() >= 1 << 31):
-            raise ValueError(f"block ids are 32-bit integers, not these of {a.dtype}")
+        if a.size and a.dtype.kind not in "iu":
+            raise ValueError(f"block ids are 32-bit integers, not {a.dtype}")
     return _i32(a)
 
 
 def hb_append_kv(layer: Layer, block_table, context_len: int, k, v) -> None:
     bt = _i32(block_table)
     n = 0 if k is None else int(k.shape[0])
-    _check(load().hb_append_kv(layer.handle, bt.ctypes.data_as(C.POINTER(C.c_int32)), len(bt), int(context_len), n,
+    _check(load().hb_append_kv(layer.handle, bt.ctypes.data_as(C.POINTER(C.c_int32)), len(bt), _int32(context_len), _int32(n),
                                C.c_void_p(_ptr(k)), C.c_void_p(_ptr(v))))
 
 
@@ -351,12 +366,12 @@ _REQ_DTYPE = np.dtype({"names": ["chunk_len", "context_len", "block_table", "n_b
 
 def _desc(requests: Sequence[Tuple[int, int, Iterable[int]]], x_in_ptr: int, x_out_ptr: int, out_dtype: int):
     n = len(requests)
-    tables = [_i32(bt) for (_, _, bt) in requests]
+    tables = [bt if getattr(bt, "dtype", None) is _INT32 else _i32(bt) for (_, _, bt) in requests]
     flat = np.concatenate(tables) if n else np.zeros(1, np.int32)
     lens = np.fromiter((len(bt) for bt in tables), dtype=np.int64, count=n)
     rec = np.zeros(max(1, n), dtype=_REQ_DTYPE)
     if n:
-        cx = np.array([(r[0], r[1]) for r in requests], dtype=np.int64).reshape(n, 2)
+        cx = _i32([(r[0], r[1]) for r in requests]).reshape(n, 2)
         rec["chunk_len"][:n] = cx[:, 0]
         rec["context_len"][:n] = cx[:, 1]
         starts = np.concatenate([[0], np.cumsum(lens)[:-1]])
@@ -565,7 +580,7 @@ def _requests_only(requests: Sequence[Tuple[int, int]]):
     """hb_request array of (chunk_len, context_len) pairs without block tables."""
     arr = (hb_request * max(1, len(requests)))()
     for i, r in enumerate(requests):
-        arr[i] = hb_request(int(r[0]), int(r[1]), None, 0)
+        arr[i] = hb_request(_int32(r[0]), _int32(r[1]), None, 0)
     return arr
 
 
