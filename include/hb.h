@@ -291,7 +291,7 @@ hb_status hb_plan_attention(hb_attention* attention, int32_t n_requests, const h
  *               will do), 16-byte aligned
  *   out         device bf16 [T] rows likewise, out_stride elements apart; what
  *               lies between the rows is left untouched. The memory from the
- *               first to the last row must not overlap that of q
+ *               first to the last row must not overlap that of q or of a pool
  * Errors: HB_ERR_INVALID (null pointer, no plan, a pool of fewer blocks, a
  * stride below n_q_heads * head_dim or not a multiple of 8, misaligned pointer,
  * overlap), HB_ERR_HIP (among others: the stream is under graph capture). */

@@ -194,6 +194,9 @@ hb_status hb_run_attention(hb_attention* a, const hb_kv_pool* pool, const void* 
   const uintptr_t q0 = (uintptr_t)q, q1 = q0 + ((uintptr_t)(p.T - 1) * q_stride + row) * 2;
   const uintptr_t o0 = (uintptr_t)out, o1 = o0 + ((uintptr_t)(p.T - 1) * out_stride + row) * 2;
   if (q0 < o1 && o0 < q1) return fail(HB_ERR_INVALID, "out overlaps q");
+  const uintptr_t pool_bytes = (uintptr_t)pool->num_blocks * a->d.nkv * 16 * a->d.hd * 2;
+  for (const void* x : {(const void*)pool->k_pool, (const void*)pool->v_pool})
+    if ((uintptr_t)x < o1 && o0 < (uintptr_t)x + pool_bytes) return fail(HB_ERR_INVALID, "out overlaps a pool");
   const DeviceGuard on(a->device);
   const hb_status st = refuse_capture(a->stream);
   if (st != HB_OK) return st;
