@@ -28,6 +28,8 @@
  *    results or reusing inputs. Host arrays passed to them (request tables,
  *    block tables) are copied during the call and may be freed on return.
  *  - A layer is used from one host thread at a time.
+ *  - No exception leaves a call: where host memory runs out, the status is
+ *    HB_ERR_OOM.
  */
 #ifndef HB_H_
 #define HB_H_
@@ -42,7 +44,7 @@ typedef enum {
   HB_OK = 0,
   HB_ERR_INVALID = 1,     /* malformed argument: null pointer, bad length, overlap */
   HB_ERR_RANGE = 2,       /* a block id outside [0, num_blocks) */
-  HB_ERR_OOM = 3,         /* device or pinned host allocation failed */
+  HB_ERR_OOM = 3,         /* device, pinned or ordinary host allocation failed */
   HB_ERR_HIP = 4,         /* a HIP runtime call failed; hb_last_error() names it */
   HB_ERR_UNSUPPORTED = 5  /* a shape the kernels do not implement */
 } hb_status;

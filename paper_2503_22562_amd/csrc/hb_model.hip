@@ -70,7 +70,8 @@ hb_status hb_create_model(const hb_layer_config* cfg, const hb_model_desc* md, v
   // the LM head is a B operand of the layer GEMM
   st = check_window("lm_head", md->vocab, d.H);
   if (st != HB_OK) return st;
-  hb_model* m = new hb_model;
+  hb_model* m = new (std::nothrow) hb_model;
+  if (!m) return host_oom();
   m->cfg = *cfg;
   m->embed = static_cast<const uint16_t*>(md->embed);
   m->g_final = static_cast<const uint16_t*>(md->g_final);
@@ -84,6 +85,8 @@ hb_status hb_create_model(const hb_layer_config* cfg, const hb_model_desc* md, v
   if (hipGetDevice(&dev) != hipSuccess || hipGetDeviceProperties(&prop, dev) != hipSuccess)
     return bail(fail(HB_ERR_HIP, "device query failed"));
   m->cu_count = prop.multiProcessorCount;
+  st = guarded([&] { return m->layers.reserve(md->n_layers), HB_OK; });
+  if (st != HB_OK) return bail(st);
   for (int l = 0; l < md->n_layers; ++l) {
     hb_layer* L = nullptr;
     st = hb_create_layer(cfg, &md->layers[l], &md->pools[l], hip_stream, &L);
@@ -118,7 +121,7 @@ hb_status hb_copy_model_blocks(hb_model* m, const int32_t* src, const int32_t* d
   return guarded([&] { return copy_stack_blocks(m->layers.data(), (int)m->layers.size(), src, dst, n); });
 }
 
-hb_status hb_run_model(hb_model* m, const hb_model_batch* b) {
+hb_status hb_run_model(hb_model* m, const hb_model_batch* b) try {
   if (!m || !b) return fail(HB_ERR_INVALID, "null model or batch");
   if (!b->token_ids || !b->next_tokens) return fail(HB_ERR_INVALID, "null token_ids or next_tokens");
   if (b->n_requests < 1) return fail(HB_ERR_INVALID, "empty batch");
@@ -126,7 +129,7 @@ hb_status hb_run_model(hb_model* m, const hb_model_batch* b) {
   const int H = c.hidden, R = b->n_requests;
   // all layers share shape and pool size; their windows may differ
   hb_batch_desc desc{b->n_requests, b->requests, m->x[0], m->x[1], HB_OUT_BF16};
-  hb_status st = guarded([&] { return check_layer_stack(m->layers.data(), (int)m->layers.size(), &desc); });
+  hb_status st = check_layer_stack(m->layers.data(), (int)m->layers.size(), &desc);
   if (st == HB_OK) st = refuse_capture(m->stream);
   if (st != HB_OK) return st;
   int T = 0;
@@ -160,7 +163,7 @@ hb_status hb_run_model(hb_model* m, const hb_model_batch* b) {
     xout[l] = next;
     cur = next;
   }
-  st = guarded([&] { return run_layer_stack(m->layers.data(), (int)nl, &desc, xin.data(), xout.data()); });
+  st = run_layer_stack(m->layers.data(), (int)nl, &desc, xin.data(), xout.data());
   if (st != HB_OK) return st;
   launch_gather_rows(m->stream, cur, T, m->rows_dev, R, H, m->last);
   launch_rmsnorm(m->stream, m->last, false, m->g_final, m->normed, R, H, c.rms_eps);
@@ -189,6 +192,8 @@ hb_status hb_run_model(hb_model* m, const hb_model_batch* b) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(HB_ERR_HIP, "model launch: %s", hipGetErrorString(e));
   return HB_OK;
+} catch (const std::bad_alloc&) {
+  return host_oom();
 }
 
 }  // extern "C"

@@ -26,6 +26,8 @@ hb_status fail(hb_status st, const char* fmt, ...) {
 
 const char* last_error() { return g_err.c_str(); }
 
+hb_status host_oom() { return fail(HB_ERR_OOM, "host allocation failed"); }
+
 hb_status check_config(const hb_layer_config* c, Dims* d) {
   if (!c) return fail(HB_ERR_INVALID, "null layer config");
   if (c->hidden <= 0 || c->n_q_heads <= 0 || c->n_kv_heads <= 0 || c->head_dim <= 0 ||
@@ -157,6 +159,7 @@ hb_status check_batch(const Dims& d, int num_blocks, const hb_batch_desc* desc, 
   SlotMarks* m = marks ? marks : &local;
   if ((int)m->mask.size() < num_blocks) m->mask.assign(num_blocks, 0);
   m->touched.clear();
+  m->touched.reserve(T);  // nothing can fail while marks stand
   for (int r = 0; r < R && st == HB_OK; ++r) {
     const hb_request& q = desc->requests[r];
     for (int64_t p = q.context_len; p < (int64_t)q.context_len + q.chunk_len; ++p) {
@@ -731,7 +734,7 @@ extern "C" hb_status hb_plan_compaction(int32_t num_blocks, int32_t* const* tabl
   try {
     return plan_compaction(num_blocks, tables, n_blocks, n_tables, src, dst, n_moves, n_used);
   } catch (const std::bad_alloc&) {
-    return fail(HB_ERR_OOM, "host allocation failed");
+    return host_oom();
   }
 }
 

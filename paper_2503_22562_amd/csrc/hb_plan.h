@@ -17,6 +17,8 @@ namespace hb {
 // Set the thread-local message returned by hb_last_error(); returns `st`.
 hb_status fail(hb_status st, const char* fmt, ...);
 const char* last_error();
+// The status of a C entry that caught std::bad_alloc: no exception leaves one.
+hb_status host_oom();
 
 struct Dims {
   int H = 0, nq = 0, nkv = 0, hd = 0, F = 0, blk = 16;

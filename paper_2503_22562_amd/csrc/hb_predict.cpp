@@ -9,6 +9,7 @@
 #include <cmath>
 #include <cstring>
 #include <limits>
+#include <new>
 #include <vector>
 
 #include "hb.h"
@@ -122,7 +123,7 @@ extern "C" hb_status hb_latency_features(const hb_layer_config* cfg, const hb_re
 
 extern "C" hb_status hb_fit_latency_model(const hb_layer_config* cfg, const int32_t* chunk_sizes, int32_t n_chunk,
                                           const hb_decode_mix* mixes, int32_t n_mix, const hb_profile_cell* cells,
-                                          hb_latency_model* out) {
+                                          hb_latency_model* out) try {
   if (!check_cfg(cfg) || !chunk_sizes || !mixes || !cells || !out || n_chunk <= 0 || n_mix <= 0)
     return fail(HB_ERR_INVALID, "hb_fit_latency_model: null pointer or empty profile");
   const int rows = n_chunk * n_mix;
@@ -181,6 +182,8 @@ extern "C" hb_status hb_fit_latency_model(const hb_layer_config* cfg, const int3
   out->fit_max_under = under;
   out->n_cells = rows;
   return HB_OK;
+} catch (const std::bad_alloc&) {
+  return host_oom();
 }
 
 extern "C" hb_status hb_predict_latency(const hb_latency_model* model, const hb_layer_config* cfg,
@@ -196,7 +199,7 @@ extern "C" hb_status hb_predict_latency(const hb_latency_model* model, const hb_
 extern "C" hb_status hb_select_chunk(const hb_latency_model* model, const hb_layer_config* cfg,
                                      const int32_t* decode_contexts, const double* decode_deadlines_ms,
                                      int32_t n_decode, double now_ms, int32_t chunk_context, int32_t max_chunk,
-                                     int32_t granularity, double margin, int32_t* chunk, double* predicted_ms) {
+                                     int32_t granularity, double margin, int32_t* chunk, double* predicted_ms) try {
   if (!model || !check_cfg(cfg) || !chunk || !predicted_ms || n_decode < 0 ||
       (n_decode > 0 && (!decode_contexts || !decode_deadlines_ms)))
     return fail(HB_ERR_INVALID, "hb_select_chunk: null pointer or bad size");
@@ -244,4 +247,6 @@ extern "C" hb_status hb_select_chunk(const hb_latency_model* model, const hb_lay
   *chunk = best;
   *predicted_ms = best_ms;
   return HB_OK;
+} catch (const std::bad_alloc&) {
+  return host_oom();
 }

@@ -47,13 +47,13 @@ class DeviceGuard {
   int before_ = -1;
 };
 
-// f(), with a failed host allocation as a status: no exception leaves a C entry.
+// f(), with a failed host allocation as a status.
 template <typename F>
 hb_status guarded(F&& f) {
   try {
     return f();
   } catch (const std::bad_alloc&) {
-    return fail(HB_ERR_OOM, "host allocation failed");
+    return host_oom();
   }
 }
 

@@ -516,8 +516,8 @@ hb_status settle_device(hb_layer* L, const hb_batch_desc* desc, hipEvent_t e0, h
 // write-back does not fall into the timed interval); the batch is planned
 // and its metadata uploaded before the start event, so the interval holds
 // the kernels alone. Fills the cell.
-hb_status time_batch(hb_layer* L, const hb_batch_desc* desc, int warmup, int iters, void* flush,
-                     int64_t flush_bytes, std::vector<hipEvent_t>& ev, std::vector<float>& lat, hb_profile_cell* cell) {
+hb_status time_batch(hb_layer* L, const hb_batch_desc* desc, int warmup, int iters, void* flush, int64_t flush_bytes,
+                     std::vector<hipEvent_t>& ev, std::vector<float>& lat, hb_profile_cell* cell) try {
   hb_status st = check_batch(L->d, L->pool.num_blocks, desc, &L->marks, L->plan_opt.window);
   if (st != HB_OK) return st;
   for (int i = 0; i < warmup && st == HB_OK; ++i) st = hb_run_iteration(L, desc);
@@ -554,6 +554,8 @@ hb_status time_batch(hb_layer* L, const hb_batch_desc* desc, int warmup, int ite
   cell->hbm_frac = (float)(bytes / sec / kPeakHbm);
   cell->mfma_frac = (float)(flops / sec / kPeakBf16);
   return HB_OK;
+} catch (const std::bad_alloc&) {  // (the caller still frees its buffers)
+  return host_oom();
 }
 
 // splitmix64 stream for the profiler's host-side draws
@@ -715,11 +717,13 @@ extern "C" {
 
 const char* hb_last_error(void) { return last_error(); }
 
-hb_status hb_validate_batch(const hb_layer_config* cfg, int32_t num_blocks, const hb_batch_desc* desc) {
+hb_status hb_validate_batch(const hb_layer_config* cfg, int32_t num_blocks, const hb_batch_desc* desc) try {
   Dims d;
   hb_status st = check_config(cfg, &d);
   if (st != HB_OK) return st;
   return check_batch(d, num_blocks, desc, nullptr);
+} catch (const std::bad_alloc&) {
+  return host_oom();
 }
 
 hb_status hb_create_layer(const hb_layer_config* cfg, const hb_layer_weights* w, const hb_kv_pool* pool,
@@ -762,9 +766,9 @@ hb_status hb_create_layer(const hb_layer_config* cfg, const hb_layer_weights* w,
   };
   for (auto& a : allocs)
     if (!dev_alloc(L, a.p, a.bytes)) return bail(fail(HB_ERR_OOM, "workspace allocation of %zu B", a.bytes));
-  std::vector<double> inv(d.hd / 2);
+  double inv[64];  // head_dim is 64 or 128
   for (int j = 0; j < d.hd / 2; ++j) inv[j] = std::pow((double)d.theta, -2.0 * j / d.hd);
-  if (hipMemcpy(L->inv_freq, inv.data(), inv.size() * sizeof(double), hipMemcpyHostToDevice) != hipSuccess)
+  if (hipMemcpy(L->inv_freq, inv, (size_t)d.hd / 2 * sizeof(double), hipMemcpyHostToDevice) != hipSuccess)
     return bail(fail(HB_ERR_HIP, "upload of RoPE frequencies failed"));
   if (hipStreamCreateWithFlags(&L->copy_stream, hipStreamNonBlocking) != hipSuccess)
     return bail(fail(HB_ERR_HIP, "hipStreamCreate failed"));
@@ -836,7 +840,7 @@ hb_status hb_set_attention_window(hb_layer* L, int32_t window, int32_t sinks) {
   return HB_OK;
 }
 
-hb_status hb_run_iteration(hb_layer* L, const hb_batch_desc* desc) {
+hb_status hb_run_iteration(hb_layer* L, const hb_batch_desc* desc) try {
   if (!L) return fail(HB_ERR_INVALID, "null layer");
   hb_status st = check_batch(L->d, L->pool.num_blocks, desc, &L->marks, L->plan_opt.window);
   if (st != HB_OK) return st;
@@ -845,9 +849,11 @@ hb_status hb_run_iteration(hb_layer* L, const hb_batch_desc* desc) {
   if (st != HB_OK) return st;
   build_plan(L->d, desc, L->cu_count, &L->plan, L->plan_opt);
   return enqueue_layer(L, desc);
+} catch (const std::bad_alloc&) {
+  return host_oom();
 }
 
-hb_status hb_run_iteration_noalloc(hb_layer* L, const hb_batch_desc* desc) {
+hb_status hb_run_iteration_noalloc(hb_layer* L, const hb_batch_desc* desc) try {
   if (!L) return fail(HB_ERR_INVALID, "null layer");
   hb_status st = check_batch(L->d, L->pool.num_blocks, desc, &L->marks, L->plan_opt.window);
   if (st != HB_OK) return st;
@@ -922,6 +928,8 @@ hb_status hb_run_iteration_noalloc(hb_layer* L, const hb_batch_desc* desc) {
   pp.timing_mask = 0;  // no events: creating them may allocate
   for (int i = 0; i < HB_GEMM_COUNT; ++i) L->last_plans[i] = pl[i];
   return launch_layer(L, desc, pp);
+} catch (const std::bad_alloc&) {
+  return host_oom();
 }
 
 hb_status hb_set_kernel_timing(hb_layer* L, uint32_t mask) {
@@ -1047,7 +1055,7 @@ hb_status hb_layer_stage(hb_layer* L, int32_t stage, void** dev_ptr, int64_t* ro
 }
 
 hb_status hb_profile(hb_layer* L, const int32_t* chunk_sizes, int32_t n_chunk, const hb_decode_mix* mixes,
-                     int32_t n_mix, int32_t warmup, int32_t iters, uint64_t seed, hb_profile_cell* out) {
+                     int32_t n_mix, int32_t warmup, int32_t iters, uint64_t seed, hb_profile_cell* out) try {
   if (!L || !chunk_sizes || !mixes || !out) return fail(HB_ERR_INVALID, "null argument");
   if (n_chunk < 1 || n_mix < 1 || iters < 1 || warmup < 0) return fail(HB_ERR_INVALID, "empty grid or iters < 1");
   const Dims& d = L->d;
@@ -1079,7 +1087,11 @@ hb_status hb_profile(hb_layer* L, const int32_t* chunk_sizes, int32_t n_chunk, c
   const int64_t flush_bytes = (int64_t)1 << 30;  // 512 MiB written, 512 MiB read
   void *x_in = nullptr, *x_out = nullptr, *flush = nullptr;
   int32_t* blocks_dev = nullptr;
-  std::vector<hipEvent_t> ev;
+  std::vector<hipEvent_t> ev(2 * (size_t)iters, nullptr);
+  std::vector<int32_t> perm(NB);
+  std::vector<hb_request> reqs;
+  std::vector<float> lat(iters);
+  reqs.reserve(1 + (size_t)max_dec);
   hb_status st = HB_OK;
   auto cleanup = [&]() {
     (void)hipStreamSynchronize(L->stream);
@@ -1087,21 +1099,18 @@ hb_status hb_profile(hb_layer* L, const int32_t* chunk_sizes, int32_t n_chunk, c
     if (x_out) (void)hipFree(x_out);
     if (flush) (void)hipFree(flush);
     if (blocks_dev) (void)hipFree(blocks_dev);
-    for (hipEvent_t e : ev) (void)hipEventDestroy(e);
+    for (hipEvent_t e : ev)
+      if (e) (void)hipEventDestroy(e);
   };
   if (hipMalloc(&x_in, maxT * d.H * 2) != hipSuccess || hipMalloc(&x_out, maxT * d.H * 4) != hipSuccess ||
       hipMalloc(&flush, flush_bytes) != hipSuccess || hipMalloc(&blocks_dev, (size_t)NB * sizeof(int32_t)) != hipSuccess) {
     cleanup();
     return fail(HB_ERR_OOM, "profiler buffers");
   }
-  ev.resize(2 * (size_t)iters);
   for (auto& e : ev)
     if (hipEventCreate(&e) != hipSuccess) { cleanup(); return fail(HB_ERR_HIP, "hipEventCreate failed"); }
   launch_fill_random_bf16(L->stream, static_cast<uint16_t*>(x_in), maxT * d.H, seed ^ 0xA5A5u, 1.7f);
 
-  std::vector<int32_t> perm(NB);
-  std::vector<hb_request> reqs;
-  std::vector<float> lat(iters);
   for (int mi = 0; mi < n_mix && st == HB_OK; ++mi) {
     const hb_decode_mix& mx = mixes[mi];
     for (int ci = 0; ci < n_chunk && st == HB_OK; ++ci) {
@@ -1132,10 +1141,12 @@ hb_status hb_profile(hb_layer* L, const int32_t* chunk_sizes, int32_t n_chunk, c
   }
   cleanup();
   return st;
+} catch (const std::bad_alloc&) {
+  return host_oom();
 }
 
 hb_status hb_profile_batches(hb_layer* L, const hb_batch_desc* batches, int32_t n_batches, int32_t warmup,
-                             int32_t iters, hb_profile_cell* out) {
+                             int32_t iters, hb_profile_cell* out) try {
   if (!L || !out || n_batches < 0 || (n_batches > 0 && !batches)) return fail(HB_ERR_INVALID, "null argument");
   if (iters < 1 || warmup < 0) return fail(HB_ERR_INVALID, "iters < 1 or warmup < 0");
   for (int b = 0; b < n_batches; ++b) {
@@ -1164,6 +1175,8 @@ hb_status hb_profile_batches(hb_layer* L, const hb_batch_desc* batches, int32_t 
     st = time_batch(L, &batches[b], warmup, iters, flush, flush_bytes, ev, lat, &out[b]);
   cleanup();
   return st;
+} catch (const std::bad_alloc&) {
+  return host_oom();
 }
 
 }  // extern "C"
