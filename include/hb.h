@@ -246,8 +246,12 @@ hb_status hb_run_iteration_noalloc(hb_layer* layer, const hb_batch_desc* desc);
  * query row and head, K and V read from a pool in the layouts above, keys
  * visible as in hb_run_iteration or under a sliding window with sinks
  * (hb_set_attention_window). Softmax statistics and sums are fp32; the
- * probabilities enter the product with V as bf16. Long key ranges are split and
- * their parts joined in the order of the keys, so a plan's results do not depend
+ * probabilities enter the product with V as bf16. Queries, and the keys and
+ * values that some row sees, must be finite, and |q . k| log2(e) / sqrt(head_dim)
+ * below 2^24: an exponent is the score's product with that factor less the
+ * maximum in one fused step, and the maximum's own rounding, half a unit in its
+ * last place, must stay small against the exponents fp32 has. Long key ranges are
+ * split and their parts joined in a fixed order, so a plan's results do not depend
  * on timing; the splits may differ from hb_run_iteration's, and with them the
  * last bits.
  *

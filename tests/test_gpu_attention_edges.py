@@ -48,3 +48,36 @@ def test_out_must_not_overlap_a_pool(hb):
         H.hb_run_attention(att, q, k, v, out(at))
         torch.cuda.synchronize()
         assert torch.equal(out(at), want), at
+
+
+@pytest.mark.parametrize("nqkvhd,c,x,window", [((8, 2, 128), 1, 700, 1), ((4, 2, 64), 5, 40, 1), ((8, 2, 128), 90, 200, 1),
+                                               ((8, 2, 128), 1, 3000, 0), ((8, 1, 128), 80, 900, 0)])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_scores_of_any_documented_size(hb, nqkvhd, c, x, window, sign):
+    """Scores of 2^26 (exponents of 2^23 and 2^23.5), of either sign. Where a row sees one key, that key's V; where it
+    sees them all, the mean of V over the first 7 keys, whose scores are equal and lie 2^20 and more above the others'.
+    The weights are powers of two off by up to half a unit of the maximum, so they and the output are rounded once each."""
+    import torch
+    from paper_2503_22562_amd import hb as H
+    from paper_2503_22562_amd.harness import to_device_bf16
+    from hb_workloads import bf16_bits_to_f32, f32_to_bf16_bits
+    nq, nkv, hd = nqkvhd
+    n = x + c
+    cache = Cache(heads(*nqkvhd), -(-n // 16), c, 1, seed=43)
+    k, q = np.zeros((n, nkv, hd), np.float32), np.zeros((c, nq, hd), np.float32)
+    q[:, :, 0] = 2.0 ** 13
+    k[:, :, 0] = sign * 2.0 ** 13
+    if not window:
+        k[7:, :, 0] = sign * 2.0 ** 13 - 2.0 ** 8 * (1 + np.arange(n - 7) % 3)[:, None]
+    kb, qb, vb = f32_to_bf16_bits(k), f32_to_bf16_bits(q), cache.bits(n, nkv, hd)
+    table = cache.perm.copy()
+    cache.dl.append_kv(table, 0, kb, vb)
+    att = H.hb_create_attention(cache.dl.cfg, cache.num_blocks)
+    H.hb_plan_attention(att, [(c, x, table)], window, 0)
+    out = torch.empty(c, nq, hd, dtype=torch.bfloat16, device="cuda")
+    H.hb_run_attention(att, to_device_bf16(qb), cache.dl.k_pool, cache.dl.v_pool, out)
+    torch.cuda.synchronize()
+    v = np.repeat(bf16_bits_to_f32(vb).astype(np.float64), nq // nkv, 1)
+    want, size = (v[x:], np.abs(v[x:])) if window else (v[:7].mean(0)[None], np.abs(v[:7]).mean(0)[None])
+    got = out.float().cpu().numpy().astype(np.float64)
+    assert (np.abs(got - want) <= (2.0 ** -8 + 2.0 ** -12) * (size + np.abs(want))).all()
