@@ -519,12 +519,13 @@ def hb_copy_model_blocks(model: Model, src, dst) -> None:
 
 def hb_plan_compaction(num_blocks: int, tables: Sequence[Iterable[int]]):
     """(tables, src, dst, n_used): the tables over blocks [0, n_used), and the moves that make them true."""
+    num_blocks = _int32(num_blocks)
     ts = [_ids(t).reshape(-1).copy() for t in tables]
     ptrs = (C.c_void_p * max(1, len(ts)))(*[t.ctypes.data for t in ts])
     lens = _i32([len(t) for t in ts] or [0])
-    src, dst = (np.zeros(max(1, int(num_blocks) // 2), np.int32) for _ in range(2))
+    src, dst = (np.zeros(max(1, num_blocks // 2), np.int32) for _ in range(2))
     moves, used = C.c_int32(), C.c_int32()
-    _check(load().hb_plan_compaction(_int32(num_blocks), ptrs, lens.ctypes.data_as(C.POINTER(C.c_int32)), len(ts),
+    _check(load().hb_plan_compaction(num_blocks, ptrs, lens.ctypes.data_as(C.POINTER(C.c_int32)), len(ts),
                                      src.ctypes.data, dst.ctypes.data, C.byref(moves), C.byref(used)))
     return ts, src[:moves.value], dst[:moves.value], used.value
 

@@ -71,3 +71,10 @@ def test_requests_arrive_as_given(H, table):
     cfg = H.make_config(Shape, 64, 4)
     assert H.hb_validate_batch(cfg, 8, [(5, 20, table)], 0x1000, 0x100000) == H.HB_OK
     assert H.hb_validate_batch(cfg, 7, [(5, 20, table)], 0x1000, 0x100000) == H.HB_ERR_RANGE
+
+
+def test_a_pool_of_too_many_blocks(H):
+    """Refused before the list of its moves is allocated."""
+    for num_blocks in (WIDE + 4, 1 << 45, -WIDE):
+        with pytest.raises(ValueError):
+            H.hb_plan_compaction(num_blocks, [[1, 2]])
