@@ -244,6 +244,10 @@ void iteration_work(const Dims& d, const hb_request* reqs, int n, double* flops,
 
 static int round_up(int64_t x, int m) { return (int)((x + m - 1) / m * m); }
 
+// The rules of PlanOptions::fit_round. Their limits, in keys, were measured at head
+// dimension 128; at 64, where a key is half the bytes and half the products, the
+// same ones are used.
+
 // Smallest split length from `finest` on (multiples of 64 keys, at most 1024) at
 // which key ranges of these lengths, each in nkv kv heads, take `slots`
 // workgroups at most, a workgroup taking `waves` splits; 0 where none does.

@@ -155,9 +155,11 @@ struct PlanOptions {
   int min_item = 64;   // least item split the planner chooses by itself
   int unit_block = 0;  // runs of tiles / item groups in the unit order (0: one per CU; < 0: fine interleave)
   Window window;
-  // as hb_attention plans: launches that need one round of workgroups at most are
-  // cut for that round, chunks into items too where that is sooner done, and
-  // where items are few no wave takes more than 256 keys alone
+  // As hb_attention plans (layers do not). Launches that need one round of
+  // workgroups at most are cut for that round: item ranges are split for it, small
+  // launches with chunks take no tiles (their units in the order by die), few tiles
+  // are halved or split. And where items are few, in launches of any size, no wave
+  // takes more than 256 keys alone.
   bool fit_round = false;
 };
 
