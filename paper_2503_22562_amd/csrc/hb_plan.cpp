@@ -443,7 +443,7 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
                                       : fit_item_split(item_lengths, d.nkv, cus);
   const int S_i = opt.split_item > 0 ? round_up(opt.split_item, 64)
                   : S_i_fit > 0      ? S_i_fit
-                                     : std::max(S_i_fill, round_up((int64_t)(item_keys / (16.0 * cus)) + 1, 64));
+                                     : std::max(S_i_fill, round_up((int64_t)std::min(item_keys / (16.0 * cus), 1.0e9) + 1, 64));
   // Longest range that one wave takes alone. With few item groups a lone wave of
   // S_i keys is what the launch ends on, so ranges above 256 keys are cut over a
   // unit's four waves already (beside a 512-token chunk, 64 decodes behind a

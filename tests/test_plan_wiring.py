@@ -136,6 +136,13 @@ def test_random_launches(driver, seed):
     check(plan, shape, reqs)
 
 
+@pytest.mark.parametrize("fit", [False, True], ids=["layer", "handle"])
+def test_the_most_keys_of_a_launch(driver, fit):
+    """Heads and context at the interface's limits: 2^44 keys over 4096 waves are 2^32 each."""
+    shape, reqs = (64, 1 << 14, 1 << 14, 64, 16), [(1, (1 << 30) - 1)]
+    check(run(driver, shape, 256, fit, reqs), shape, reqs)
+
+
 def test_the_check_sees_a_wrong_plan(driver):
     """Mistakes planted in a plan's text: a unit launched twice in another's place, parts that share a slot, a part or
     a column block that is not merged, a key range that misses a step."""

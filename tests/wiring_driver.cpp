@@ -20,17 +20,17 @@ int main() {
   c.kv_block_size = 16;
   c.rope_theta = 5e5f;
   c.rms_eps = 1e-5f;
-  c.max_batch_tokens = 1 << 16;
   c.max_requests = 1 << 16;
   opt.fit_round = fit;
-  Dims d;
-  if (check_config(&c, &d) != HB_OK) return 3;
   std::vector<hb_request> reqs(n);
   int longest = 0;
   for (hb_request& r : reqs) {
     if (scanf("%d %d", &r.chunk_len, &r.context_len) != 2) return 4;
     longest = std::max(longest, r.chunk_len + r.context_len);
+    c.max_batch_tokens += r.chunk_len;
   }
+  Dims d;
+  if (check_config(&c, &d) != HB_OK) return 3;
   const std::vector<int32_t> table((longest + 15) / 16, 0);
   for (hb_request& r : reqs) {
     r.block_table = table.data();
