@@ -287,6 +287,88 @@ void hb_destroy_attention(hb_attention* attention);
 hb_status hb_plan_attention(hb_attention* attention, int32_t n_requests, const hb_request* requests, int32_t window,
                             int32_t sinks);
 
+/* Requests [first, first + count) of a batch whose first prefix_len tokens are
+ * the same cached tokens: the first prefix_len / 16 entries of their block
+ * tables are equal (a common prompt, the samples drawn from it). */
+typedef struct {
+  int32_t first, count, prefix_len;
+} hb_prefix_group;
+
+/* hb_plan_attention for a batch in which groups of requests share a prefix: runs
+ * read a shared prefix's keys and values once for all rows of its group and join
+ * that with each row's own keys. The results are those of hb_plan_attention but
+ * for the order in which a row's keys are added up; the same bits every time. A
+ * request whose own rows fill half a matrix tile (chunk_len * n_q_heads /
+ * n_kv_heads >= 64) reads its prefix by itself, as it would gain nothing.
+ *   groups  host [n_groups], ascending and disjoint; prefix_len a multiple of
+ *           16, at most the context_len of every request of the group
+ * No window. Errors: those of hb_plan_attention; HB_ERR_INVALID (null groups,
+ * n_groups < 0, a group that is empty, reaches outside the batch or does not
+ * follow the one before, a prefix_len that is negative, no multiple of 16 or
+ * above a context_len, tables that differ in the prefix: the plan before
+ * stays); HB_ERR_UNSUPPORTED (more than 2^30 partial results: no plan is held). */
+hb_status hb_plan_shared_attention(hb_attention* attention, int32_t n_requests, const hb_request* requests,
+                                   int32_t n_groups, const hb_prefix_group* groups);
+
+/* Rotary positions. A head's first rotary_dim dimensions are rotated in pairs, pair
+ * j at position p by the angle p * inv_freq[j]:
+ *   (a, b) -> magnitude * (a cos - b sin, b cos + a sin)
+ * The others stay as they are. HB_ROPE_HALF pairs dimension j with j +
+ * rotary_dim / 2, HB_ROPE_INTERLEAVED 2j with 2j + 1. */
+enum { HB_ROPE_HALF = 0, HB_ROPE_INTERLEAVED = 1 };
+
+/* Frequencies scaled for contexts longer than a model was trained on:
+ *   HB_ROPE_UNSCALED  f_j = theta^(-2j / rotary_dim)
+ *   HB_ROPE_LINEAR    f_j / factor
+ *   HB_ROPE_BY_PARTS  with r_j = original_context f_j / (2 pi), the turns of pair j
+ *                     over the original context: f_j where r_j >= high, f_j / factor
+ *                     where r_j <= low, between them f_j (g + (1 - g) / factor)
+ *                     with g = (r_j - low) / (high - low)
+ * (Any others are the caller's own array. Where scores are scaled too, as
+ * 0.1 ln(factor) + 1 for queries and keys each, that is the magnitude.) */
+enum { HB_ROPE_UNSCALED = 0, HB_ROPE_LINEAR = 1, HB_ROPE_BY_PARTS = 2 };
+typedef struct {
+  int32_t kind, original_context;
+  double factor, low, high;
+} hb_rope_scaling;
+
+/* Write the rotary_dim / 2 frequencies (host). scaling: NULL for none. Host only.
+ * Errors: HB_ERR_INVALID (null inv_freq, rotary_dim < 0 or odd, theta not above 1 or
+ * infinite, an unknown kind, a factor that is not positive and finite; by parts,
+ * original_context < 1 or not 0 <= low < high < infinity). */
+hb_status hb_rope_frequencies(int32_t rotary_dim, double theta, const hb_rope_scaling* scaling, double* inv_freq);
+
+/* Rotation of the handle's later hb_run_append calls. Plans made from now on hold
+ * where a batch's new tokens go in the cache; one made before cannot append.
+ *   rotary_dim  a multiple of 16 up to head_dim; 0: nothing is rotated
+ *   inv_freq    host [rotary_dim / 2], copied (NULL if rotary_dim is 0)
+ * Errors: HB_ERR_INVALID (null pointer, a layout that is none, a frequency or
+ * magnitude that is negative or not finite, a frequency above 2^20), HB_ERR_UNSUPPORTED
+ * (another rotary_dim); the rotation before stays. */
+hb_status hb_set_attention_rope(hb_attention* attention, int32_t rotary_dim, int32_t layout, const double* inv_freq,
+                                double magnitude);
+
+/* Rotate the planned batch's new queries and keys and put its new keys and values
+ * into the cache: what hb_run_attention (and every later iteration) then reads.
+ * Row t of q, k and v is the batch's new token t, in plan order, at its position.
+ *   pool           as for hb_run_attention; only the new tokens' slots change
+ *   q, k, v        device bf16 [T] rows of n_q_heads, n_kv_heads and n_kv_heads
+ *                  heads of head_dim values, as they leave the projections (slices
+ *                  of a fused QKV output will do)
+ *   q_out          device bf16 [T] rows of the rotated queries; q itself, with its
+ *                  stride, or memory that no row of q, k and v shares
+ * Strides in elements, multiples of 8; 16-byte aligned pointers. Angles are formed
+ * and reduced in fp64, cosines, sines and products in fp32, rounded once to bf16;
+ * v is copied bit by bit, as are the dimensions that are not rotated. Enqueues on
+ * the handle's stream and returns; allocates nothing. Errors: HB_ERR_INVALID (null
+ * pointer, no plan, a plan made before hb_set_attention_rope or of requests that
+ * write one slot twice, a pool of fewer blocks, a stride below the row, no multiple
+ * of 8 or above 2^40, misaligned pointer, an overlap of q_out with k, v or part of q, of a
+ * pool with any row or with the other), HB_ERR_HIP (among others: the stream is
+ * under graph capture). */
+hb_status hb_run_append(hb_attention* attention, const hb_kv_pool* pool, const void* q, int64_t q_stride, const void* k,
+                        int64_t k_stride, const void* v, int64_t v_stride, void* q_out, int64_t q_out_stride);
+
 /* Run the planned batch. Enqueues on the handle's stream and returns; allocates
  * nothing.
  *   pool        the pool the plan's tables name blocks of: at least the
@@ -490,6 +572,58 @@ typedef struct {
   void* hidden_states;
 } hb_model_batch;
 hb_status hb_run_model(hb_model* model, const hb_model_batch* batch);
+
+/* Sampling: one token of each row of logits, drawn by given random numbers (the
+ * greedy choice is hb_run_model's own). Row r's tokens stand in descending order of
+ * their logits x_i, the lower index first among equals, and with t = temperature[r]
+ * have the weights w_i = exp((x_i - max x) / t). Kept is the shortest of
+ *   - the first top_k[r] tokens (top_k <= 0: all);
+ *   - of those, the fewest first ones whose weights add up to top_p[r] of theirs
+ *     together, the one that reaches it among them (not top_p < 1: all);
+ *   - the tokens with w_i >= min_p[r] (not min_p > 0: all),
+ * but never less than the first token. Drawn is the first kept token at which the
+ * running sum of the weights exceeds u[r] times the kept weight, so u = 0 gives the
+ * most likely one. tokens[r] receives it, probs[r] the probability it was drawn
+ * with, its share of the kept weight.
+ *   temperature  not above 0 (or not a number): the most likely token, probability 1
+ *   u            below 0 or not a number: 0; from 1 on: 1 - 2^-24
+ *   logits       not a number, or -infinity: never drawn; +infinity: as the largest
+ *                fp32 value; a row of none but the former: token 0, probability 0
+ * Weights are formed in fp64 and summed as integer multiples of 2^-45 of the largest
+ * (2^-44 for a vocabulary above 2^17, 2^-42 at 2^20): the order of additions changes
+ * nothing, and two calls give the same tokens. */
+typedef struct hb_sampler hb_sampler; /* opaque, library-owned */
+typedef struct {
+  int32_t n_rows;
+  int32_t logits_dtype;      /* HB_OUT_F32 or HB_OUT_BF16 */
+  const void* logits;        /* device, [n_rows] rows of vocab values, row_stride elements apart */
+  int64_t row_stride;
+  const float* temperature;  /* device [n_rows] each, or NULL: 1 */
+  const int32_t* top_k;      /* NULL: all */
+  const float* top_p;        /* NULL: all */
+  const float* min_p;        /* NULL: all */
+  const float* u;            /* device [n_rows], uniform on [0, 1) */
+  int32_t* tokens;           /* device [n_rows] */
+  float* probs;              /* device [n_rows], or NULL */
+} hb_sample_desc;
+
+/* Create a sampler for up to max_rows rows of vocab logits, on a HIP stream of the
+ * current device (hipStream_t; NULL selects the null stream). Errors: HB_ERR_INVALID
+ * (null pointer, a size below 1), HB_ERR_UNSUPPORTED (a size above 2^20),
+ * HB_ERR_OOM, HB_ERR_HIP. On error *out is set to NULL. */
+hb_status hb_create_sampler(int32_t max_rows, int32_t vocab, void* hip_stream, hb_sampler** out);
+
+/* Free the sampler (after synchronising its stream). NULL is a no-op. */
+void hb_destroy_sampler(hb_sampler* sampler);
+
+/* Draw. Enqueues on the sampler's stream and returns; allocates nothing, and may be
+ * captured into a graph. Nothing is written behind row n_rows - 1. The calls of one
+ * sampler (replays of captured ones among them) must not overlap. Errors:
+ * HB_ERR_INVALID (null logits, u or tokens, n_rows outside [0, max_rows], an unknown
+ * dtype, a row stride below vocab or above 2^40, an array that is not aligned to
+ * its elements, tokens or probs that overlap another array), HB_ERR_HIP. n_rows ==
+ * 0 is a no-op. */
+hb_status hb_sample(hb_sampler* sampler, const hb_sample_desc* desc);
 
 /* Per-kernel timing of hb_run_iteration, for roofline accounting. Every
  * launch of kernel k with bit k of kernel_mask set is bracketed by HIP events

@@ -36,6 +36,12 @@ struct hb_attention {
   Plan plan, next;  // the current plan, and the one being built
   RecordPlan records, next_records;
   bool planned = false;
+  // appends: the rotation, and whether and where the plan's units stand
+  bool rope_set = false, can_append = false;
+  int rotary = 0, rope_layout = HB_ROPE_HALF, n_append = 0, off_append = 0;
+  float magnitude = 1.f;
+  double turns[64] = {};
+  SlotMarks marks;
   int32_t* meta = nullptr;  // the current plan's metadata; in stream order with the runs that read it
   size_t meta_cap = 0;      // int32
   float *part_o = nullptr, *part_ml = nullptr;
@@ -75,22 +81,19 @@ bool regrow(hb_attention* a, void** p, size_t bytes) {
   return true;
 }
 
-hb_status plan_attention(hb_attention* a, int n, const hb_request* requests, int window, int sinks) {
-  hb_status st = check_window_args(window, sinks);
-  if (st != HB_OK) return st;
-  PlanOptions opt = a->opt;
-  opt.window.window = window;
-  opt.window.sinks = window > 0 ? sinks : 0;
-  int64_t T = 0;
-  st = check_requests(a->d, a->num_blocks, requests, n, opt.window, &T);
-  if (st != HB_OK) return st;
+// The plan of a checked batch of T tokens.
+hb_status plan_checked(hb_attention* a, int n, const hb_request* requests, int64_t T, const PlanOptions& opt) {
+  const bool can_append = a->rope_set && check_slots(a->num_blocks, requests, n, T, &a->marks) == HB_OK;
   const DeviceGuard on(a->device);
-  st = refuse_capture(a->stream);
+  const hb_status st = refuse_capture(a->stream);
   if (st != HB_OK) return st;
   a->planned = false;  // until the new one stands
   const hb_batch_desc desc{n, requests, nullptr, nullptr, HB_OUT_BF16};
   build_plan(a->d, &desc, a->cu_count, &a->next, opt);
+  if (a->next.too_many_slots) return fail(HB_ERR_UNSUPPORTED, "more than 2^30 partial results of shared prefixes");
   build_records(a->next, &a->next_records);
+  if (can_append) a->n_append = build_append(requests, n, &a->next_records.meta, &a->off_append);
+  a->can_append = can_append;
   const size_t words = a->next_records.meta.size();
   PlanStage& s = a->stage[a->stage_next];
   if (s.pending) {
@@ -136,6 +139,54 @@ hb_status plan_attention(hb_attention* a, int n, const hb_request* requests, int
   return HB_OK;
 }
 
+hb_status plan_attention(hb_attention* a, int n, const hb_request* requests, int window, int sinks) {
+  hb_status st = check_window_args(window, sinks);
+  if (st != HB_OK) return st;
+  PlanOptions opt = a->opt;
+  opt.window.window = window;
+  opt.window.sinks = window > 0 ? sinks : 0;
+  int64_t T = 0;
+  st = check_requests(a->d, a->num_blocks, requests, n, opt.window, &T);
+  return st != HB_OK ? st : plan_checked(a, n, requests, T, opt);
+}
+
+hb_status plan_shared(hb_attention* a, int n, const hb_request* requests, int n_groups, const hb_prefix_group* groups) {
+  int64_t T = 0;
+  const hb_status st = check_shared(a->d, a->num_blocks, requests, n, groups, n_groups, &T);
+  if (st != HB_OK) return st;
+  PlanOptions opt = a->opt;
+  opt.groups = groups;
+  opt.n_groups = n_groups;
+  return plan_checked(a, n, requests, T, opt);
+}
+
+hb_status run_append(hb_attention* a, const hb_kv_pool* pool, const Rows& q, const Rows& k, const Rows& v,
+                     const Rows& out) {
+  hb_status st = check_append(a->d, a->num_blocks, a->plan.T, pool, q, k, v, out);
+  if (st != HB_OK) return st;
+  const DeviceGuard on(a->device);
+  st = refuse_capture(a->stream);
+  if (st != HB_OK) return st;
+  AppendArgs g{};
+  g.units = a->meta + a->off_append;
+  g.n_units = a->n_append;
+  g.q = (const uint16_t*)q.at; g.q_stride = q.stride;
+  g.k = (const uint16_t*)k.at; g.k_stride = k.stride;
+  g.v = (const uint16_t*)v.at; g.v_stride = v.stride;
+  g.q_out = (uint16_t*)out.at; g.q_out_stride = out.stride;
+  g.k_pool = (uint16_t*)pool->k_pool;
+  g.v_pool = (uint16_t*)pool->v_pool;
+  g.nq = a->d.nq; g.nkv = a->d.nkv; g.hd = a->d.hd;
+  g.rotary = a->rotary;
+  g.interleaved = a->rope_layout == HB_ROPE_INTERLEAVED;
+  g.magnitude = a->magnitude;
+  std::copy(a->turns, a->turns + 64, g.turns);
+  launch_append(a->stream, g);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return fail(HB_ERR_HIP, "append launch: %s", hipGetErrorString(e));
+  return HB_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -174,6 +225,38 @@ hb_status hb_plan_attention(hb_attention* a, int32_t n_requests, const hb_reques
                             int32_t sinks) {
   if (!a) return fail(HB_ERR_INVALID, "null attention handle");
   return guarded([&] { return plan_attention(a, n_requests, requests, window, sinks); });
+}
+
+hb_status hb_plan_shared_attention(hb_attention* a, int32_t n_requests, const hb_request* requests, int32_t n_groups,
+                                   const hb_prefix_group* groups) {
+  if (!a) return fail(HB_ERR_INVALID, "null attention handle");
+  return guarded([&] { return plan_shared(a, n_requests, requests, n_groups, groups); });
+}
+
+hb_status hb_set_attention_rope(hb_attention* a, int32_t rotary_dim, int32_t layout, const double* inv_freq,
+                                double magnitude) {
+  if (!a) return fail(HB_ERR_INVALID, "null attention handle");
+  const hb_status st = check_rope(a->d.hd, rotary_dim, layout, inv_freq, magnitude);
+  if (st != HB_OK) return st;
+  for (int j = 0; j < rotary_dim / 2; ++j) a->turns[j] = inv_freq[j] / 6.283185307179586;
+  a->rotary = rotary_dim;
+  a->rope_layout = layout;
+  a->magnitude = (float)magnitude;
+  a->rope_set = true;
+  return HB_OK;
+}
+
+hb_status hb_run_append(hb_attention* a, const hb_kv_pool* pool, const void* q, int64_t q_stride, const void* k,
+                        int64_t k_stride, const void* v, int64_t v_stride, void* q_out, int64_t q_out_stride) {
+  if (!a) return fail(HB_ERR_INVALID, "null attention handle");
+  if (!a->planned) return fail(HB_ERR_INVALID, "hb_run_append before a successful plan");
+  if (!a->can_append)
+    return fail(HB_ERR_INVALID, "hb_run_append: the plan was made before hb_set_attention_rope, or two of its requests "
+                                "write one slot");
+  if (a->plan.T == 0) return HB_OK;
+  const int64_t row = (int64_t)a->d.nq * a->d.hd, kv_row = (int64_t)a->d.nkv * a->d.hd;
+  return run_append(a, pool, {(uintptr_t)q, q_stride, row}, {(uintptr_t)k, k_stride, kv_row},
+                    {(uintptr_t)v, v_stride, kv_row}, {(uintptr_t)q_out, q_out_stride, row});
 }
 
 hb_status hb_run_attention(hb_attention* a, const hb_kv_pool* pool, const void* q, int64_t q_stride, void* out,

@@ -115,6 +115,21 @@ void launch_append_kv(hipStream_t s, const uint16_t* k, const uint16_t* v, int n
 void launch_append_kv_inline(hipStream_t s, const uint16_t* k, const uint16_t* v, int n_tokens, int ctx,
                              const int32_t* bt, int nkv, int hd, uint16_t* k_pool, uint16_t* v_pool);
 
+// Rotate the new queries and keys of a planned batch (AppendUnit) and put its new
+// keys and values into the pool.
+struct AppendArgs {
+  const int32_t* units;  // AppendUnit
+  int n_units, parts;    // (parts: workgroups of a unit, set by the launch)
+  const uint16_t *q, *k, *v;
+  int64_t q_stride, k_stride, v_stride, q_out_stride;  // elements from row to row
+  uint16_t *q_out, *k_pool, *v_pool;
+  int nq, nkv, hd;
+  int rotary, interleaved;  // dimensions of a head that are rotated, a multiple of 16
+  float magnitude;
+  double turns[64];  // per pair and position: frequency / 2 pi
+};
+void launch_append(hipStream_t s, AppendArgs a);
+
 // Copy whole blocks, all kv heads of K and V, inside each of n_pools pools: block
 // dst[i] becomes block src[i]. No block of dst occurs again in src or dst. The ids
 // are in device memory or (inline) in host memory and travel with the launches.
@@ -192,5 +207,18 @@ void launch_gather_rows(hipStream_t s, const uint16_t* src, int64_t n_src, const
                         uint16_t* out);
 // out[r] = index of the largest of x[r][0..V) (lowest index on ties).
 void launch_argmax(hipStream_t s, const float* x, int n_rows, int V, int32_t* out);
+// Tokens drawn from rows of logits (hb_sample_desc).
+struct SampleArgs {
+  const void* logits;
+  int64_t stride;  // elements from row to row
+  int bf16, rows, vocab;
+  int shift;  // weights are summed as multiples of 2^-shift (set by the launch)
+  const float* temperature;
+  const int32_t* top_k;
+  const float *top_p, *min_p, *u;
+  int32_t* tokens;
+  float* probs;
+};
+void launch_sample(hipStream_t s, SampleArgs a);
 
 }  // namespace hb

@@ -102,7 +102,7 @@ DeadBlocks dead_blocks(const Window& w, int pos) {
 }
 
 hb_status check_requests(const Dims& d, int num_blocks, const hb_request* requests, int n, const Window& w,
-                         int64_t* n_tokens) {
+                         int64_t* n_tokens, const std::vector<int>* skip) {
   if (n < 0) return fail(HB_ERR_INVALID, "n_requests < 0");
   if (n > d.max_R) return fail(HB_ERR_INVALID, "n_requests %d exceeds max_requests %d", n, d.max_R);
   if (n > 0 && !requests) return fail(HB_ERR_INVALID, "null request array");
@@ -118,7 +118,7 @@ hb_status check_requests(const Dims& d, int num_blocks, const hb_request* reques
     if (q.n_blocks < blocks_for(kv))
       return fail(HB_ERR_INVALID, "request %d: block table has %d blocks, needs %lld", r, q.n_blocks,
                   (long long)blocks_for(kv));
-    const DeadBlocks dead = dead_blocks(w, q.context_len);
+    const DeadBlocks dead = skip ? DeadBlocks{0, (*skip)[r]} : dead_blocks(w, q.context_len);
     for (int64_t i = 0; i < blocks_for(kv); ++i) {
       if (i == dead.first) i += dead.count;
       int32_t b = q.block_table[i];
@@ -154,14 +154,18 @@ hb_status check_batch(const Dims& d, int num_blocks, const hb_batch_desc* desc, 
     uintptr_t b0 = (uintptr_t)desc->x_out, b1 = b0 + (uintptr_t)T * d.H * (desc->out_dtype == HB_OUT_F32 ? 4 : 2);
     if (a0 < b1 && b0 < a1) return fail(HB_ERR_INVALID, "x_out overlaps x_in");
   }
-  // no two new tokens may be written to the same physical slot
+  return check_slots(num_blocks, desc->requests, R, T, marks);
+}
+
+hb_status check_slots(int num_blocks, const hb_request* requests, int n, int64_t n_tokens, SlotMarks* marks) {
+  hb_status st = HB_OK;
   SlotMarks local;
   SlotMarks* m = marks ? marks : &local;
   if ((int)m->mask.size() < num_blocks) m->mask.assign(num_blocks, 0);
   m->touched.clear();
-  m->touched.reserve(T);  // nothing can fail while marks stand
-  for (int r = 0; r < R && st == HB_OK; ++r) {
-    const hb_request& q = desc->requests[r];
+  m->touched.reserve(n_tokens);  // nothing can fail while marks stand
+  for (int r = 0; r < n && st == HB_OK; ++r) {
+    const hb_request& q = requests[r];
     for (int64_t p = q.context_len; p < (int64_t)q.context_len + q.chunk_len; ++p) {
       int32_t b = q.block_table[p / 16];
       uint16_t bit = (uint16_t)(1u << (p % 16));
@@ -177,6 +181,128 @@ hb_status check_batch(const Dims& d, int num_blocks, const hb_batch_desc* desc, 
   for (int32_t b : m->touched) m->mask[b] = 0;
   m->touched.clear();
   return st;
+}
+
+hb_status check_shared(const Dims& d, int num_blocks, const hb_request* requests, int n, const hb_prefix_group* groups,
+                       int n_groups, int64_t* n_tokens) {
+  if (n < 0) return fail(HB_ERR_INVALID, "n_requests < 0");
+  if (n > d.max_R) return fail(HB_ERR_INVALID, "n_requests %d exceeds max_requests %d", n, d.max_R);
+  if (n_groups < 0 || (n_groups > 0 && !groups)) return fail(HB_ERR_INVALID, "n_groups < 0 or null groups");
+  std::vector<int> skip(n, 0);
+  int next = 0;
+  for (int i = 0; i < n_groups; ++i) {
+    const hb_prefix_group& g = groups[i];
+    if (g.count < 1 || g.first < next || g.first > n - g.count)
+      return fail(HB_ERR_INVALID, "group %d: requests [%d, %d + %d) are empty, outside the batch or in or before group %d's",
+                  i, g.first, g.first, g.count, i - 1);
+    if (g.prefix_len < 0 || g.prefix_len % 16)
+      return fail(HB_ERR_INVALID, "group %d: prefix_len %d is no multiple of 16", i, g.prefix_len);
+    next = g.first + g.count;
+    if (!requests) break;  // (refused below)
+    for (int r = g.first; r < next; ++r) {
+      if (requests[r].context_len < g.prefix_len)
+        return fail(HB_ERR_INVALID, "request %d: context_len %d below its group's prefix_len %d", r,
+                    requests[r].context_len, g.prefix_len);
+      if (r > g.first) skip[r] = g.prefix_len / 16;
+    }
+  }
+  const hb_status st = check_requests(d, num_blocks, requests, n, Window(), n_tokens, &skip);
+  if (st != HB_OK) return st;
+  for (int i = 0; i < n_groups; ++i)
+    for (int r = groups[i].first + 1; r < groups[i].first + groups[i].count; ++r)
+      if (std::memcmp(requests[r].block_table, requests[groups[i].first].block_table,
+                      sizeof(int32_t) * (groups[i].prefix_len / 16)) != 0)
+        return fail(HB_ERR_INVALID, "request %d: its first %d blocks are not those of request %d, of its group", r,
+                    groups[i].prefix_len / 16, groups[i].first);
+  return HB_OK;
+}
+
+static hb_status check_rows(const char* name, const Rows& r) {
+  if (r.stride < r.width || r.stride % 8 || r.stride > (int64_t)1 << 40)
+    return fail(HB_ERR_INVALID, "%s: row stride %lld: a multiple of 8 from %lld to 2^40", name, (long long)r.stride,
+                (long long)r.width);
+  if (r.at % 16) return fail(HB_ERR_INVALID, "%s must be 16-byte aligned", name);
+  return HB_OK;
+}
+
+// Whether some row of the one shares memory with some row of the other. (Rows of
+// different strides that reach into each other's range are taken to.)
+static bool rows_overlap(const Rows& x, const Rows& y, int T) {
+  if (x.at >= y.end(T) || y.at >= x.end(T)) return false;
+  if (x.stride != y.stride || T == 1) return true;
+  const uintptr_t s = (uintptr_t)x.stride * 2, d = y.at >= x.at ? (y.at - x.at) % s : s - 1 - (x.at - y.at - 1) % s;
+  return d < (uintptr_t)x.width * 2 || d + (uintptr_t)y.width * 2 > s;
+}
+
+hb_status check_append(const Dims& d, int num_blocks, int T, const hb_kv_pool* pool, const Rows& q, const Rows& k,
+                       const Rows& v, const Rows& out) {
+  if (!pool || !pool->k_pool || !pool->v_pool || !q.at || !k.at || !v.at || !out.at)
+    return fail(HB_ERR_INVALID, "null pool, q, k, v or q_out");
+  if (pool->num_blocks < num_blocks)
+    return fail(HB_ERR_INVALID, "pool of %d blocks, the plan's tables are over %d", pool->num_blocks, num_blocks);
+  const struct {
+    const char* name;
+    const Rows& rows;
+  } all[] = {{"q", q}, {"k", k}, {"v", v}, {"q_out", out}};
+  for (const auto& r : all) {
+    const hb_status st = check_rows(r.name, r.rows);
+    if (st != HB_OK) return st;
+  }
+  const uintptr_t kp = (uintptr_t)pool->k_pool, vp = (uintptr_t)pool->v_pool;
+  const uintptr_t bytes = (uintptr_t)pool->num_blocks * d.nkv * 16 * d.hd * 2;
+  if (kp % 16 || vp % 16) return fail(HB_ERR_INVALID, "pools must be 16-byte aligned");
+  if (kp < vp + bytes && vp < kp + bytes) return fail(HB_ERR_INVALID, "the pools overlap");
+  for (const auto& r : all)
+    for (const uintptr_t p : {kp, vp})
+      if (p < r.rows.end(T) && r.rows.at < p + bytes) return fail(HB_ERR_INVALID, "%s overlaps a pool", r.name);
+  const bool in_place = out.at == q.at && (out.stride == q.stride || T == 1);
+  if ((!in_place && rows_overlap(out, q, T)) || rows_overlap(out, k, T) || rows_overlap(out, v, T))
+    return fail(HB_ERR_INVALID, "q_out overlaps k, v or part of q");
+  return HB_OK;
+}
+
+hb_status check_rope(int head_dim, int rotary_dim, int layout, const double* inv_freq, double magnitude) {
+  if (rotary_dim < 0 || rotary_dim > head_dim || rotary_dim % 16)
+    return fail(HB_ERR_UNSUPPORTED, "rotary_dim %d: a multiple of 16 up to %d", rotary_dim, head_dim);
+  if (layout != HB_ROPE_HALF && layout != HB_ROPE_INTERLEAVED) return fail(HB_ERR_INVALID, "unknown rotary layout %d", layout);
+  if (rotary_dim > 0 && !inv_freq) return fail(HB_ERR_INVALID, "null inv_freq");
+  if (!(magnitude >= 0 && std::isfinite((float)magnitude))) return fail(HB_ERR_INVALID, "magnitude %g", magnitude);
+  for (int j = 0; j < rotary_dim / 2; ++j)
+    if (!(inv_freq[j] >= 0 && inv_freq[j] <= 1 << 20)) return fail(HB_ERR_INVALID, "inv_freq[%d] = %g", j, inv_freq[j]);
+  return HB_OK;
+}
+
+hb_status check_sample(int max_rows, int vocab, const hb_sample_desc* d) {
+  if (!d) return fail(HB_ERR_INVALID, "null sample descriptor");
+  const int n = d->n_rows;
+  if (n < 0 || n > max_rows) return fail(HB_ERR_INVALID, "n_rows %d outside [0, %d]", n, max_rows);
+  if (d->logits_dtype != HB_OUT_F32 && d->logits_dtype != HB_OUT_BF16)
+    return fail(HB_ERR_INVALID, "logits_dtype must be HB_OUT_F32 or HB_OUT_BF16");
+  if (n == 0) return HB_OK;
+  if (!d->logits || !d->u || !d->tokens) return fail(HB_ERR_INVALID, "null logits, u or tokens");
+  if (d->row_stride < vocab || d->row_stride > (int64_t)1 << 40)
+    return fail(HB_ERR_INVALID, "row stride %lld: from %d to 2^40", (long long)d->row_stride, vocab);
+  const uintptr_t size = d->logits_dtype == HB_OUT_F32 ? 4 : 2, x = (uintptr_t)d->logits, m = 4 * (uintptr_t)n;
+  struct Range {
+    uintptr_t at, bytes;
+  };
+  const Range in[] = {{x, ((uintptr_t)(n - 1) * d->row_stride + vocab) * size}, {(uintptr_t)d->u, m},
+                      {(uintptr_t)d->temperature, m}, {(uintptr_t)d->top_k, m},
+                      {(uintptr_t)d->top_p, m}, {(uintptr_t)d->min_p, m}};
+  const Range out[] = {{(uintptr_t)d->tokens, m}, {(uintptr_t)d->probs, m}};
+  auto overlap = [](const Range& a, const Range& b) {
+    return a.at && b.at && a.at < b.at + b.bytes && b.at < a.at + a.bytes;
+  };
+  if (x % size) return fail(HB_ERR_INVALID, "misaligned logits");
+  for (int i = 1; i < 6; ++i)
+    if (in[i].at % 4) return fail(HB_ERR_INVALID, "misaligned u or settings");
+  for (const Range& o : out) {
+    if (o.at % 4) return fail(HB_ERR_INVALID, "misaligned tokens or probs");
+    for (const Range& i : in)
+      if (overlap(o, i)) return fail(HB_ERR_INVALID, "tokens or probs overlap an input");
+  }
+  if (overlap(out[0], out[1])) return fail(HB_ERR_INVALID, "tokens and probs overlap");
+  return HB_OK;
 }
 
 static hb_status plan_compaction(int num_blocks, int32_t* const* tables, const int32_t* n_blocks, int n_tables,
@@ -334,6 +460,46 @@ static std::vector<int32_t> by_die(const std::vector<int32_t>& units, F&& item_o
   return order;
 }
 
+namespace {
+// Rows that read one key range of one block table: a request's own, or those of
+// consecutive requests over the prefix that they share.
+struct Span {
+  int r, tok0, rows;
+  int x;    // position of the first row
+  int lo;   // first key
+  int end;  // end of the keys, every one of which each row sees; or -1: a row's keys end with itself
+  int run;  // the shared run whose parts these rows leave, or -1
+};
+// Consecutive requests whose prefix is read for all of them at once. Column
+// slots: part s of a column (row, head) of kv head g is slot
+// base + (g parts + s) columns + column, the prefix's parts first.
+struct Run {
+  int first, count, len, rows;
+  int prefix_parts = 0, parts = 0;
+  int64_t base = 0;
+};
+
+// The requests of a group that are joined, as runs of consecutive ones.
+std::vector<Run> shared_runs(const Dims& d, const hb_request* rq, const PlanOptions& opt) {
+  std::vector<Run> runs;
+  for (int i = 0; i < opt.n_groups; ++i) {
+    const hb_prefix_group& g = opt.groups[i];
+    int rows = 0, first = g.first;
+    auto close = [&](int end) {
+      if (end - first > 1 && g.prefix_len > 0) runs.push_back({first, end - first, g.prefix_len, rows});
+      first = end + 1;
+      rows = 0;
+    };
+    for (int r = g.first; r < g.first + g.count; ++r) {
+      if ((int64_t)rq[r].chunk_len * d.G >= kTileCols / 2) close(r);  // fills its own tiles: nothing to share
+      else rows += rq[r].chunk_len;
+    }
+    close(g.first + g.count);
+  }
+  return runs;
+}
+}  // namespace
+
 void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p, const PlanOptions& opt) {
   const int R = desc->n_requests;
   const hb_request* rq = desc->requests;
@@ -341,11 +507,18 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   std::vector<int> tok_start(R + 1, 0);
   const Window& win = opt.window;
   p->windowed = false;
+  // table entries that are not uploaded: hidden by the window, or uploaded with the
+  // first request of a shared run
+  std::vector<DeadBlocks> absent(R);
+  std::vector<Run> runs = shared_runs(d, rq, opt);
+  for (int r = 0; r < R; ++r) absent[r] = dead_blocks(win, rq[r].context_len);
+  for (const Run& u : runs)
+    for (int r = u.first + 1; r < u.first + u.count; ++r) absent[r] = {0, u.len / 16};
   for (int r = 0; r < R; ++r) {
     tok_start[r] = T;
     T += rq[r].chunk_len;
     const int64_t kv = (int64_t)rq[r].context_len + rq[r].chunk_len;
-    nbt += (int)blocks_for(kv) - dead_blocks(win, rq[r].context_len).count + kBtPad;
+    nbt += (int)blocks_for(kv) - absent[r].count + kBtPad;
     p->windowed |= win.window > 0 && kv - win.window > win.sinks;  // the last row's window hides a key
   }
   p->window = win;
@@ -355,10 +528,19 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   p->R = R;
 
   const int cus = std::max(1, cu_count);
-  // keys of the w rows from i0 on of request r
-  auto range_len = [&](int r, int i0, int w) {
-    const int x = rq[r].context_len;
-    return x + std::min(rq[r].chunk_len, i0 + w) - 16 * dead_blocks(win, x + i0).count;
+  std::vector<Span> spans;
+  spans.reserve(R + runs.size());
+  for (int r = 0, u = 0; r < R; ++r) {
+    if (u < (int)runs.size() && r == runs[u].first + runs[u].count) ++u;
+    const bool joined = u < (int)runs.size() && r >= runs[u].first;
+    if (joined && r == runs[u].first)
+      spans.push_back({r, tok_start[r], runs[u].rows, runs[u].len, 0, runs[u].len, u});
+    spans.push_back({r, tok_start[r], rq[r].chunk_len, rq[r].context_len, joined ? runs[u].len : 0, -1, joined ? u : -1});
+  }
+  // keys of the w rows from i0 on of a span
+  auto range_len = [&](const Span& s, int i0, int w) {
+    if (s.end >= 0) return s.end - s.lo;
+    return s.x + std::min(s.rows, i0 + w) - s.lo - 16 * dead_blocks(win, s.x + i0).count;
   };
   // A small launch is latency: a wave item starts sooner than a tile (its K and V
   // go straight to registers, no ring and barrier) and its four waves share the
@@ -372,7 +554,7 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   // up to 256 keys a wave (256 behind 200 17.8 -> 12.0, a fresh 256 13.3 -> 10.4; at
   // 320 128 behind 1000 beside 8 decodes of 1000 21.5 -> 23.8; with ranges split 128
   // behind 2000 22.3 -> 25.1; a second round 512 behind 300 23.4 -> 32.8).
-  auto fills_tile = [&](int r) { return (int64_t)rq[r].chunk_len * d.G >= kTileCols / 2; };
+  auto fills_tile = [&](const Span& s) { return (int64_t)s.rows * d.G >= kTileCols / 2; };
   bool items_only = false;
   int S_items = 0;
   p->paired = false;
@@ -380,14 +562,14 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   if (fit_chunks) {
     int64_t n = 0;
     bool chunks = false;
-    for (int r = 0; r < R; ++r) {
-      n += (rq[r].chunk_len + d.P - 1) / d.P;
-      chunks |= fills_tile(r);
+    for (const Span& s : spans) {
+      n += (s.rows + d.P - 1) / d.P;
+      chunks |= fills_tile(s);
     }
     if (chunks && n * d.nkv <= 2 * cus) {
       std::vector<int> all;
-      for (int r = 0; r < R; ++r)
-        for (int i0 = 0; i0 < rq[r].chunk_len; i0 += d.P) all.push_back(range_len(r, i0, d.P));
+      for (const Span& s : spans)
+        for (int i0 = 0; i0 < s.rows; i0 += d.P) all.push_back(range_len(s, i0, d.P));
       const int longest = *std::max_element(all.begin(), all.end());
       p->paired = n * d.nkv > cus;
       S_items = p->paired ? round_up(((int64_t)longest + kItemsPerUnit - 1) / kItemsPerUnit, 64)
@@ -398,15 +580,15 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   }
   // Otherwise a chunk that fills at least half a workgroup tile goes to the
   // workgroup path; decodes and short chunks become 16-column wave items.
-  auto is_tile = [&](int r) { return !items_only && fills_tile(r); };
+  auto is_tile = [&](const Span& s) { return !items_only && fills_tile(s); };
   double tile_keys = 0, item_keys = 0;
   std::vector<int> item_lengths, tile_lengths;  // of one kv head
-  for (int r = 0; r < R; ++r) {
-    const int w = is_tile(r) ? d.BQ : d.P;
-    for (int i0 = 0; i0 < rq[r].chunk_len; i0 += w) {
-      const int len = range_len(r, i0, w);
-      (is_tile(r) ? tile_keys : item_keys) += (double)d.nkv * len;
-      if (opt.fit_round) (is_tile(r) ? tile_lengths : item_lengths).push_back(len);
+  for (const Span& s : spans) {
+    const int w = is_tile(s) ? d.BQ : d.P;
+    for (int i0 = 0; i0 < s.rows; i0 += w) {
+      const int len = range_len(s, i0, w);
+      (is_tile(s) ? tile_keys : item_keys) += (double)d.nkv * len;
+      if (opt.fit_round) (is_tile(s) ? tile_lengths : item_lengths).push_back(len);
     }
   }
   // split lengths (multiples of 64 keys): about one round of tile workgroups
@@ -494,53 +676,83 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   std::vector<AttnItem> merged_items;
   std::vector<Unit> merged_units;
   struct SplitTile {
-    int first, n, kv_len;  // its pieces are tiles[first .. first + n)
+    int first, n, begin, end;  // its pieces are tiles[first .. first + n), over these keys
   };
   std::vector<SplitTile> split_tiles;
   std::vector<MergeGroup> groups;
   int slots = 0;
-  for (int r = 0; r < R; ++r) {
-    const int c = rq[r].chunk_len, x = rq[r].context_len;
-    const bool tile = is_tile(r);
+  // units that a range of `len` keys takes one after the other (for a wave alone: one)
+  auto parts_of = [&](bool tile, int len) {
+    const int nspl = (len + (tile ? S_t : S_i) - 1) / (tile ? S_t : S_i);
+    return tile ? nspl : len <= S_1 ? 1 : (nspl + kItemsPerUnit - 1) / kItemsPerUnit;
+  };
+  // slots of the shared runs, every unit of which leaves parts
+  int64_t run_slots = 0;
+  for (const Span& s : spans) {
+    if (s.run < 0) continue;
+    Run& u = runs[s.run];
+    if (s.end >= 0) u.parts = u.prefix_parts = parts_of(is_tile(s), s.end - s.lo);
+    else u.parts = std::max(u.parts, u.prefix_parts + parts_of(false, range_len(s, s.rows - 1, 1)));
+  }
+  int64_t run_rows = 0;
+  for (Run& u : runs) {
+    u.base = run_slots;
+    run_slots += (int64_t)u.parts * u.rows * d.G * d.nkv;
+    run_rows += (int64_t)u.rows * d.nkv;
+  }
+  p->too_many_slots = run_slots > 1 << 30 || run_rows > 1 << 26;  // (merge units have 27 bits for a group)
+  if (p->too_many_slots) {
+    p->n_slots = 0;
+    return;
+  }
+  slots = (int)run_slots;
+  for (const Span& sp : spans) {
+    const int r = sp.r, c = sp.rows, x = sp.x;
+    const bool tile = is_tile(sp);
     const int w = !tile ? d.P : p->half_tiles ? d.BQ / 2 : d.BQ, S = tile ? S_t : S_i;
     for (int g = 0; g < d.nkv; ++g) {
       for (int i0 = 0; i0 < c; i0 += w) {
-        const int npos = std::min(w, c - i0);
+        const int npos = std::min(w, c - i0), tok0 = sp.tok0 + i0;
         const int gap = 16 * dead_blocks(win, x + i0).count;
-        const int pos0 = x + i0 - gap, kv_len = pos0 + npos;
-        const int nspl = (kv_len + S - 1) / S;
-        if (tile) {
-          int part0 = -1;
-          if (nspl > 1) {
-            part0 = slots;
-            groups.push_back({slots, nspl, kTileCols, tok_start[r] + i0, npos, g, 0, 0});
-            slots += nspl * kTileCols;
+        const int pos0 = sp.end >= 0 ? x : x + i0 - gap, kv_end = sp.end >= 0 ? sp.end : pos0 + npos;
+        const int kv_len = kv_end - sp.lo;
+        const int nspl = (kv_len + S - 1) / S, k = parts_of(tile, kv_len);
+        // where the unit's parts go: the first one's slots, and those between two of them
+        int part0 = -1, stride = 0;
+        if (sp.run >= 0) {
+          const Run& u = runs[sp.run];
+          const int row0 = tok0 - tok_start[u.first];
+          stride = u.rows * d.G;
+          part0 = (int)(u.base + (int64_t)g * u.parts * stride) + row0 * d.G;
+          if (sp.end < 0) {
+            groups.push_back({part0, u.prefix_parts + k, stride, tok0, npos, g, 0, 0});
+            part0 += u.prefix_parts * stride;
           }
-          if (nspl > 1) split_tiles.push_back({(int)tiles.size(), nspl, kv_len});
+        } else if (k > 1) {
+          part0 = slots;
+          stride = tile ? kTileCols : 16;
+          groups.push_back({slots, k, stride, tok0, npos, g, 0, 0});
+          slots += k * stride;
+        }
+        if (tile) {
+          if (nspl > 1) split_tiles.push_back({(int)tiles.size(), nspl, sp.lo, kv_end});
           for (int s = 0; s < nspl; ++s)
-            tiles.push_back({r, g, tok_start[r] + i0, pos0, npos, s * S, std::min(kv_len, (s + 1) * S),
-                             nspl > 1 ? part0 + s * kTileCols : -1});
+            tiles.push_back({r, g, tok0, pos0, npos, sp.lo + s * S, std::min(kv_end, sp.lo + (s + 1) * S),
+                             part0 < 0 ? -1 : part0 + s * stride});
           continue;
         }
         if (kv_len <= S_1) {
-          singles.push_back({r, g, tok_start[r] + i0, pos0, npos, 0, kv_len, -1});
+          singles.push_back({r, g, tok0, pos0, npos, sp.lo, kv_end, part0});
           continue;
         }
-        const int k = (nspl + kItemsPerUnit - 1) / kItemsPerUnit;
         const int wlen = round_up((kv_len + k - 1) / k, 64);
-        int part0 = -1;
-        if (k > 1) {
-          part0 = slots;
-          groups.push_back({slots, k, 16, tok_start[r] + i0, npos, g, 0, 0});
-          slots += 16 * k;
-        }
         for (int j = 0; j < k; ++j) {
-          const int b = j * wlen, e = std::min(kv_len, b + wlen);
+          const int b = sp.lo + j * wlen, e = std::min(kv_end, b + wlen);
           const int plen = round_up((e - b + kItemsPerUnit - 1) / kItemsPerUnit, 64);
           merged_units.push_back({plen, (int)merged_items.size(), true});
           for (int q = 0; q < kItemsPerUnit; ++q) {
             const int pb = std::min(e, b + q * plen), pe = std::min(e, pb + plen);
-            merged_items.push_back({r, g, tok_start[r] + i0, pos0, npos, pb, pe, k > 1 ? part0 + 16 * j : -1});
+            merged_items.push_back({r, g, tok0, pos0, npos, pb, pe, part0 < 0 ? -1 : part0 + j * stride});
           }
         }
       }
@@ -556,10 +768,10 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   const int64_t item_unit_count = (int64_t)merged_units.size() + ((int64_t)singles.size() + kItemsPerUnit - 1) / kItemsPerUnit;
   if ((int64_t)tiles.size() + item_unit_count <= 2 * (int64_t)std::max(1, cu_count)) {
     for (const SplitTile& st : split_tiles) {
-      const int piece = round_up((st.kv_len + st.n - 1) / st.n, 64);
+      const int piece = round_up((st.end - st.begin + st.n - 1) / st.n, 64);
       for (int s = 0; s < st.n; ++s) {
-        tiles[st.first + s].kv_begin = s * piece;
-        tiles[st.first + s].kv_end = std::min(st.kv_len, (s + 1) * piece);
+        tiles[st.first + s].kv_begin = st.begin + s * piece;
+        tiles[st.first + s].kv_end = std::min(st.end, st.begin + (s + 1) * piece);
       }
     }
   }
@@ -652,8 +864,8 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
       m[p->off_tok_pos + tok_start[r] + i] = rq[r].context_len + i;
       m[p->off_tok_req + tok_start[r] + i] = r;
     }
-    // dead blocks are left out: block i behind them stands at req_bt + i all the same
-    const DeadBlocks dead = dead_blocks(win, rq[r].context_len);
+    // absent blocks are left out: block i behind them stands at req_bt + i all the same
+    const DeadBlocks dead = absent[r];
     const int nb = (int)blocks_for((int64_t)rq[r].context_len + rq[r].chunk_len);
     m[p->off_req_bt + r] = bt_off - dead.count;
     int32_t* bt = m + p->off_bt + bt_off;
@@ -681,6 +893,27 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   if (!groups.empty()) std::memcpy(m + p->off_groups, groups.data(), sizeof(MergeGroup) * groups.size());
   if (!merge.empty()) std::memcpy(m + p->off_merge, merge.data(), sizeof(int32_t) * merge.size());
   iteration_work(d, rq, R, &p->flops, &p->bytes, win);
+  for (const Run& u : runs) p->bytes -= (u.count - 1.0) * u.len * 4 * d.nkv * d.hd;
+}
+
+int build_append(const hb_request* requests, int n, std::vector<int32_t>* out, int* off) {
+  *off = align16((int)out->size());
+  int units = 0;
+  for (int r = 0; r < n; ++r)
+    units += (requests[r].context_len + requests[r].chunk_len - 1) / 16 - requests[r].context_len / 16 + 1;
+  out->resize((size_t)*off + align16(4 * units), 0);
+  AppendUnit* u = reinterpret_cast<AppendUnit*>(out->data() + *off);
+  int tok = 0;
+  for (int r = 0; r < n; ++r) {
+    const hb_request& q = requests[r];
+    for (int p = q.context_len, end = p + q.chunk_len; p < end;) {
+      const int m = std::min(end, (p & ~15) + 16) - p;
+      *u++ = {tok, p, m, q.block_table[p / 16]};
+      tok += m;
+      p += m;
+    }
+  }
+  return units;
 }
 
 void build_records(const Plan& p, RecordPlan* out) {
@@ -751,5 +984,27 @@ extern "C" hb_status hb_window_dead_blocks(int32_t context_len, int32_t window, 
   const DeadBlocks b = dead_blocks({window, sinks}, context_len);
   *first = b.first;
   *count = b.count;
+  return HB_OK;
+}
+
+extern "C" hb_status hb_rope_frequencies(int32_t rotary_dim, double theta, const hb_rope_scaling* scaling,
+                                         double* inv_freq) {
+  if (!inv_freq) return fail(HB_ERR_INVALID, "null inv_freq");
+  if (rotary_dim < 0 || rotary_dim % 2) return fail(HB_ERR_INVALID, "rotary_dim %d: even, from 0 on", rotary_dim);
+  if (!(theta > 1 && std::isfinite(theta))) return fail(HB_ERR_INVALID, "theta %g: above 1 and finite", theta);
+  const hb_rope_scaling s = scaling ? *scaling : hb_rope_scaling{};
+  if (s.kind != HB_ROPE_UNSCALED && s.kind != HB_ROPE_LINEAR && s.kind != HB_ROPE_BY_PARTS)
+    return fail(HB_ERR_INVALID, "unknown scaling %d", s.kind);
+  if (s.kind != HB_ROPE_UNSCALED && !(s.factor > 0 && std::isfinite(s.factor)))
+    return fail(HB_ERR_INVALID, "scaling factor %g", s.factor);
+  if (s.kind == HB_ROPE_BY_PARTS && !(s.original_context >= 1 && s.low >= 0 && s.low < s.high && std::isfinite(s.high)))
+    return fail(HB_ERR_INVALID, "scaling by parts: original_context %d, low %g, high %g", s.original_context, s.low, s.high);
+  for (int j = 0; j < rotary_dim / 2; ++j) {
+    const double f = std::pow(theta, -2.0 * j / rotary_dim);
+    double g = s.kind == HB_ROPE_UNSCALED ? 1.0 : 0.0;  // share of the frequency that is not scaled
+    if (s.kind == HB_ROPE_BY_PARTS)
+      g = std::min(1.0, std::max(0.0, (s.original_context * f / 6.283185307179586 - s.low) / (s.high - s.low)));
+    inv_freq[j] = g == 1.0 ? f : f * (g + (1.0 - g) / s.factor);
+  }
   return HB_OK;
 }

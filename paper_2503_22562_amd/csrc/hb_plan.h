@@ -42,6 +42,18 @@ hb_status check_config(const hb_layer_config* cfg, Dims* d);
 // HB_ERR_UNSUPPORTED unless rows x cols bf16 values fit the operand window.
 hb_status check_window(const char* what, int64_t rows, int64_t cols);
 
+// Rows of `width` elements, `stride` apart.
+struct Rows {
+  uintptr_t at;
+  int64_t stride, width;
+  uintptr_t end(int T) const { return at + ((uintptr_t)(T - 1) * stride + width) * 2; }
+};
+// The arguments of hb_run_append (T > 0 rows), hb_set_attention_rope and hb_sample.
+hb_status check_append(const Dims& d, int num_blocks, int T, const hb_kv_pool* pool, const Rows& q, const Rows& k,
+                       const Rows& v, const Rows& out);
+hb_status check_rope(int head_dim, int rotary_dim, int layout, const double* inv_freq, double magnitude);
+hb_status check_sample(int max_rows, int vocab, const hb_sample_desc* desc);
+
 // Sliding window with sinks. A row at position p sees key j <= p when
 // j > p - window or j < sinks (window 0: every j <= p).
 struct Window {
@@ -117,6 +129,7 @@ struct Plan {
   int T = 0, R = 0;
   int n_tiles = 0, n_items = 0, n_units = 0, n_groups = 0, n_merge_units = 0;
   int n_slots = 0;  // partial-result column slots
+  bool too_many_slots = false;  // a shared plan of more than 2^30 of them, which cannot run
   int split_tile = 0, split_item = 0;
   // some row's window hides a key from it: the units have shifts, and the
   // kernels that apply `window` run
@@ -145,8 +158,14 @@ struct SlotMarks {
 hb_status check_batch(const Dims& d, int num_blocks, const hb_batch_desc* desc, SlotMarks* marks,
                       const Window& w = Window());
 // The part of it that concerns the requests alone; *n_tokens receives their rows.
+// skip: leading table entries of each request that are not looked at, or null.
 hb_status check_requests(const Dims& d, int num_blocks, const hb_request* requests, int n, const Window& w,
-                         int64_t* n_tokens);
+                         int64_t* n_tokens, const std::vector<int>* skip = nullptr);
+// The part of it that forbids two requests to write one slot (of checked requests).
+hb_status check_slots(int num_blocks, const hb_request* requests, int n, int64_t n_tokens, SlotMarks* marks);
+// Requests (checked by this, too) and the groups of them that share a prefix.
+hb_status check_shared(const Dims& d, int num_blocks, const hb_request* requests, int n, const hb_prefix_group* groups,
+                       int n_groups, int64_t* n_tokens);
 
 // Fixed split lengths (keys, multiples of 64; 0 = chosen from the batch),
 // for tuning and tests.
@@ -161,6 +180,9 @@ struct PlanOptions {
   // are halved or split. And where items are few, in launches of any size, no wave
   // takes more than 256 keys alone.
   bool fit_round = false;
+  // groups of requests that share a prefix (checked; no window then)
+  const hb_prefix_group* groups = nullptr;
+  int n_groups = 0;
 };
 
 // Build the plan of a validated batch for a GPU with cu_count compute units.
@@ -175,6 +197,15 @@ struct RecordPlan {
   std::vector<int32_t> meta;
 };
 void build_records(const Plan& p, RecordPlan* out);
+
+// New tokens of one request that go to one pool block: rows tok0 .. tok0 + n - 1
+// at positions pos0 .., slots pos0 % 16 .. of `block`.
+struct AppendUnit {
+  int32_t tok0, pos0, n, block;
+};
+static_assert(sizeof(AppendUnit) == 16, "packed as 4 int32");
+// The batch's append units, behind what `out` holds; returns their number and their offset (int32).
+int build_append(const hb_request* requests, int n, std::vector<int32_t>* out, int* off);
 
 // Algorithmic flops and HBM bytes of one iteration (what the method must
 // compute and move, not what an implementation happens to do).

@@ -28,8 +28,11 @@ EXPORTED = ("hb_create_layer", "hb_destroy_layer", "hb_append_kv", "hb_run_itera
             "hb_gemm_tile_count", "hb_plan_gemms", "hb_layer_gemm_plans", "hb_run_iteration_noalloc",
             "hb_measure_device_rates", "hb_set_attention_window", "hb_window_dead_blocks", "hb_create_attention",
             "hb_destroy_attention", "hb_plan_attention", "hb_run_attention", "hb_copy_blocks", "hb_copy_model_blocks",
-            "hb_plan_compaction")
+            "hb_plan_compaction", "hb_plan_shared_attention", "hb_rope_frequencies", "hb_set_attention_rope",
+            "hb_run_append", "hb_create_sampler", "hb_destroy_sampler", "hb_sample")
 HB_LAT_FEATURES = 5
+HB_ROPE_HALF, HB_ROPE_INTERLEAVED = 0, 1
+HB_ROPE_UNSCALED, HB_ROPE_LINEAR, HB_ROPE_BY_PARTS = range(3)
 
 
 class hb_layer_config(C.Structure):
@@ -55,6 +58,20 @@ class hb_request(C.Structure):
 class hb_batch_desc(C.Structure):
     _fields_ = [("n_requests", C.c_int32), ("requests", C.POINTER(hb_request)),
                 ("x_in", C.c_void_p), ("x_out", C.c_void_p), ("out_dtype", C.c_int32)]
+
+
+class hb_prefix_group(C.Structure):
+    _fields_ = [("first", C.c_int32), ("count", C.c_int32), ("prefix_len", C.c_int32)]
+
+
+class hb_rope_scaling(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("original_context", C.c_int32), ("factor", C.c_double), ("low", C.c_double),
+                ("high", C.c_double)]
+
+
+class hb_sample_desc(C.Structure):
+    _fields_ = ([("n_rows", C.c_int32), ("logits_dtype", C.c_int32), ("logits", C.c_void_p), ("row_stride", C.c_int64)]
+                + [(n, C.c_void_p) for n in ("temperature", "top_k", "top_p", "min_p", "u", "tokens", "probs")])
 
 
 class hb_device_rates(C.Structure):
@@ -182,6 +199,21 @@ def load() -> C.CDLL:
     lib.hb_plan_attention.restype = st
     lib.hb_run_attention.argtypes = [C.c_void_p, C.POINTER(hb_kv_pool), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64]
     lib.hb_run_attention.restype = st
+    lib.hb_plan_shared_attention.argtypes = [C.c_void_p, C.c_int32, C.POINTER(hb_request), C.c_int32, C.c_void_p]
+    lib.hb_plan_shared_attention.restype = st
+    lib.hb_rope_frequencies.argtypes = [C.c_int32, C.c_double, C.POINTER(hb_rope_scaling), C.c_void_p]
+    lib.hb_rope_frequencies.restype = st
+    lib.hb_set_attention_rope.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_double]
+    lib.hb_set_attention_rope.restype = st
+    lib.hb_run_append.argtypes = [C.c_void_p, C.POINTER(hb_kv_pool), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                  C.c_void_p, C.c_int64, C.c_void_p, C.c_int64]
+    lib.hb_run_append.restype = st
+    lib.hb_create_sampler.argtypes = [C.c_int32, C.c_int32, C.c_void_p, C.POINTER(C.c_void_p)]
+    lib.hb_create_sampler.restype = st
+    lib.hb_destroy_sampler.argtypes = [C.c_void_p]
+    lib.hb_destroy_sampler.restype = None
+    lib.hb_sample.argtypes = [C.c_void_p, C.POINTER(hb_sample_desc)]
+    lib.hb_sample.restype = st
     for f in (lib.hb_copy_blocks, lib.hb_copy_model_blocks):
         f.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32]
         f.restype = st
@@ -423,6 +455,7 @@ class Attention:
         self.cfg = cfg
         self.num_blocks = num_blocks
         self.row = cfg.n_q_heads * cfg.head_dim             # values of a row of q
+        self.kv_row = cfg.n_kv_heads * cfg.head_dim         # values of a row of k or v
         self.block_values = cfg.n_kv_heads * 16 * cfg.head_dim  # values of a block of one pool
         self.n_tokens = 0
         self.pool = hb_kv_pool(0, 0, num_blocks)            # of the call at hand
@@ -459,6 +492,36 @@ def hb_plan_attention(attention: Attention, requests: Sequence[Tuple[int, int, I
     attention.n_tokens = sum(int(r[0]) for r in requests)
 
 
+def hb_plan_shared_attention(attention: Attention, requests: Sequence[Tuple[int, int, Iterable[int]]],
+                             groups: Sequence[Tuple[int, int, int]]) -> None:
+    """requests as for hb_plan_attention; groups: (first request, number of requests, prefix_len in tokens)."""
+    d, keep = _desc(requests, 0, 0, HB_OUT_BF16)
+    g = np.asarray(groups if len(groups) else np.zeros((0, 3), np.int32))
+    if g.ndim != 2 or g.shape[1] != 3 or g.dtype.kind not in "iu":
+        raise ValueError(f"groups: (first, count, prefix_len) each, not {g.dtype} {g.shape}")
+    g = _i32(g)
+    _check(load().hb_plan_shared_attention(attention.handle, d.n_requests, d.requests, len(g), g.ctypes.data))
+    attention.n_tokens = sum(int(r[0]) for r in requests)
+
+
+def hb_rope_frequencies(rotary_dim: int, theta: float, factor: Optional[float] = None, low: Optional[float] = None,
+                        high: Optional[float] = None, original_context: int = 0) -> np.ndarray:
+    """The rotary_dim / 2 frequencies: unscaled, divided by factor, or (low and high given) scaled by parts."""
+    if (low is None) != (high is None) or (low is not None and factor is None):
+        raise ValueError("scaling by parts: factor, low, high and original_context")
+    kind = HB_ROPE_UNSCALED if factor is None else HB_ROPE_LINEAR if low is None else HB_ROPE_BY_PARTS
+    s = hb_rope_scaling(kind, _int32(original_context), factor or 0.0, low or 0.0, high or 0.0)
+    f = np.zeros(max(1, _int32(rotary_dim) // 2))
+    _check(load().hb_rope_frequencies(_int32(rotary_dim), theta, C.byref(s), f.ctypes.data))
+    return f[:rotary_dim // 2]
+
+
+def hb_set_attention_rope(attention: Attention, inv_freq, layout: int = HB_ROPE_HALF, magnitude: float = 1.0) -> None:
+    """Rotation of later hb_run_append calls: the first 2 len(inv_freq) dimensions of a head; plan after it."""
+    f = np.ascontiguousarray(inv_freq, dtype=np.float64).reshape(-1)
+    _check(load().hb_set_attention_rope(attention.handle, 2 * len(f), _int32(layout), f.ctypes.data, magnitude))
+
+
 _bf16 = None  # torch.bfloat16, once torch is there
 
 
@@ -479,8 +542,7 @@ def _rows(name: str, t, n: int, row: int, device: int) -> int:
     return stride[0] if n > 1 else row
 
 
-def hb_run_attention(attention: Attention, q, k_pool, v_pool, out) -> None:
-    """q, out: bf16 [T][n_q_heads][head_dim] (or [T][n_q_heads * head_dim]), rows any multiple of 8 elements apart."""
+def _pools(attention: Attention, k_pool, v_pool) -> hb_kv_pool:
     # (written for few calls of few attributes: beside a small launch they are most of the time)
     blocks, device = attention.num_blocks, attention.device
     for p in (k_pool, v_pool):
@@ -490,8 +552,28 @@ def hb_run_attention(attention: Attention, q, k_pool, v_pool, out) -> None:
         if have < blocks * attention.block_values or have % attention.block_values:
             raise ValueError(f"{'k_pool' if p is k_pool else 'v_pool'}: at least {blocks} blocks of "
                              f"{attention.block_values} values, not {tuple(p.shape)}")
-    n, row, pool = attention.n_tokens, attention.row, attention.pool
+    pool = attention.pool
     pool.k_pool, pool.v_pool = k_pool.data_ptr(), v_pool.data_ptr()
+    return pool
+
+
+def hb_run_append(attention: Attention, q, k, v, k_pool, v_pool, q_out) -> None:
+    """q, k, v, q_out: bf16 [T][heads][head_dim] (or [T][heads * head_dim]), rows any multiple of 8 elements apart;
+    q_out may be q."""
+    pool = _pools(attention, k_pool, v_pool)
+    n, row, kv_row, device = attention.n_tokens, attention.row, attention.kv_row, attention.device
+    status = load().hb_run_append(attention.handle, pool, q.data_ptr(), _rows("q", q, n, row, device),
+                                  k.data_ptr(), _rows("k", k, n, kv_row, device),
+                                  v.data_ptr(), _rows("v", v, n, kv_row, device),
+                                  q_out.data_ptr(), _rows("q_out", q_out, n, row, device))
+    if status:
+        _check(status)
+
+
+def hb_run_attention(attention: Attention, q, k_pool, v_pool, out) -> None:
+    """q, out: bf16 [T][n_q_heads][head_dim] (or [T][n_q_heads * head_dim]), rows any multiple of 8 elements apart."""
+    pool = _pools(attention, k_pool, v_pool)
+    n, row, device = attention.n_tokens, attention.row, attention.device
     status = load().hb_run_attention(attention.handle, pool, q.data_ptr(), _rows("q", q, n, row, device),
                                      out.data_ptr(), _rows("out", out, n, row, device))
     if status:
@@ -634,6 +716,67 @@ def hb_select_chunk(model: hb_latency_model, cfg: hb_layer_config, decode_contex
                                   int(chunk_context), int(max_chunk), int(granularity), float(margin),
                                   C.byref(chunk), C.byref(ms)))
     return chunk.value, ms.value
+
+
+class Sampler:
+    """Owns an hb_sampler handle."""
+
+    def __init__(self, handle: C.c_void_p, max_rows: int, vocab: int, device: int):
+        import torch
+        self.handle = handle
+        self.max_rows = max_rows
+        self.vocab = vocab
+        self.device = device
+        self.dtypes = {torch.float32: HB_OUT_F32, torch.bfloat16: HB_OUT_BF16}
+        self.f32, self.i32 = torch.float32, torch.int32
+
+    def __del__(self):
+        try:
+            hb_destroy_sampler(self)
+        except Exception:
+            pass
+
+
+def hb_create_sampler(max_rows: int, vocab: int, stream: Optional[int] = None) -> Sampler:
+    import torch
+    if stream is None:
+        stream = torch.cuda.current_stream().cuda_stream
+    h = C.c_void_p()
+    _check(load().hb_create_sampler(_int32(max_rows), _int32(vocab), C.c_void_p(stream), C.byref(h)))
+    return Sampler(h, int(max_rows), int(vocab), torch.cuda.current_device())
+
+
+def hb_destroy_sampler(sampler: Sampler) -> None:
+    if sampler.handle is not None and sampler.handle.value:
+        load().hb_destroy_sampler(sampler.handle)
+        sampler.handle = None
+
+
+def hb_sample(sampler: Sampler, logits, u, tokens, temperature=None, top_k=None, top_p=None, min_p=None,
+              probs=None) -> None:
+    """logits: fp32 or bf16 [n][vocab], rows any distance apart; the others [n], top_k and tokens int32, the rest fp32."""
+    dtype = sampler.dtypes.get(logits.dtype)
+    if dtype is None or logits.get_device() != sampler.device:
+        raise ValueError(f"logits: an fp32 or bf16 tensor on GPU {sampler.device}, not {logits.dtype} on {logits.device}")
+    if logits.dim() != 2 or logits.size(1) != sampler.vocab or (logits.size(1) > 1 and logits.stride(1) != 1):
+        raise ValueError(f"logits: rows of {sampler.vocab} contiguous values, not {tuple(logits.shape)}, strides {logits.stride()}")
+    n = logits.size(0)
+
+    def row(name, t, want):
+        if t is None:
+            return 0
+        if t.dtype is not want or t.get_device() != sampler.device or t.dim() != 1 or t.size(0) != n or not t.is_contiguous():
+            raise ValueError(f"{name}: {n} contiguous values of {want} on GPU {sampler.device}, not {tuple(t.shape)} "
+                             f"of {t.dtype} on {t.device}")
+        return t.data_ptr()
+
+    f32, i32 = sampler.f32, sampler.i32
+    d = hb_sample_desc(n, dtype, logits.data_ptr(), logits.stride(0) if n > 1 else sampler.vocab,
+                       row("temperature", temperature, f32), row("top_k", top_k, i32), row("top_p", top_p, f32),
+                       row("min_p", min_p, f32), row("u", u, f32), row("tokens", tokens, i32), row("probs", probs, f32))
+    status = load().hb_sample(sampler.handle, C.byref(d))
+    if status:
+        _check(status)
 
 
 def hb_set_kernel_timing(layer: Layer, kernels) -> None:

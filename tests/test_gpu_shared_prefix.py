@@ -1,0 +1,163 @@
+"""hb_plan_shared_attention against 64-bit attention, through the C ABI. Pools are NaN in every slot that is no request's.
+The tolerance is attnref's: sharing changes the order in which fp32 parts are added, by no more than it allows for."""
+import numpy as np
+import pytest
+
+from attnref import Cache, assert_close, reference
+from hb_workloads import LayerShape, bf16_bits_to_f32
+
+pytestmark = pytest.mark.gpu
+
+
+def heads(nq, nkv, hd):
+    return LayerShape(f"{nq}q{nkv}kv{hd}", 64, nq, nkv, hd, 16, weight_seed=7)
+
+
+class Run:
+    """One batch: lens (chunk, context) per request, groups (first, count, prefix_len)."""
+
+    def __init__(self, shape, lens, groups, seed=0):
+        import torch
+        from paper_2503_22562_amd import hb as H
+        from paper_2503_22562_amd.harness import to_device_bf16
+        self.H, self.shape, self.groups = H, shape, groups
+        nb = sum(-(-(c + x) // 16) for c, x in lens) + 3
+        self.T = sum(c for c, _ in lens)
+        self.cache = cache = Cache(shape, nb, self.T, len(lens), seed)
+        group_of = {r: g for g in groups for r in range(g[0], g[0] + g[1])}
+        self.reqs, self.kv = [], []
+        for r, (c, x) in enumerate(lens):
+            first, _, p = group_of.get(r, (r, 1, 0))
+            if r == first:
+                req, k, v = cache.request(c, x, 0, 0)
+            else:
+                own, ko, vo = cache.request(c, x - p, 0, 0)  # its pages behind the prefix
+                k, v = np.concatenate([self.kv[first][0][:p], ko]), np.concatenate([self.kv[first][1][:p], vo])
+                req = (c, x, np.concatenate([self.reqs[first][2][:p // 16], own[2]]))
+            self.reqs.append(req)
+            self.kv.append((k, v))
+        self.q_bits = cache.bits(self.T, shape.n_q_heads, shape.head_dim)
+        self.q = to_device_bf16(self.q_bits)
+        self.out = torch.full((self.T, shape.n_q_heads, shape.head_dim), float("nan"), dtype=torch.bfloat16, device="cuda")
+        self.att = H.hb_create_attention(cache.dl.cfg, nb)
+        H.hb_plan_shared_attention(self.att, self.reqs, groups)
+
+    def run(self, out=None, q=None):
+        import torch
+        out = self.out if out is None else out
+        self.H.hb_run_attention(self.att, self.q if q is None else q, self.cache.dl.k_pool, self.cache.dl.v_pool, out)
+        torch.cuda.synchronize()
+        return out.float().cpu().numpy().astype(np.float64).reshape(self.T, self.shape.n_q_heads, self.shape.head_dim)
+
+    def check(self, got, what=""):
+        q = bf16_bits_to_f32(self.q_bits).astype(np.float64)
+        at = 0
+        for r, ((c, x, _), (k, v)) in enumerate(zip(self.reqs, self.kv)):
+            o, pv = reference(q[at:at + c], k, v, np.arange(x, x + c), 0, 0)
+            assert_close(got[at:at + c], o, pv, f"{what} request {r} ({c}, {x})")
+            at += c
+
+
+HEADS = [(4, 2, 64), (2, 2, 128), (8, 2, 128), (8, 1, 128), (16, 1, 64), (32, 8, 128)]
+CASES = {
+    "two": ([(1, 40), (1, 33)], [(0, 2, 32)]),
+    "only new tokens of their own": ([(1, 32)] * 3, [(0, 3, 32)]),
+    "one page": ([(1, 16 + 7 * i) for i in range(9)], [(0, 9, 16)]),
+    "odd lengths": ([(1, 700 + 13 * i) for i in range(20)], [(0, 20, 688)]),
+    "two groups and others": ([(1, 5)] + [(1, 700 + 13 * i) for i in range(20)] + [(1, 300)], [(2, 9, 640), (12, 5, 16)]),
+    "drafts": ([(1, 5), (2, 3000), (1, 2100), (4, 2100), (1, 9)], [(1, 3, 2096)]),
+    "chunks between": ([(1, 500), (90, 500), (1, 600), (1, 480), (70, 480), (1, 481)], [(0, 6, 480)]),
+    "long and short": ([(1, 6000)] + [(1, 2050)] * 33, [(0, 34, 2048)]),
+    "more rows than columns": ([(1, 500)] * 70, [(0, 40, 496), (40, 30, 16)]),
+}
+
+
+@pytest.mark.parametrize("nqkvhd", HEADS, ids=str)
+@pytest.mark.parametrize("name", CASES)
+def test_shared_prefixes(hb, nqkvhd, name):
+    r = Run(heads(*nqkvhd), *CASES[name], seed=len(name))
+    r.check(r.run(), name)
+
+
+@pytest.mark.parametrize("nqkvhd", [(4, 2, 64), (8, 2, 128), (8, 8, 128)], ids=str)
+@pytest.mark.parametrize("name", ["odd lengths", "drafts", "chunks between", "more rows than columns"])
+@pytest.mark.parametrize("split_tile,split_item", [(64, 64), (256, 64), (4096, 4096)])
+def test_splits(hb, monkeypatch, nqkvhd, name, split_tile, split_item):
+    """Prefixes and own keys cut finely, and not at all."""
+    monkeypatch.setenv("HB_ATTN_SPLIT_TILE", str(split_tile))
+    monkeypatch.setenv("HB_ATTN_SPLIT_ITEM", str(split_item))
+    r = Run(heads(*nqkvhd), *CASES[name], seed=21)
+    r.check(r.run(), name)
+
+
+def test_many_rows_behind_a_long_prefix(hb):
+    r = Run(heads(16, 4, 128), [(1, 5008 + 9 * i) for i in range(100)], [(0, 100, 5008)], seed=22)
+    r.check(r.run())
+
+
+def test_keys_that_dominate(hb):
+    """The largest scores in the prefix for some rows and behind it for others: parts whose maxima lie far apart."""
+    import torch
+    r = Run(heads(8, 2, 128), [(1, 400 + i) for i in range(12)], [(0, 12, 384)], seed=23)
+    q = torch.zeros_like(r.q)
+    q[::2, :, 0], q[1::2, :, 0] = 60.0, -60.0
+    r.q, r.q_bits = q, q.view(torch.int16).cpu().numpy().view(np.uint16)
+    r.check(r.run())
+
+
+def test_the_same_bits_every_time_and_strided_rows(hb):
+    import torch
+    r = Run(heads(8, 2, 128), *CASES["odd lengths"], seed=24)
+    want = r.run()
+    row = 8 * 128
+    for _ in range(3):
+        r.out.fill_(float("nan"))
+        assert np.array_equal(r.run(), want)
+    fused = torch.randn(r.T, row + 512, device="cuda").to(torch.bfloat16)
+    fused[:, :row] = r.q.view(r.T, row)
+    wide = torch.full((r.T + 2, row + 24), 7.0, dtype=torch.bfloat16, device="cuda")
+    assert np.array_equal(r.run(wide[:r.T, :row], fused[:, :row]), want)
+    assert (wide[r.T:] == 7.0).all() and (wide[:, row:] == 7.0).all()
+
+
+def test_plans_replace_each_other(hb):
+    """Shared, unshared and other batches in turn on one handle; no groups: hb_plan_attention's own bits."""
+    import torch
+    r = Run(heads(8, 2, 128), *CASES["drafts"], seed=25)
+    shared = r.run()
+    hb.hb_plan_attention(r.att, r.reqs)
+    alone = r.run()
+    r.check(alone)
+    for none in ([], [(0, 2, 0)], [(2, 1, 2096)]):
+        hb.hb_plan_shared_attention(r.att, r.reqs, none)
+        assert np.array_equal(r.run(), alone)
+    hb.hb_plan_shared_attention(r.att, [], [])
+    hb.hb_run_attention(r.att, r.q[:0], r.cache.dl.k_pool, r.cache.dl.v_pool, r.out[:0])
+    with pytest.raises(hb.HBError) as e:  # the plan before stays: of no rows
+        hb.hb_plan_shared_attention(r.att, r.reqs, [(1, 3, 2112)])
+    assert e.value.status == hb.HB_ERR_INVALID
+    hb.hb_run_attention(r.att, r.q[:0], r.cache.dl.k_pool, r.cache.dl.v_pool, r.out[:0])
+    hb.hb_plan_shared_attention(r.att, r.reqs, r.groups)
+    with pytest.raises(hb.HBError):
+        hb.hb_plan_shared_attention(r.att, r.reqs, [(0, 3, 16)])
+    assert np.array_equal(r.run(), shared)
+    torch.cuda.synchronize()
+
+
+def test_two_handles_on_two_streams(hb):
+    import torch
+    runs = [Run(heads(8, 2, 128), *CASES["odd lengths"], seed=26)]
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        runs.append(Run(heads(8, 2, 128), *CASES["long and short"], seed=27))
+    want = [r.run() for r in runs]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for r in runs:
+            r.out.fill_(float("nan"))
+        torch.cuda.synchronize()
+        for r in runs:
+            r.H.hb_run_attention(r.att, r.q, r.cache.dl.k_pool, r.cache.dl.v_pool, r.out)
+        torch.cuda.synchronize()
+        for r, w in zip(runs, want):
+            assert np.array_equal(r.out.float().cpu().numpy().astype(np.float64), w)
