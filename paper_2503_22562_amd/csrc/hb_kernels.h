@@ -4,6 +4,7 @@
 #include <hip/hip_runtime_api.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <atomic>
 
 #include "hb_plan.h"
@@ -207,17 +208,40 @@ void launch_gather_rows(hipStream_t s, const uint16_t* src, int64_t n_src, const
                         uint16_t* out);
 // out[r] = index of the largest of x[r][0..V) (lowest index on ties).
 void launch_argmax(hipStream_t s, const float* x, int n_rows, int V, int32_t* out);
-// Tokens drawn from rows of logits (hb_sample_desc).
+// Tokens drawn from rows of logits (hb_sample_desc), at most kSampleRows at a time,
+// in slices: their extents, then the rows' histograms, then the tokens.
+constexpr int kSampleRows = 256, kSampleSlices = 64, kSampleBins = 2048, kSampleNear = 1024;
+struct SampleExtent {
+  unsigned long long top, lo;  // places of the largest element and of the least finite one
+};
+struct SampleState {
+  unsigned long long w[kSampleBins];  // weights and counts of the bins
+  uint32_t c[kSampleBins];
+  unsigned long long min_w;  // weight that min_p keeps
+  uint32_t n, pad;           // likely tokens found, of which the list holds the first kSampleNear
+  unsigned long long list[kSampleNear];
+};
+// Slices of a row (all of slice_len elements but the last): about eight workgroups
+// per CU in all, of 2048 elements at least.
+inline void sample_slices(int rows, int vocab, int* slices, int* slice_len) {
+  const int want = std::max(1, std::min(kSampleSlices, 2048 / rows));
+  *slice_len = std::max(2048, ((vocab + want - 1) / want + 7) / 8 * 8);
+  *slices = (vocab + *slice_len - 1) / *slice_len;
+}
 struct SampleArgs {
   const void* logits;
   int64_t stride;  // elements from row to row
   int bf16, rows, vocab;
-  int shift;  // weights are summed as multiples of 2^-shift (set by the launch)
   const float* temperature;
   const int32_t* top_k;
   const float *top_p, *min_p, *u;
   int32_t* tokens;
   float* probs;
+  // workspace: [kSampleRows or the sampler's rows] each, kSampleSlices extents a row
+  SampleExtent* extents;
+  SampleState* state;
+  // set by the launch: the first row, its slices; weights are summed as multiples of 2^-shift
+  int row0, slices, slice_len, shift;
 };
 void launch_sample(hipStream_t s, SampleArgs a);
 

@@ -1,6 +1,6 @@
 // Sampling handles: the argument checks around k_sample.hip.
+#include <algorithm>
 #include <new>
-#include <utility>
 
 #include <hip/hip_runtime.h>
 
@@ -14,7 +14,20 @@ using namespace hb;
 struct hb_sampler {
   int max_rows = 0, vocab = 0, device = 0;
   hipStream_t stream = nullptr;
+  SampleExtent* extents = nullptr;
+  SampleState* state = nullptr;
 };
+
+namespace {
+void free_sampler(hb_sampler* s) {
+  if (!s) return;
+  const DeviceGuard on(s->device);
+  (void)hipStreamSynchronize(s->stream);
+  for (void* p : {(void*)s->extents, (void*)s->state})
+    if (p) (void)hipFree(p);
+  delete s;
+}
+}  // namespace
 
 extern "C" {
 
@@ -32,12 +45,19 @@ hb_status hb_create_sampler(int32_t max_rows, int32_t vocab, void* hip_stream, h
     s->vocab = vocab;
     s->device = device;
     s->stream = static_cast<hipStream_t>(hip_stream);
+    const size_t rows = std::min(max_rows, kSampleRows);
+    if (hipMalloc((void**)&s->extents, rows * kSampleSlices * sizeof(SampleExtent)) != hipSuccess ||
+        hipMalloc((void**)&s->state, rows * sizeof(SampleState)) != hipSuccess) {
+      (void)hipGetLastError();
+      free_sampler(s);
+      return fail(HB_ERR_OOM, "sampling workspace of %d rows", (int)rows);
+    }
     *out = s;
     return HB_OK;
   });
 }
 
-void hb_destroy_sampler(hb_sampler* s) { delete s; }
+void hb_destroy_sampler(hb_sampler* s) { free_sampler(s); }
 
 hb_status hb_sample(hb_sampler* s, const hb_sample_desc* d) {
   if (!s) return fail(HB_ERR_INVALID, "null sampler handle");
@@ -57,6 +77,8 @@ hb_status hb_sample(hb_sampler* s, const hb_sample_desc* d) {
   a.u = d->u;
   a.tokens = d->tokens;
   a.probs = d->probs;
+  a.extents = s->extents;
+  a.state = s->state;
   launch_sample(s->stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(HB_ERR_HIP, "sampling launch: %s", hipGetErrorString(e));
