@@ -210,23 +210,34 @@ void launch_gather_rows(hipStream_t s, const uint16_t* src, int64_t n_src, const
 void launch_argmax(hipStream_t s, const float* x, int n_rows, int V, int32_t* out);
 // Tokens drawn from rows of logits (hb_sample_desc), at most kSampleRows at a time,
 // in slices: their extents, then the rows' histograms, then the tokens.
-constexpr int kSampleRows = 256, kSampleSlices = 64, kSampleBins = 2048, kSampleNear = 1024;
+constexpr int kSampleRows = 256, kSampleSlices = 64, kSampleBins = 2048, kSampleNear = 256, kSampleList = 2048;
 struct SampleExtent {
   unsigned long long top, lo;  // places of the largest element and of the least finite one
 };
 struct SampleState {
   unsigned long long w[kSampleBins];  // weights and counts of the bins
   uint32_t c[kSampleBins];
-  unsigned long long min_w;  // weight that min_p keeps
-  uint32_t n, pad;           // likely tokens found, of which the list holds the first kSampleNear
-  unsigned long long list[kSampleNear];
+  uint32_t n_near, n_list;  // elements found, of which the lists hold the first ones
+  uint32_t slices_done, parts_done;
+  int32_t pending, search[7];  // a row whose likely tokens do not tell, and the bins to look into
+  unsigned long long near[kSampleNear], list[kSampleList];
 };
-// Slices of a row (all of slice_len elements but the last): about eight workgroups
-// per CU in all, of 2048 elements at least.
+// Slices of a row (all of slice_len elements but the last): few rows in as many as
+// are worth a workgroup's start, many in about eight per CU, of which each adds its
+// histogram to the row's once (64 rows of 128256, weights: 8K elements 17.6 us, 4K
+// 22.8, 16K 20.1; 256 rows: 16K 40.6, 32K 42.8).
 inline void sample_slices(int rows, int vocab, int* slices, int* slice_len) {
   const int want = std::max(1, std::min(kSampleSlices, 2048 / rows));
-  *slice_len = std::max(2048, ((vocab + want - 1) / want + 7) / 8 * 8);
+  const int least = (int64_t)rows * ((vocab + 2047) / 2048) > 1024 ? 8192 : 2048;
+  *slice_len = std::max(least, ((vocab + want - 1) / want + 7) / 8 * 8);
   *slices = (vocab + *slice_len - 1) / *slice_len;
+}
+// Parts of a row (of part_len elements) where it has to be read again: as many as are
+// worth a workgroup's start, for few rows and where all rows are (about eight per CU).
+inline void sample_parts(int rows, int vocab, int* parts, int* part_len) {
+  const int want = std::max(1, std::min(32, 2048 / rows));
+  *part_len = std::max(4096, ((vocab + want - 1) / want + 7) / 8 * 8);
+  *parts = (vocab + *part_len - 1) / *part_len;
 }
 struct SampleArgs {
   const void* logits;
@@ -240,8 +251,8 @@ struct SampleArgs {
   // workspace: [kSampleRows or the sampler's rows] each, kSampleSlices extents a row
   SampleExtent* extents;
   SampleState* state;
-  // set by the launch: the first row, its slices; weights are summed as multiples of 2^-shift
-  int row0, slices, slice_len, shift;
+  // set by the launch: the first row, slices and parts of a row; weights are summed as multiples of 2^-shift
+  int row0, slices, slice_len, parts, part_len, shift;
 };
 void launch_sample(hipStream_t s, SampleArgs a);
 

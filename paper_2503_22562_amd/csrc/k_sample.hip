@@ -16,6 +16,7 @@
 #include <algorithm>
 #include <cfloat>
 #include <cstddef>
+#include <type_traits>
 
 #include "hb_device.h"
 #include "hb_kernels.h"
@@ -25,15 +26,38 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int kBins = 2048;   // of a row's histogram: 1/64 of a factor e or less, over the 32 factors that have weight
-constexpr int kList = 4096;   // elements sorted at a time
-constexpr int kNearList = kSampleNear;
+constexpr int kBins = kSampleBins, kList = kSampleList, kNearList = kSampleNear;
 constexpr float kNear = 8.f;  // tokens whose weight is above e^-8 are listed while the histogram is made
-constexpr int kSteps = 32;    // steps of an octave in the table of powers of two
-constexpr int kSliceThreads = 256, kSliceList = 512, kRowThreads = 1024;
-static_assert(kBins == kSampleBins, "workspace");
+constexpr int kSteps = 64;    // steps of an octave in the table of powers of two
+constexpr int kThreads = 256, kWaves = kThreads / 64;
 
-// The elements (fp32 or bf16) [first, first + n) of a row, f(value, index in the row) for each; any alignment.
+// 2^(j / kSteps), rounded to fp64
+__device__ const double kPow2[kSteps] = {
+    0x1.0000000000000p+0, 0x1.02c9a3e778061p+0, 0x1.059b0d3158574p+0, 0x1.0874518759bc8p+0,
+    0x1.0b5586cf9890fp+0, 0x1.0e3ec32d3d1a2p+0, 0x1.11301d0125b51p+0, 0x1.1429aaea92de0p+0,
+    0x1.172b83c7d517bp+0, 0x1.1a35beb6fcb75p+0, 0x1.1d4873168b9aap+0, 0x1.2063b88628cd6p+0,
+    0x1.2387a6e756238p+0, 0x1.26b4565e27cddp+0, 0x1.29e9df51fdee1p+0, 0x1.2d285a6e4030bp+0,
+    0x1.306fe0a31b715p+0, 0x1.33c08b26416ffp+0, 0x1.371a7373aa9cbp+0, 0x1.3a7db34e59ff7p+0,
+    0x1.3dea64c123422p+0, 0x1.4160a21f72e2ap+0, 0x1.44e086061892dp+0, 0x1.486a2b5c13cd0p+0,
+    0x1.4bfdad5362a27p+0, 0x1.4f9b2769d2ca7p+0, 0x1.5342b569d4f82p+0, 0x1.56f4736b527dap+0,
+    0x1.5ab07dd485429p+0, 0x1.5e76f15ad2148p+0, 0x1.6247eb03a5585p+0, 0x1.6623882552225p+0,
+    0x1.6a09e667f3bcdp+0, 0x1.6dfb23c651a2fp+0, 0x1.71f75e8ec5f74p+0, 0x1.75feb564267c9p+0,
+    0x1.7a11473eb0187p+0, 0x1.7e2f336cf4e62p+0, 0x1.82589994cce13p+0, 0x1.868d99b4492edp+0,
+    0x1.8ace5422aa0dbp+0, 0x1.8f1ae99157736p+0, 0x1.93737b0cdc5e5p+0, 0x1.97d829fde4e50p+0,
+    0x1.9c49182a3f090p+0, 0x1.a0c667b5de565p+0, 0x1.a5503b23e255dp+0, 0x1.a9e6b5579fdbfp+0,
+    0x1.ae89f995ad3adp+0, 0x1.b33a2b84f15fbp+0, 0x1.b7f76f2fb5e47p+0, 0x1.bcc1e904bc1d2p+0,
+    0x1.c199bdd85529cp+0, 0x1.c67f12e57d14bp+0, 0x1.cb720dcef9069p+0, 0x1.d072d4a07897cp+0,
+    0x1.d5818dcfba487p+0, 0x1.da9e603db3285p+0, 0x1.dfc97337b9b5fp+0, 0x1.e502ee78b3ff6p+0,
+    0x1.ea4afa2a490dap+0, 0x1.efa1bee615a27p+0, 0x1.f50765b6e4540p+0, 0x1.fa7c1819e90d8p+0,
+};
+
+// Consecutive elements of a row, from index `first` on.
+template <int N>
+struct Run {
+  float x[N];
+  int first;
+};
+// Elements (fp32 or bf16) [first, first + n) of a row, f(Run) for all of them; any alignment.
 template <bool BF16>
 struct Logits {
   const uint16_t* h;
@@ -41,42 +65,50 @@ struct Logits {
   int first, n;
   __device__ __forceinline__ Logits(const void* p, int64_t row, int first, int n)
       : h(static_cast<const uint16_t*>(p) + row), f(static_cast<const float*>(p) + row), first(first), n(n) {}
-  // Not a number: never drawn, as -infinity; +infinity: as the largest finite value; -0: as 0.
-  static __device__ __forceinline__ float clean(float x) { return x == x ? fminf(x, FLT_MAX) + 0.0f : -INFINITY; }
-  __device__ __forceinline__ float at(int i) const { return clean(BF16 ? bf16_to_f32(h[i]) : f[i]); }
+  __device__ __forceinline__ float at(int i) const { return BF16 ? bf16_to_f32(h[i]) : f[i]; }
+  static constexpr int kPer = BF16 ? 8 : 4;  // elements of a 16-byte load
+  static __device__ __forceinline__ Run<kPer> run(u32x4 r, int e) {
+    Run<kPer> v;
+    v.first = e;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (BF16) {
+        v.x[2 * j] = bf16_lo(r[j]);
+        v.x[2 * j + 1] = bf16_hi(r[j]);
+      } else {
+        v.x[j] = __uint_as_float(r[j]);
+      }
+    }
+    return v;
+  }
   // LOADS 16-byte loads of a thread in flight
-  template <int THREADS, int LOADS, typename F>
+  template <int LOADS, typename F>
   __device__ __forceinline__ void each(F&& fn) const {
-    constexpr int PER = BF16 ? 8 : 4, SIZE = BF16 ? 2 : 4;
+    constexpr int SIZE = BF16 ? 2 : 4;
     const int tid = threadIdx.x;
     const uintptr_t p = BF16 ? reinterpret_cast<uintptr_t>(h + first) : reinterpret_cast<uintptr_t>(f + first);
     const int head = min(n, (int)((16 - (p & 15)) & 15) / SIZE);  // elements before the first 16-byte boundary
-    const int nv = (n - head) / PER, tail = head + nv * PER;
-    if (tid < head) fn(at(first + tid), first + tid);
-    if (tid < n - tail) fn(at(first + tail + tid), first + tail + tid);
+    const int nv = (n - head) / kPer, tail = head + nv * kPer;
     const u32x4* v = BF16 ? reinterpret_cast<const u32x4*>(h + first + head) : reinterpret_cast<const u32x4*>(f + first + head);
-    for (int i0 = tid; i0 < nv; i0 += LOADS * THREADS) {
+    int i0 = tid;
+    for (; i0 - tid + LOADS * kThreads <= nv; i0 += LOADS * kThreads) {
       u32x4 r[LOADS];
 #pragma unroll
-      for (int k = 0; k < LOADS; ++k)
-        if (i0 + k * THREADS < nv) r[k] = v[i0 + k * THREADS];
+      for (int k = 0; k < LOADS; ++k) r[k] = v[i0 + k * kThreads];
 #pragma unroll
-      for (int k = 0; k < LOADS; ++k) {
-        if (i0 + k * THREADS >= nv) break;
-        const int e = first + head + (i0 + k * THREADS) * PER;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (BF16) {
-            fn(clean(bf16_lo(r[k][j])), e + 2 * j);
-            fn(clean(bf16_hi(r[k][j])), e + 2 * j + 1);
-          } else {
-            fn(clean(__uint_as_float(r[k][j])), e + j);
-          }
-        }
-      }
+      for (int k = 0; k < LOADS; ++k) fn(run(r[k], first + head + (i0 + k * kThreads) * kPer));
     }
+#pragma unroll 1
+    for (; i0 < nv; i0 += kThreads) fn(run(v[i0], first + head + i0 * kPer));
+    // the ragged ends: fewer than kPer elements each
+    const int at = first + (tid < head ? tid : tail + tid - head);
+    if (tid < head + n - tail) fn(Run<1>{{this->at(at)}, at});
   }
 };
+
+// A logit as it counts: not a number: never drawn, as -infinity; +infinity: as the largest
+// finite value; -0: as 0.
+__device__ __forceinline__ float clean(float x) { return x == x ? fminf(x, FLT_MAX) + 0.0f : -INFINITY; }
 
 // Place in the descending order, as a number: larger first. (No two are the same.)
 __device__ __forceinline__ u64 place_of(float x, int i) {
@@ -89,21 +121,19 @@ __device__ __forceinline__ float value_of(u64 place) {
 }
 __device__ __forceinline__ int index_of(u64 place) { return (int)~(uint32_t)place; }
 
-// Weights of a row: w = 2^(y / 32), y = (x - max) 32 log2(e) / t, from the nearest whole
-// step's power (a table and the exponent) and the rest's, |r| <= 1/2, the series of
-// exp(r ln2 / 32) to its fifth power: what is left out is below 2^-48 of it.
+// Weights of a row, w 2^shift with w = 2^(y / 64), y = (x - max) 64 log2(e) / t: the
+// power of the nearest whole step (a table, with the shift in it, and the exponent)
+// times the rest's, |r| <= 1/2, by the series of exp(r ln2 / 64) to its fourth power:
+// what is left out is below 2^-44 of it. |y| < 2^16 (Scale::clamp).
 struct Weights {
   double max, rate;
-  int shift;
-  const double* pow2;
-  // w 2^shift, not rounded
+  const double* pow2;  // in LDS
   __device__ __forceinline__ double scaled(float x) const {
-    // -infinity, and whatever is too far away: 2^-128, which rounds to none
-    const double y = fmax(((double)x - max) * rate, -128.0 * kSteps);
-    const double k = rint(y), a = (y - k) * (0.693147180559945309417 / kSteps);
-    const double p = fma(a, fma(a, fma(a, fma(a, fma(a, 1.0 / 120, 1.0 / 24), 1.0 / 6), 0.5), 1.0), 1.0);
+    const double y = ((double)x - max) * rate, k = rint(y), r = y - k;
+    const double p = fma(r, fma(r, fma(r, fma(r, 0x1.3b2ab6fba4e77p-31, 0x1.c6b08d704a0cp-23), 0x1.ebfbdff82c58fp-15),
+                                0x1.62e42fefa39efp-7), 1.0);  // (ln2 / 64)^n / n!
     const int n = (int)k;
-    return ldexp(p * pow2[n & (kSteps - 1)], (n >> 5) + shift);
+    return ldexp(p * pow2[n & (kSteps - 1)], n >> 6);
   }
   // to the nearest integer below 2^52, by the addition of 2^52
   static __device__ __forceinline__ u64 whole(double s) {
@@ -111,31 +141,24 @@ struct Weights {
   }
 };
 
-// f over all threads' values; every thread gets the result. red: a word per wave.
-template <int THREADS, typename T, typename F>
-__device__ __forceinline__ T block_reduce(T v, F&& f, u64* red) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) v = f(v, (T)__shfl_xor(v, d));
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = (u64)v;
-  __syncthreads();
-  T r = (T)red[0];
-#pragma unroll
-  for (int w = 1; w < THREADS / 64; ++w) r = f(r, (T)red[w]);
-  __syncthreads();
-  return r;
-}
 struct Least {
   __device__ __forceinline__ u64 operator()(u64 a, u64 b) const { return a < b ? a : b; }
-};
-struct Largest {
-  __device__ __forceinline__ u64 operator()(u64 a, u64 b) const { return a > b ? a : b; }
 };
 struct Sum {
   __device__ __forceinline__ u64 operator()(u64 a, u64 b) const { return a + b; }
 };
+struct Largest {
+  __device__ __forceinline__ u64 operator()(u64 a, u64 b) const { return a > b ? a : b; }
+};
+template <typename F>
+__device__ __forceinline__ u64 wave_reduce(u64 v, F&& f) {
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) v = f(v, (u64)__shfl_xor(v, d));
+  return v;
+}
 
-// Running sums, over all threads, of a value of each.
-template <int THREADS, typename T>
+// Running sums, over all threads, of a value of each. red: a word per wave, free again after the next barrier.
+template <typename T>
 __device__ __forceinline__ T block_scan(T v, u64* red) {
   T incl = v;
 #pragma unroll
@@ -145,9 +168,22 @@ __device__ __forceinline__ T block_scan(T v, u64* red) {
   }
   if ((threadIdx.x & 63) == 63) red[threadIdx.x >> 6] = (u64)incl;
   __syncthreads();
-  for (int k = 0; k < (int)(threadIdx.x >> 6); ++k) incl += (T)red[k];
-  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kWaves - 1; ++k)
+    if (k < (int)(threadIdx.x >> 6)) incl += (T)red[k];
   return incl;
+}
+
+// The first of n > 0 places (n <= 64 * 64) at which met(i) holds, the last where it does
+// nowhere; met grows with i. A wave's work, with all of its lanes.
+template <typename F>
+__device__ __forceinline__ int first_met(int n, F&& met) {
+  const int lane = threadIdx.x & 63, step = (n + 63) / 64;
+  const u64 a = __ballot(met(min(n - 1, (lane + 1) * step - 1)));
+  if (a == 0) return n - 1;
+  const int i0 = (__ffsll(a) - 1) * step;
+  const u64 b = __ballot(lane < step && i0 + lane < n && met(min(n - 1, i0 + lane)));
+  return i0 + __ffsll(b) - 1;
 }
 
 // A row's settings, its extent, and what its weights and bins are then.
@@ -171,121 +207,107 @@ struct Extent {
   float lo;
 };
 // Of a whole row, from its slices'.
-template <int THREADS>
-__device__ __forceinline__ Extent row_extent(const SampleArgs& a, int r, u64* red) {
-  u64 top = 0, lo = ~0ull;
-  for (int i = threadIdx.x; i < a.slices; i += THREADS) {
-    const SampleExtent e = a.extents[(size_t)r * a.slices + i];
-    top = Largest()(top, e.top);
-    lo = Least()(lo, e.lo);
-  }
-  top = block_reduce<THREADS>(top, Largest(), red);
-  return {top, value_of(block_reduce<THREADS>(lo, Least(), red))};
+__device__ __forceinline__ Extent row_extent(const SampleArgs& a, int r) {
+  static_assert(kSampleSlices <= 64, "one a lane");
+  const int i = threadIdx.x & 63;
+  SampleExtent e = {0, ~0ull};
+  if (i < a.slices) e = a.extents[(size_t)r * a.slices + i];
+  const u64 top = wave_reduce(e.top, Largest()), lo = wave_reduce(e.lo, Least());
+  return {top, value_of(lo)};
 }
 // Greedy rows, and those of which nothing may be drawn, need no more than that.
 __device__ __forceinline__ bool no_weights(const Setting& g, const Extent& e) {
   return !(g.t > 0.f) || g.k == 1 || value_of(e.top) == -INFINITY;
 }
 struct Scale {
-  Weights weight;
-  float max, per;  // bins: (max - x) per
-  double least;    // scaled weights that min_p keeps
+  Weights weights;
+  float max, cut;  // logits below `cut` have no weight
+  float per;       // bins: (max - x) per
+  bool far;        // the temperature is so high that there is no such cut
   int near;        // bins that are listed while the histogram is made
-  // (A NaN, from a scale of 0 or infinity, and the elements without weight: the last bin.)
-  __device__ __forceinline__ int bin_of(float v) const { return (int)fminf((max - v) * per, (float)(kBins - 1)); }
+  int shift;
+  // A logit as its weight needs it: neither below the cut nor above the largest. (Not a number: the cut.)
+  __device__ __forceinline__ float clamp(float v) const { return fminf(fmaxf(v, cut), max); }
+  template <bool FAR>
+  __device__ __forceinline__ u64 weight(float v) const {
+    const u64 w = Weights::whole(weights.scaled(clamp(v)));
+    return FAR && !(v > -INFINITY) ? 0 : w;
+  }
+  __device__ __forceinline__ u64 weight_of(float v) const { return far ? weight<true>(v) : weight<false>(v); }
+  __device__ __forceinline__ int bin_of(float v) const {
+    return (int)fminf((max - clamp(v)) * per, (float)(kBins - 1));
+  }
 };
 __device__ __forceinline__ Scale scale_of(const Setting& g, const Extent& e, int shift, const double* pow2) {
   Scale c;
   c.max = value_of(e.top);
-  // distances beyond which a weight rounds to none
-  const float reach = fminf(c.max - e.lo, (shift + 2) * 0.6931472f * g.t);
-  c.weight = {(double)c.max, 1.4426950408889634 * kSteps / (double)g.t, shift, pow2};
-  c.per = reach > 0.f ? kBins / reach : 0.f;
-  c.least = g.min_p > 0.f ? ldexp((double)g.min_p, shift) : 0.0;
+  // a weight of 2^-(shift + 2) rounds to none, and so does the cut's: it lies no nearer to the largest
+  const float reach = (shift + 2) * 0.6931472f * g.t;
+  c.cut = c.max - reach;
+  if ((double)c.max - (double)c.cut < (double)reach) c.cut = value_of(place_of(c.cut, 0) - (1ull << 32));
+  c.far = !(c.cut >= -FLT_MAX);
+  if (c.far) c.cut = -FLT_MAX;
+  // (the second rate: temperatures for which the logit next to the largest has no weight)
+  c.weights = {(double)c.max, fmin(1.4426950408889634 * kSteps / (double)g.t, 65536.0 / ((double)c.max - (double)c.cut)), pow2};
+  const float used = fminf(c.max - e.lo, reach);  // (infinite, or next to nothing: one bin)
+  c.per = used > 1e-30f ? kBins / used : 0.f;
   c.near = min(kBins, (int)fminf(kNear * g.t * c.per, (float)kBins));
+  c.shift = shift;
   return c;
 }
-__device__ __forceinline__ void fill_table(double* pow2) {
-  if (threadIdx.x < kSteps) pow2[threadIdx.x] = exp2((double)threadIdx.x / kSteps);
-  __syncthreads();
-}
-
-template <bool BF16>
-__device__ __forceinline__ Logits<BF16> slice_of(const SampleArgs& a, int r, int s) {
-  const int first = s * a.slice_len;
-  return Logits<BF16>(a.logits, (int64_t)(a.row0 + r) * a.stride, first, min(a.slice_len, a.vocab - first));
+// The table, with a barrier to come before it is read.
+__device__ __forceinline__ void fill_table(double* pow2, int shift) {
+  if (threadIdx.x < kSteps) pow2[threadIdx.x] = ldexp(kPow2[threadIdx.x], shift);
 }
 
 // A slice of a row: its extent. (And the row's state is cleared for the next kernel.)
 template <bool BF16>
-__global__ __launch_bounds__(kSliceThreads) void sample_extent_kernel(SampleArgs a) {
-  __shared__ u64 red[kSliceThreads / 64];
+__global__ __launch_bounds__(kThreads) void sample_extent_kernel(SampleArgs a) {
+  __shared__ u64 red[2][kWaves];
   const int r = blockIdx.x / a.slices, s = blockIdx.x - r * a.slices;
-  uint32_t* state = reinterpret_cast<uint32_t*>(a.state + r);
-  constexpr int words = offsetof(SampleState, list) / 4;
-  for (int i = s * kSliceThreads + threadIdx.x; i < words; i += a.slices * kSliceThreads) state[i] = 0;
-  u64 top = 0;
-  float lo = INFINITY;
-  slice_of<BF16>(a, r, s).template each<kSliceThreads, 8>([&](float v, int i) {
-    top = Largest()(top, place_of(v, i));
-    lo = v > -INFINITY ? fminf(lo, v) : lo;
-  });
-  top = block_reduce<kSliceThreads>(top, Largest(), red);
-  const u64 low = block_reduce<kSliceThreads>(place_of(lo, 0), Least(), red);
-  if (threadIdx.x == 0) a.extents[blockIdx.x] = {top, low};
-}
-
-// A slice of a row: its weights into the row's histogram, its likely tokens into the row's list.
-template <bool BF16>
-__global__ __launch_bounds__(kSliceThreads) void sample_weights_kernel(SampleArgs a) {
-  __shared__ u64 hist_w[kBins];
-  __shared__ uint32_t hist_c[kBins];
-  __shared__ u64 list[kSliceList];
-  __shared__ u64 red[kSliceThreads / 64];
-  __shared__ double pow2[kSteps];
-  __shared__ uint32_t n, base;
-  const int r = blockIdx.x / a.slices, tid = threadIdx.x;
-  const Setting g = setting_of(a, a.row0 + r);
-  const Extent e = row_extent<kSliceThreads>(a, r, red);
-  if (no_weights(g, e)) return;
-  for (int i = tid; i < kBins; i += kSliceThreads) {
-    hist_w[i] = 0;
-    hist_c[i] = 0;
-  }
-  if (tid == 0) n = 0;
-  fill_table(pow2);
-  const Scale c = scale_of(g, e, a.shift, pow2);
-  const bool count = g.k > 0 && g.k < a.vocab;
-  u64 min_w = 0;
-  slice_of<BF16>(a, r, blockIdx.x - r * a.slices).template each<kSliceThreads, 4>([&](float v, int i) {
-    const double ws = c.weight.scaled(v);
-    const u64 w = Weights::whole(ws);
-    if (w == 0) return;
-    const int b = c.bin_of(v);
-    atomicAdd(&hist_w[b], w);
-    if (count) atomicAdd(&hist_c[b], 1u);
-    if (ws >= c.least) min_w += w;
-    if (b < c.near && n < kSliceList) {
-      const uint32_t at = atomicAdd(&n, 1u);
-      if (at < kSliceList) list[at] = place_of(v, i);
+  const int first = s * a.slice_len;
+  const Logits<BF16> x(a.logits, (int64_t)(a.row0 + r) * a.stride, first, min(a.slice_len, a.vocab - first));
+  // the largest, the first run that holds it, and the least finite one
+  float top = -INFINITY, lo = INFINITY;
+  int at = first;
+  x.template each<8>([&](const auto& v) {
+    constexpr int N = sizeof v.x / 4;
+    float hi = v.x[0], least = v.x[0];
+#pragma unroll
+    for (int j = 1; j < N; ++j) {
+      hi = fmaxf(hi, v.x[j]);
+      least = fminf(least, v.x[j]);
     }
+    hi = fminf(hi, hi == hi ? FLT_MAX : -INFINITY);
+    if (hi > top || (N == 1 && hi == top && v.first < at)) {
+      top = hi;
+      at = v.first;
+    }
+    if (!(least > -INFINITY)) {  // masked ones among them
+      least = INFINITY;
+#pragma unroll
+      for (int j = 0; j < N; ++j) least = fminf(least, v.x[j] > -INFINITY ? v.x[j] : INFINITY);
+    }
+    lo = fminf(lo, least);
   });
-  min_w = block_reduce<kSliceThreads>(min_w, Sum(), red);
-  SampleState& st = a.state[r];
-  // (a slice whose list may have lost some counts as more than the row's list holds)
-  const uint32_t listed = n < kSliceList ? n : kNearList + 1;
-  if (tid == 0) {
-    if (min_w) atomicAdd(&st.min_w, min_w);
-    base = listed ? atomicAdd(&st.n, listed) : 0;
+  uint32_t* state = reinterpret_cast<uint32_t*>(a.state + r);
+  constexpr int words = offsetof(SampleState, near) / 4;
+  for (int i = s * kThreads + threadIdx.x; i < words; i += a.slices * kThreads) state[i] = 0;
+  const u64 t = wave_reduce(place_of(clean(top), at), Largest()), l = wave_reduce(place_of(clean(lo), 0), Least());
+  if ((threadIdx.x & 63) == 0) {
+    red[0][threadIdx.x >> 6] = t;
+    red[1][threadIdx.x >> 6] = l;
   }
   __syncthreads();
-  for (int i = tid; i < kBins; i += kSliceThreads) {
-    if (hist_w[i]) atomicAdd(&st.w[i], hist_w[i]);
-    if (hist_c[i]) atomicAdd(&st.c[i], hist_c[i]);
-  }
-  if (listed <= kSliceList)
-    for (int i = tid; i < (int)listed; i += kSliceThreads)
-      if (base + i < kNearList) st.list[base + i] = list[i];
+  if (threadIdx.x != 0) return;
+  SampleExtent e = {red[0][0], red[1][0]};
+  for (int w = 1; w < kWaves; ++w) e = {Largest()(e.top, red[0][w]), Least()(e.lo, red[1][w])};
+  // the element itself, in its run (a run of one, before the first or behind the last whole one, stands alone)
+  int i = index_of(e.top);
+  const float value = value_of(e.top);
+  while (i + 1 < first + x.n && clean(x.at(i)) != value) ++i;
+  e.top = place_of(value, i);
+  a.extents[blockIdx.x] = e;
 }
 
 // What is searched for: the first element whose running count reaches `count`, or
@@ -300,245 +322,572 @@ struct Target {
   }
 };
 
-struct Smem {
+// Running sums over a row's bins, in LDS.
+struct Bins {
   u64 w[kBins];
   uint32_t c[kBins];
-  u64 key[kList], sum[kList];
-  uint32_t cnt[kList];
-  u64 red[kRowThreads / 64];
-  double pow2[kSteps];
-  uint32_t n, found;
+  __device__ __forceinline__ u64 w_before(int b) const { return b ? w[b - 1] : 0; }
+  __device__ __forceinline__ uint32_t c_before(int b) const { return b ? c[b - 1] : 0; }
+  // The bin in which a target is met, the running sums before the first of them being (c0, w0).
+  __device__ __forceinline__ int met(const Target& t, uint32_t c0 = 0, u64 w0 = 0) const {
+    return first_met(kBins, [&](int i) { return t.met(c0 + c[i], w0 + w[i]); });
+  }
+  __device__ __forceinline__ void clear() {
+    for (int i = threadIdx.x; i < kBins; i += kThreads) {
+      w[i] = 0;
+      c[i] = 0;
+    }
+  }
+};
+constexpr int kOwnBins = kBins / kThreads;  // of a thread, one after the other
+// Each thread's bins into running sums.
+__device__ __forceinline__ void scan_bins(Bins& s, u64 (&w)[kOwnBins], uint32_t (&c)[kOwnBins], u64 (*red)[kWaves]) {
+#pragma unroll
+  for (int k = 1; k < kOwnBins; ++k) {
+    w[k] += w[k - 1];
+    c[k] += c[k - 1];
+  }
+  const u64 w0 = block_scan(w[kOwnBins - 1], red[0]) - w[kOwnBins - 1];
+  const uint32_t c0 = block_scan(c[kOwnBins - 1], red[1]) - c[kOwnBins - 1];
+#pragma unroll
+  for (int k = 0; k < kOwnBins; ++k) {
+    s.w[threadIdx.x * kOwnBins + k] = w0 + w[k];
+    s.c[threadIdx.x * kOwnBins + k] = c0 + c[k];
+  }
+  __syncthreads();
+}
+
+// A list of places, and the running weights of their elements once it is sorted.
+template <int SIZE>
+struct List {
+  u64 key[SIZE], sum[SIZE];
 };
 
-// The histogram into running sums.
-__device__ __forceinline__ void scan_hist(Smem& s) {
-  __syncthreads();
-  constexpr int PER = kBins / kRowThreads;
-  static_assert(PER == 2, "two bins a thread");
-  const int b = threadIdx.x * PER;
-  const u64 w0 = s.w[b], w1 = w0 + s.w[b + 1];
-  const uint32_t c0 = s.c[b], c1 = c0 + s.c[b + 1];
-  const u64 w = block_scan<kRowThreads>(w1, s.red) - w1;
-  const uint32_t c = block_scan<kRowThreads>(c1, s.red) - c1;
-  s.w[b] = w + w0;
-  s.w[b + 1] = w + w1;
-  s.c[b] = c + c0;
-  s.c[b + 1] = c + c1;
-  __syncthreads();
-}
-// Running sums before bin b.
-__device__ __forceinline__ u64 w_before(const Smem& s, int b) { return b ? s.w[b - 1] : 0; }
-__device__ __forceinline__ uint32_t c_before(const Smem& s, int b) { return b ? s.c[b - 1] : 0; }
-
-// The first of n > 0 places at which met(i) holds, the last where it does nowhere. (met grows with i.)
-template <typename F>
-__device__ __forceinline__ int first_met(Smem& s, int n, F&& met) {
-  if (threadIdx.x == 0) s.found = (uint32_t)(n - 1);
-  __syncthreads();
-  for (int i = threadIdx.x; i < n; i += kRowThreads)
-    if (met(i) && (i == 0 || !met(i - 1))) s.found = (uint32_t)i;
-  __syncthreads();
-  const int r = (int)s.found;
-  __syncthreads();
-  return r;
-}
-// The bin in which a target is met, the running sums before the first of them being (c0, w0).
-__device__ __forceinline__ int bin_met(Smem& s, const Target& t, uint32_t c0 = 0, u64 w0 = 0) {
-  return first_met(s, kBins, [&](int i) { return t.met(c0 + s.c[i], w0 + s.w[i]); });
-}
-
-// The s.n <= kList listed places into descending order.
-__device__ __forceinline__ void sort_list(Smem& s) {
-  const int n = (int)s.n, tid = threadIdx.x;
-  int len = 2;
-  while (len < n) len *= 2;
-  for (int i = n + tid; i < len; i += kRowThreads) s.key[i] = 0;
-  __syncthreads();
-  for (int size = 2; size <= len; size *= 2)
-    for (int d = size / 2; d >= 1; d /= 2) {
-      for (int t = tid; t < len / 2; t += kRowThreads) {
-        const int i = 2 * t - (t & (d - 1)), j = i + d;
-        const u64 a = s.key[i], b = s.key[j];
-        if ((a < b) == ((i & size) == 0)) {
-          s.key[i] = b;
-          s.key[j] = a;
+// A wave's 64 E places, element lane E + e of them in v[e], into descending order: a
+// bitonic network, by lane swaps down to a distance of E and in registers below. (The
+// loops stay rolled: such code runs once, at the rate at which it is fetched. 20 us
+// unrolled, E = 8.)
+template <int E>
+__device__ __forceinline__ void wave_sort(u64 (&v)[E]) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll 1
+  for (int size = 2; size <= 64 * E; size *= 2) {
+#pragma unroll 1
+    for (int d = size / 2; d >= E; d /= 2) {
+      const bool lower = (lane & (d / E)) == 0;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const u64 o = __shfl_xor(v[e], d / E);
+        const bool down = ((lane * E + e) & size) == 0;
+        if ((v[e] < o) == (lower == down)) v[e] = o;
+      }
+    }
+#pragma unroll
+    for (int d = E / 2; d >= 1; d /= 2) {
+      if (d >= size) continue;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        if (e & d) continue;
+        const bool down = ((lane * E + e) & size) == 0;
+        if ((v[e] < v[e | d]) == down) {
+          const u64 o = v[e];
+          v[e] = v[e | d];
+          v[e | d] = o;
         }
       }
-      __syncthreads();
     }
+  }
 }
-// Running sums of the sorted list into s.sum and s.cnt; gap(i, w, c) adds what stands
-// between element i and the one listed before it.
-template <typename G>
-__device__ __forceinline__ void scan_list(Smem& s, const Weights& weight, G&& gap) {
-  constexpr int PER = kList / kRowThreads;
-  const int n = (int)s.n, i0 = threadIdx.x * PER;
+// The n <= 256 E listed places (no two the same) into descending order: each wave sorts a
+// quarter, and every element goes to its place in the four quarters' order, which
+// binary searches in the others tell. (No barrier within a sort: 518 places 16 us as
+// one network over LDS.)
+template <int E, int SIZE>
+__device__ __forceinline__ void sort_list(List<SIZE>& s, int n) {
+  constexpr int N = 64 * E;
+  static_assert(kWaves * N <= SIZE, "a quarter a wave");
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  u64 v[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int i = wave * N + e * 64 + lane;
+    v[e] = i < n ? s.key[i] : 0;
+  }
+  wave_sort<E>(v);
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < E; ++e) s.key[wave * N + lane * E + e] = v[e];
+  __syncthreads();
+  // of each other quarter: how many are larger
+  int above[kWaves - 1][E] = {};
+#pragma unroll 1
+  for (int step = N; step >= 1; step /= 2)
+#pragma unroll
+    for (int o = 0; o < kWaves - 1; ++o)
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int to = above[o][e] + step;
+        if (to <= N && s.key[(wave + 1 + o) % kWaves * N + to - 1] > v[e]) above[o][e] = to;
+      }
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    int at = lane * E + e;
+#pragma unroll
+    for (int o = 0; o < kWaves - 1; ++o) at += above[o][e];
+    if (v[e]) s.sum[at] = v[e];
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += kThreads) s.key[i] = s.sum[i];
+  __syncthreads();
+}
+template <int SIZE>
+__device__ __forceinline__ void sort_any(List<SIZE>& s, int n) {
+  if (n <= kThreads) return sort_list<1>(s, n);
+  if constexpr (SIZE > kThreads) {
+    if (n <= 2 * kThreads) sort_list<2>(s, n);
+    else if (n <= 4 * kThreads) sort_list<4>(s, n);
+    else sort_list<SIZE / kThreads>(s, n);
+  }
+}
+// Running weights of the sorted list into s.sum; gap(i, w, c) adds what stands between
+// element i and the one listed before it. found: the first element whose running count
+// reaches `count`, n where there is none.
+template <int SIZE, typename G>
+__device__ __forceinline__ void scan_list(List<SIZE>& s, int n, const Scale& c, uint32_t count, uint32_t& found,
+                                          u64 (*red)[kWaves], G&& gap) {
+  const int per = (n + kThreads - 1) / kThreads, i0 = threadIdx.x * per, i1 = min(n, i0 + per);
+  if (threadIdx.x == 0) found = (uint32_t)n;
   u64 sum = 0;
   uint32_t cnt = 0;
-  for (int i = i0; i < min(n, i0 + PER); ++i) {
+  for (int i = i0; i < i1; ++i) {
     gap(i, sum, cnt);
-    sum += Weights::whole(weight.scaled(value_of(s.key[i])));
+    sum += c.weight_of(value_of(s.key[i]));
     ++cnt;
     s.sum[i] = sum;
-    s.cnt[i] = cnt;
   }
-  const u64 w = block_scan<kRowThreads>(sum, s.red) - sum;
-  const uint32_t c = block_scan<kRowThreads>(cnt, s.red) - cnt;
-  for (int i = i0; i < min(n, i0 + PER); ++i) {
-    s.sum[i] += w;
-    s.cnt[i] += c;
+  const u64 w0 = block_scan(sum, red[0]) - sum;
+  uint32_t c0 = block_scan(cnt, red[1]) - cnt;
+  for (int i = i0; i < i1; ++i) {
+    s.sum[i] += w0;
+    if (count) {
+      u64 none = 0;
+      gap(i, none, c0);
+      if (++c0 >= count) atomicMin(&found, (uint32_t)i);
+    }
   }
   __syncthreads();
 }
 
-// A row: the token, from its histogram and what has to be looked at of its elements.
+// Where a row's searches may end, given that the weights searched for are known up to the
+// bins of the searches before: bins [from, to] each, none if to < from.
+struct Search {
+  int k_bin, p_from, p_to, m_from, m_to, u_from, u_to;
+  __device__ __forceinline__ int last() const { return max(max(k_bin, p_to), max(m_to, u_to)); }
+  __device__ __forceinline__ bool wanted(int b) const {
+    return b == k_bin || (b >= p_from && b <= p_to) || (b >= m_from && b <= m_to) || (b >= u_from && b <= u_to);
+  }
+};
+__device__ __forceinline__ Search search_of(const Setting& g, const Scale& c, const Bins& s) {
+  Search h = {-1, 0, -1, 0, -1, 0, -1};
+  u64 lo = s.w[kBins - 1], hi = lo;  // of the kept weight
+  if (g.k > 0 && (uint32_t)g.k < s.c[kBins - 1]) {
+    h.k_bin = s.met({(uint32_t)g.k, 0.0, false});
+    lo = s.w_before(h.k_bin);
+    hi = s.w[h.k_bin];
+  }
+  if (g.p < 1.f) {
+    h.p_from = s.met({0, (double)g.p * (double)lo, false});
+    h.p_to = s.met({0, (double)g.p * (double)hi, false});
+    lo = s.w_before(h.p_from);
+    hi = s.w[h.p_to];
+  }
+  if (g.min_p > 0.f) {
+    // the logit at which a weight is min_p: its bin, and the next ones for what rounding does
+    const int b = g.min_p < 1.f ? c.bin_of(fmaxf(c.max + g.t * logf(g.min_p), -FLT_MAX)) : 0;
+    h.m_from = max(0, b - 1);
+    h.m_to = min(kBins - 1, b + 1);
+    if (s.w[h.m_to] <= lo) {  // min_p ends before the others
+      h.k_bin = -1;
+      h.p_from = 0;
+      h.p_to = -1;
+    } else if (s.w_before(h.m_from) >= hi) {  // or behind them
+      h.m_from = 0;
+      h.m_to = -1;
+    }
+    if (h.m_to >= h.m_from) {
+      lo = Least()(lo, s.w_before(h.m_from));
+      hi = Least()(hi, s.w[h.m_to]);
+    }
+  }
+  h.u_from = s.met({0, (double)g.u * (double)lo, true});
+  h.u_to = s.met({0, (double)g.u * (double)hi, true});
+  return h;
+}
+
+struct Pick {
+  u64 place, kept_w;
+  bool some;  // (min_p above 1 keeps nothing but the first token)
+};
+__device__ __forceinline__ void answer(const SampleArgs& a, int r, const Scale& c, const Pick& f) {
+  if (threadIdx.x != 0) return;
+  a.tokens[r] = index_of(f.place);
+  if (a.probs) a.probs[r] = f.some ? (float)(c.weights.scaled(c.clamp(value_of(f.place))) / (double)f.kept_w) : 1.f;
+}
+// As pick_listed, of at most 64 elements: all in the registers of a wave (every wave does
+// the same), with no barrier.
+template <int SIZE, typename W, typename C>
+__device__ __forceinline__ Pick pick_few(List<SIZE>& s, int n, const Setting& g, const Scale& c, const Search& h,
+                                         W&& w_before, C&& c_before) {
+  const int lane = threadIdx.x & 63;
+  u64 place = lane < n ? s.key[lane] : 0;
+  int rank = 0;
+#pragma unroll 1
+  for (int j = 0; j < n; ++j) rank += s.key[j] > place;
+  __syncthreads();
+  if (threadIdx.x < n) s.key[rank] = place;
+  __syncthreads();
+  place = s.key[min(lane, n - 1)];
+  const float x = value_of(place);
+  const int b = c.bin_of(x);
+  int before = __shfl_up(b, 1);
+  if (lane == 0) before = -1;
+  const u64 own = lane < n ? c.weight_of(x) : 0;
+  u64 sum = own;
+  uint32_t cnt = lane < n;
+  if (b != before) {
+    sum += w_before(b) - w_before(before + 1);
+    cnt += c_before(b) - c_before(before + 1);
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const u64 w = __shfl_up(sum, d);
+    const uint32_t k = __shfl_up(cnt, d);
+    if (lane >= d) {
+      sum += w;
+      cnt += k;
+    }
+  }
+  // the first of the elements that does, the last where none does
+  auto first = [&](bool does) {
+    const u64 m = __ballot(does && lane < n);
+    return m ? __ffsll(m) - 1 : n - 1;
+  };
+  Pick f = {0, w_before(kBins), true};
+  if (h.k_bin >= 0) f.kept_w = __shfl(sum, first(cnt >= (uint32_t)g.k));
+  if (h.p_to >= h.p_from) f.kept_w = __shfl(sum, first((double)sum >= (double)g.p * (double)f.kept_w));
+  if (h.m_to >= h.m_from) {
+    const bool keeps = c.weights.scaled(c.clamp(x)) >= ldexp((double)g.min_p, c.shift);
+    const int j = first(!keeps);
+    const u64 all = w_before(h.m_to + 1), m = __shfl((int)keeps, j) ? all : Least()(all, __shfl(sum - own, j));
+    f.some = m > 0;
+    f.kept_w = Least()(f.kept_w, m);
+  }
+  f.place = __shfl(place, first((double)sum > (double)g.u * (double)f.kept_w));
+  return f;
+}
+// The token, from the n listed elements of the wanted bins. w_before, c_before(b): running sums.
+template <int SIZE, typename W, typename C>
+__device__ __forceinline__ Pick pick_listed(List<SIZE>& s, int n, const Setting& g, const Scale& c, const Search& h,
+                                            uint32_t& found, u64 (*red)[kWaves], W&& w_before, C&& c_before) {
+  n = max(n, 1);  // (the element drawn is always there)
+  if (n <= 64) return pick_few(s, n, g, c, h, w_before, c_before);
+  sort_any(s, n);
+  auto bin_at = [&](int i) { return c.bin_of(value_of(s.key[i])); };
+  scan_list(s, n, c, h.k_bin >= 0 ? (uint32_t)g.k : 0u, found, red, [&](int i, u64& w, uint32_t& cnt) {
+    const int b = bin_at(i), before = i ? bin_at(i - 1) : -1;
+    if (b == before) return;
+    w += w_before(b) - w_before(before + 1);
+    cnt += c_before(b) - c_before(before + 1);
+  });
+  Pick f = {0, w_before(kBins), true};
+  if (h.k_bin >= 0) f.kept_w = s.sum[min((int)found, n - 1)];
+  if (h.p_to >= h.p_from) {
+    const double want = (double)g.p * (double)f.kept_w;
+    f.kept_w = s.sum[first_met(n, [&](int i) { return (double)s.sum[i] >= want; })];
+  }
+  if (h.m_to >= h.m_from) {
+    // the elements that min_p keeps come first
+    const double least = ldexp((double)g.min_p, c.shift);
+    auto keeps = [&](int i) { return c.weights.scaled(c.clamp(value_of(s.key[i]))) >= least; };
+    const int j = first_met(n, [&](int i) { return !keeps(i); });
+    const u64 all = w_before(h.m_to + 1), m = keeps(j) ? all : Least()(all, s.sum[j] - c.weight_of(value_of(s.key[j])));
+    f.some = m > 0;
+    f.kept_w = Least()(f.kept_w, m);
+  }
+  const double want = (double)g.u * (double)f.kept_w;
+  f.place = s.key[first_met(n, [&](int i) { return (double)s.sum[i] > want; })];
+  return f;
+}
+
+// Stores and loads of what another workgroup of the same launch reads or has written: past
+// the L2s (agent scope), so that a ticket need only wait for them to arrive. A fence would
+// write back all of an L2, 20 us of it.
+template <typename T>
+__device__ __forceinline__ void put(T* p, T v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+template <typename T>
+__device__ __forceinline__ T get(const T* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+// Whether this workgroup is the last of n to come here. With barriers.
+__device__ __forceinline__ bool last_of(uint32_t n, uint32_t* tickets, uint32_t& mine) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // each wave's own stores and atomics have arrived
+  __syncthreads();
+  if (threadIdx.x == 0) mine = atomicAdd(tickets, 1u);
+  __syncthreads();
+  return mine == n - 1;
+}
+
+// A slice of a row: its weights into the row's histogram, its likely tokens into the
+// row's list. The last of the row's workgroups to be done draws the token, or leaves
+// what it has found out to the next kernel where the listed tokens do not tell.
 template <bool BF16>
-__global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(SampleArgs a) {
-  extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-  Smem& s = *reinterpret_cast<Smem*>(smem);
-  const int r = blockIdx.x, out = a.row0 + r, tid = threadIdx.x;
+__global__ __launch_bounds__(kThreads) void sample_weights_kernel(SampleArgs a) {
+  __shared__ __attribute__((aligned(16))) Bins bins;
+  __shared__ List<kSampleNear> list;
+  __shared__ u64 red[2][kWaves];
+  __shared__ double pow2[kSteps];
+  __shared__ uint32_t n, base;
+  const int r = blockIdx.x / a.slices, out = a.row0 + r, slice = blockIdx.x - r * a.slices, tid = threadIdx.x;
   const Setting g = setting_of(a, out);
-  const Extent e = row_extent<kRowThreads>(a, r, s.red);
+  const Extent e = row_extent(a, r);
   if (no_weights(g, e)) {
     const bool none = value_of(e.top) == -INFINITY;
-    if (tid == 0) {
+    if (tid == 0 && slice == 0) {
       a.tokens[out] = none ? 0 : index_of(e.top);
       if (a.probs) a.probs[out] = none ? 0.f : 1.f;
     }
     return;
   }
-  const SampleState& st = a.state[r];
-  for (int i = tid; i < kBins; i += kRowThreads) {
-    s.w[i] = st.w[i];
-    s.c[i] = st.c[i];
+  bins.clear();
+  if (tid == 0) n = 0;
+  fill_table(pow2, a.shift);
+  const Scale c = scale_of(g, e, a.shift, pow2);
+  const bool count = g.k > 0 && g.k < a.vocab;
+  __syncthreads();
+  const int first = slice * a.slice_len;
+  const Logits<BF16> x(a.logits, (int64_t)out * a.stride, first, min(a.slice_len, a.vocab - first));
+  // (a run's weights are formed together, with their reads of the table in flight together)
+  auto add = [&](auto far, const auto& v) {
+    constexpr int N = sizeof v.x / 4;
+    u64 w[N];
+    int b[N], least = kBins;
+#pragma unroll
+    for (int j = 0; j < N; ++j) w[j] = c.weight<decltype(far)::value>(v.x[j]);
+#pragma unroll
+    for (int j = 0; j < N; ++j) b[j] = c.bin_of(v.x[j]);
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (w[j]) {
+        atomicAdd(&bins.w[b[j]], w[j]);
+        least = min(least, b[j]);
+      }
+    if (count) {
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (w[j]) atomicAdd(&bins.c[b[j]], 1u);
+    }
+    if (least < c.near && n < kNearList) {
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (w[j] && b[j] < c.near) {
+          const uint32_t at = atomicAdd(&n, 1u);
+          if (at < kNearList) list.key[at] = place_of(clean(v.x[j]), v.first + j);
+        }
+    }
+  };
+  if (c.far) x.template each<2>([&](const auto& v) { add(std::true_type{}, v); });
+  else x.template each<4>([&](const auto& v) { add(std::false_type{}, v); });
+  __syncthreads();
+  SampleState& st = a.state[r];
+  // (a slice whose list may have lost some counts as more than the row's list holds)
+  const uint32_t mine = n < kNearList ? n : kNearList + 1;
+  if (tid == 0) base = mine ? atomicAdd(&st.n_near, mine) : 0;
+  for (int i = tid; i < kBins; i += kThreads) {
+    if (bins.w[i]) atomicAdd(&st.w[i], bins.w[i]);
+    if (bins.c[i]) atomicAdd(&st.c[i], bins.c[i]);
   }
-  const u64 min_w = st.min_w;
-  const uint32_t listed = st.n;
-  fill_table(s.pow2);
-  const Scale c = scale_of(g, e, a.shift, s.pow2);
-  scan_hist(s);
-  // The bins that each search may end in, given that the weights searched for are
-  // known up to the bins of the searches before: [from, to] each, none if to < from.
-  const u64 all_w = s.w[kBins - 1];
-  const bool by_k = g.k > 0 && (uint32_t)g.k < s.c[kBins - 1], by_p = g.p < 1.f;
-  int k_bin = -1, p_from = 0, p_to = -1;
-  u64 lo = all_w, hi = all_w;  // of the kept weight
-  if (by_k) {
-    k_bin = bin_met(s, {(uint32_t)g.k, 0.0, false});
-    lo = w_before(s, k_bin);
-    hi = s.w[k_bin];
+  __syncthreads();
+  if (mine <= kNearList)
+    for (int i = tid; i < (int)mine; i += kThreads)
+      if (base + i < kNearList) put(&st.near[base + i], list.key[i]);
+  if (!last_of(a.slices, &st.slices_done, base)) return;
+
+  u64 own_w[kOwnBins];
+  uint32_t own_c[kOwnBins];
+#pragma unroll
+  for (int k = 0; k < kOwnBins; ++k) {
+    own_w[k] = get(&st.w[tid * kOwnBins + k]);
+    own_c[k] = get(&st.c[tid * kOwnBins + k]);
   }
-  if (by_p) {
-    p_from = bin_met(s, {0, (double)g.p * (double)lo, false});
-    p_to = bin_met(s, {0, (double)g.p * (double)hi, false});
-    lo = w_before(s, p_from);
-    hi = s.w[p_to];
+  const uint32_t listed = get(&st.n_near);
+  if (tid == 0) n = 0;
+  scan_bins(bins, own_w, own_c, red);
+  const Search h = search_of(g, c, bins);
+  if (listed > kNearList || h.last() >= c.near) {
+    // running sums, for the next kernel, and where to look
+#pragma unroll
+    for (int k = 0; k < kOwnBins; ++k) {
+      st.w[tid * kOwnBins + k] = bins.w[tid * kOwnBins + k];
+      st.c[tid * kOwnBins + k] = bins.c[tid * kOwnBins + k];
+    }
+    if (tid == 0) {
+      st.search[0] = h.k_bin; st.search[1] = h.p_from; st.search[2] = h.p_to; st.search[3] = h.m_from;
+      st.search[4] = h.m_to;  st.search[5] = h.u_from; st.search[6] = h.u_to;
+      st.pending = 1;
+    }
+    return;
   }
-  if (min_w <= lo) {  // min_p ends before them
-    k_bin = -1;
-    p_from = 0;
-    p_to = -1;
+  for (int i = tid; i < (int)listed; i += kThreads) {
+    const u64 q = get(&st.near[i]);
+    if (h.wanted(c.bin_of(value_of(q)))) list.key[atomicAdd(&n, 1u)] = q;
   }
-  lo = Least()(lo, min_w);
-  hi = Least()(hi, min_w);
-  const int u_from = bin_met(s, {0, (double)g.u * (double)lo, true});
-  const int u_to = bin_met(s, {0, (double)g.u * (double)hi, true});
-  auto wanted = [&](int b) { return b == k_bin || (b >= p_from && b <= p_to) || (b >= u_from && b <= u_to); };
-  const Logits<BF16> x(a.logits, (int64_t)out * a.stride, 0, a.vocab);
-  // List the elements that take(value, index) wants and that have weight; s.n counts
-  // all of them, and the first kList to arrive are there.
-  auto gather = [&](auto&& take) {
-    if (tid == 0) s.n = 0;
-    __syncthreads();
-    x.template each<kRowThreads, 8>([&](float v, int i) {
-      if (!take(v, i) || Weights::whole(c.weight.scaled(v)) == 0) return;
-      const uint32_t at = atomicAdd(&s.n, 1u);
-      if (at < kList) s.key[at] = place_of(v, i);
+  __syncthreads();
+  const Pick f = pick_listed(
+      list, (int)n, g, c, h, base, red, [&](int b) { return bins.w_before(b); }, [&](int b) { return bins.c_before(b); });
+  answer(a, out, c, f);
+}
+
+// A part of a row that the kernel before left: its elements of the wanted bins. The last
+// of the row's workgroups draws the token from them.
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void sample_rest_kernel(SampleArgs a) {
+  __shared__ union {
+    List<kList> list;
+    Bins bins;
+  } s;
+  __shared__ u64 red[2][kWaves];
+  __shared__ double pow2[kSteps];
+  __shared__ uint32_t n, base;
+  const int r = blockIdx.x / a.parts, out = a.row0 + r, tid = threadIdx.x;
+  SampleState& st = a.state[r];
+  if (!const_load(&st.pending)) return;
+  const Search h = {st.search[0], st.search[1], st.search[2], st.search[3], st.search[4], st.search[5], st.search[6]};
+  const Setting g = setting_of(a, out);
+  const Extent e = row_extent(a, r);
+  fill_table(pow2, a.shift);
+  const Scale c = scale_of(g, e, a.shift, pow2);
+  if (tid == 0) n = 0;
+  __syncthreads();
+  // List the elements that take(value, index) wants; n (0 before) counts all of them, and
+  // the first kList to arrive are there.
+  auto gather = [&](const Logits<BF16>& x, auto&& take) {
+    x.template each<8>([&](const auto& v) {
+      constexpr int N = sizeof v.x / 4;
+      bool any = false, takes[N];
+#pragma unroll
+      for (int j = 0; j < N; ++j) any |= takes[j] = take(v.x[j], v.first + j);
+      if (!any) return;
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (takes[j]) {
+          const uint32_t at = atomicAdd(&n, 1u);
+          if (at < kList) s.list.key[at] = place_of(clean(v.x[j]), v.first + j);
+        }
     });
     __syncthreads();
   };
-  const int last = max(max(k_bin, p_to), u_to);
-  if (listed <= kNearList && last < c.near) {
-    if (tid == 0) s.n = 0;
+  // Of the part: wanted(bin_of(v)), as ranges of what bin_of rounds down. The elements at
+  // the cut have no weight.
+  const int first = (blockIdx.x - r * a.parts) * a.part_len;
+  const float least_v = c.far ? -INFINITY : c.cut, end = INFINITY;
+  auto above = [&](int to) { return to == kBins - 1 ? end : (float)(to + 1); };  // (the last bin holds all that is further away)
+  const float f0 = h.k_bin < 0 ? end : h.k_bin, f1 = above(h.k_bin), f2 = h.p_to < h.p_from ? end : h.p_from;
+  const float f3 = above(h.p_to), f4 = h.m_to < h.m_from ? end : h.m_from, f5 = above(h.m_to);
+  const float f6 = h.u_from, f7 = above(h.u_to);
+  gather(Logits<BF16>(a.logits, (int64_t)out * a.stride, first, max(0, min(a.part_len, a.vocab - first))), [&](float v, int) {
+    const float b = (c.max - c.clamp(v)) * c.per;
+    return (v > least_v) & (((b >= f0) & (b < f1)) | ((b >= f2) & (b < f3)) | ((b >= f4) & (b < f5)) | ((b >= f6) & (b < f7)));
+  });
+  const uint32_t mine = n;
+  if (tid == 0) base = mine ? atomicAdd(&st.n_list, mine) : 0;
+  __syncthreads();
+  for (uint32_t i = tid; i < min(mine, (uint32_t)kList); i += kThreads)
+    if (base + i < kList) put(&st.list[base + i], s.list.key[i]);
+  if (!last_of(a.parts, &st.parts_done, base)) return;
+  const uint32_t all = get(&st.n_list);
+  if (all <= kList) {
+    for (int i = tid; i < (int)all; i += kThreads) s.list.key[i] = get(&st.list[i]);
     __syncthreads();
-    for (int i = tid; i < (int)listed; i += kRowThreads) {
-      const u64 q = st.list[i];
-      if (wanted(c.bin_of(value_of(q)))) s.key[atomicAdd(&s.n, 1u)] = q;
-    }
-    __syncthreads();
-  } else {
-    gather([&](float v, int) { return wanted(c.bin_of(v)); });
+    const Pick f = pick_listed(
+        s.list, (int)all, g, c, h, base, red, [&](int b) { return b ? st.w[b - 1] : 0; },
+        [&](int b) { return b ? st.c[b - 1] : 0; });
+    answer(a, out, c, f);
+    return;
   }
-  u64 kept_w = all_w, place = 0;
-  if (s.n <= kList) {
-    sort_list(s);
-    auto bin_at = [&](int i) { return c.bin_of(value_of(s.key[i])); };
-    scan_list(s, c.weight, [&](int i, u64& w, uint32_t& n) {
-      const int b = bin_at(i), before = i ? bin_at(i - 1) : -1;
-      if (b == before) return;
-      w += w_before(s, b) - w_before(s, before + 1);
-      n += c_before(s, b) - c_before(s, before + 1);
-    });
-    const int n = (int)s.n;
-    if (k_bin >= 0) kept_w = s.sum[first_met(s, n, [&](int i) { return s.cnt[i] >= (uint32_t)g.k; })];
-    if (p_to >= p_from) {
-      const double want = (double)g.p * (double)kept_w;
-      kept_w = s.sum[first_met(s, n, [&](int i) { return (double)s.sum[i] >= want; })];
-    }
-    kept_w = Least()(kept_w, min_w);
-    const double want = (double)g.u * (double)kept_w;
-    place = s.key[first_met(s, n, [&](int i) { return (double)s.sum[i] > want; })];
-  } else {
-    // Bins that hold more than the list (many equal logits): each search narrows the
-    // places by histograms of its own until the list holds what is left.
-    for (int stage = by_k ? 0 : by_p ? 1 : 2; stage < 3; ++stage) {
-      if (stage == 1 && !by_p) continue;
-      if (stage == 2) kept_w = Least()(kept_w, min_w);
-      const Target t = {stage == 0 ? (uint32_t)g.k : 0u, (double)(stage == 1 ? g.p : g.u) * (double)kept_w, stage == 2};
-      u64 to = e.top, from = place_of(e.lo, 0x7FFFFFFF), w0 = 0;
-      uint32_t c0 = 0, n = kList + 1;
-      while (n > kList) {
-        int sh = 0;
-        while (((to - from) >> sh) >= kBins) ++sh;
-        __syncthreads();
-        for (int i = tid; i < kBins; i += kRowThreads) {
-          s.w[i] = 0;
-          s.c[i] = 0;
-        }
-        __syncthreads();
-        x.template each<kRowThreads, 8>([&](float v, int i) {
-          const u64 q = place_of(v, i);
-          if (q < from || q > to) return;
-          const u64 w = Weights::whole(c.weight.scaled(v));
-          if (w == 0) return;
-          const int b = (int)((to - q) >> sh);
-          atomicAdd(&s.w[b], w);
-          atomicAdd(&s.c[b], 1u);
-        });
-        scan_hist(s);
-        const int b = bin_met(s, t, c0, w0);
-        n = s.c[b] - c_before(s, b);
-        c0 += c_before(s, b);
-        w0 += w_before(s, b);
-        to -= (u64)b << sh;
-        const u64 span = ((u64)1 << sh) - 1;
-        from = to - from > span ? to - span : from;
+  // Bins that hold more than the list (many equal logits): each search narrows the
+  // places by histograms of its own until the list holds what is left.
+  const Logits<BF16> x(a.logits, (int64_t)out * a.stride, 0, a.vocab);
+  const double least = ldexp((double)g.min_p, a.shift);
+  const bool by_k = g.k > 0 && (uint32_t)g.k < st.c[kBins - 1], by_p = g.p < 1.f, by_m = g.min_p > 0.f;
+  Pick f = {0, st.w[kBins - 1], true};
+  u64 min_w = f.kept_w;
+  if (by_m) {
+    u64 sum = 0;
+    x.template each<2>([&](const auto& v) {
+      for (const float y : v.x) {
+        const u64 w = c.weight_of(y);
+        if (w && c.weights.scaled(c.clamp(y)) >= least) sum += w;
       }
-      gather([&](float v, int i) {
-        const u64 q = place_of(v, i);
-        return q >= from && q <= to;
-      });
-      sort_list(s);
-      scan_list(s, c.weight, [](int, u64&, uint32_t&) {});
-      const int j = first_met(s, (int)s.n, [&](int i) { return t.met(c0 + s.cnt[i], w0 + s.sum[i]); });
-      place = s.key[j];
-      kept_w = stage < 2 ? w0 + s.sum[j] : kept_w;
-    }
+    });
+    sum = wave_reduce(sum, Sum());
+    if ((tid & 63) == 0) red[0][tid >> 6] = sum;
+    __syncthreads();
+    min_w = red[0][0] + red[0][1] + red[0][2] + red[0][3];
+    f.some = min_w > 0;
   }
-  if (tid != 0) return;
-  a.tokens[out] = index_of(place);
-  // (min_p above 1 keeps nothing but the first token)
-  if (a.probs) a.probs[out] = min_w ? (float)(c.weight.scaled(value_of(place)) / (double)kept_w) : 1.f;
+  for (int stage = by_k ? 0 : by_p ? 1 : 2; stage < 3; ++stage) {
+    if (stage == 1 && !by_p) continue;
+    if (stage == 2) f.kept_w = Least()(f.kept_w, min_w);
+    const Target t = {stage == 0 ? (uint32_t)g.k : 0u, (double)(stage == 1 ? g.p : g.u) * (double)f.kept_w, stage == 2};
+    u64 to = e.top, from = place_of(e.lo, 0x7FFFFFFF), w0 = 0;
+    uint32_t c0 = 0, left = kList + 1;
+    while (left > kList) {
+      int sh = 0;
+      while (((to - from) >> sh) >= kBins) ++sh;
+      __syncthreads();
+      s.bins.clear();
+      __syncthreads();
+      x.template each<2>([&](const auto& v) {
+        for (int j = 0; j < (int)(sizeof v.x / 4); ++j) {
+          const u64 q = place_of(clean(v.x[j]), v.first + j);
+          if (q < from || q > to) continue;
+          const u64 w = c.weight_of(v.x[j]);
+          if (w == 0) continue;
+          const int b = (int)((to - q) >> sh);
+          atomicAdd(&s.bins.w[b], w);
+          atomicAdd(&s.bins.c[b], 1u);
+        }
+      });
+      __syncthreads();
+      u64 own_w[kOwnBins];
+      uint32_t own_c[kOwnBins];
+#pragma unroll
+      for (int k = 0; k < kOwnBins; ++k) {
+        own_w[k] = s.bins.w[tid * kOwnBins + k];
+        own_c[k] = s.bins.c[tid * kOwnBins + k];
+      }
+      scan_bins(s.bins, own_w, own_c, red);
+      const int b = s.bins.met(t, c0, w0);
+      left = s.bins.c[b] - s.bins.c_before(b);
+      c0 += s.bins.c_before(b);
+      w0 += s.bins.w_before(b);
+      to -= (u64)b << sh;
+      const u64 span = ((u64)1 << sh) - 1;
+      from = to - from > span ? to - span : from;
+    }
+    __syncthreads();
+    if (tid == 0) n = 0;
+    __syncthreads();
+    gather(x, [&](float v, int i) {
+      const u64 q = place_of(clean(v), i);
+      return q >= from && q <= to && c.weight_of(v) != 0;
+    });
+    const int m = (int)min(n, (uint32_t)kList);
+    sort_any(s.list, m);
+    scan_list(s.list, m, c, stage == 0 ? (uint32_t)g.k - c0 : 0u, base, red, [](int, u64&, uint32_t&) {});
+    const int j = stage == 0 ? min((int)base, m - 1) : first_met(m, [&](int i) { return t.met(0, w0 + s.list.sum[i]); });
+    f.place = s.list.key[j];
+    if (stage < 2) f.kept_w = w0 + s.list.sum[j];
+  }
+  answer(a, out, c, f);
 }
 
 }  // namespace
@@ -551,16 +900,14 @@ void launch_sample(hipStream_t s, SampleArgs a) {
   for (a.row0 = 0; a.row0 < rows; a.row0 += kSampleRows) {
     a.rows = std::min(rows - a.row0, kSampleRows);
     sample_slices(a.rows, a.vocab, &a.slices, &a.slice_len);
-    auto go = [&](auto extent, auto weights, auto pick, std::atomic<uint64_t>& raised) {
-      static_assert(sizeof(Smem) <= 160 * 1024, "LDS of a CU");
-      raise_dynamic_lds(reinterpret_cast<const void*>(pick), sizeof(Smem), raised);
-      extent<<<a.rows * a.slices, kSliceThreads, 0, s>>>(a);
-      weights<<<a.rows * a.slices, kSliceThreads, 0, s>>>(a);
-      pick<<<a.rows, kRowThreads, sizeof(Smem), s>>>(a);
+    sample_parts(a.rows, a.vocab, &a.parts, &a.part_len);
+    auto go = [&](auto bf16) {
+      constexpr bool B = decltype(bf16)::value;
+      sample_extent_kernel<B><<<a.rows * a.slices, kThreads, 0, s>>>(a);
+      sample_weights_kernel<B><<<a.rows * a.slices, kThreads, 0, s>>>(a);
+      sample_rest_kernel<B><<<a.rows * a.parts, kThreads, 0, s>>>(a);
     };
-    static std::atomic<uint64_t> raised_f32{0}, raised_bf16{0};
-    if (a.bf16) go(&sample_extent_kernel<true>, &sample_weights_kernel<true>, &sample_pick_kernel<true>, raised_bf16);
-    else go(&sample_extent_kernel<false>, &sample_weights_kernel<false>, &sample_pick_kernel<false>, raised_f32);
+    a.bf16 ? go(std::true_type{}) : go(std::false_type{});
   }
 }
 
