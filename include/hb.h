@@ -297,9 +297,10 @@ typedef struct {
 /* hb_plan_attention for a batch in which groups of requests share a prefix: runs
  * read a shared prefix's keys and values once for all rows of its group and join
  * that with each row's own keys. The results are those of hb_plan_attention but
- * for the order in which a row's keys are added up; the same bits every time. A
- * request whose own rows fill half a matrix tile (chunk_len * n_q_heads /
- * n_kv_heads >= 64) reads its prefix by itself, as it would gain nothing.
+ * for the order in which a row's keys are added up; the same bits every time. Where
+ * nothing is gained each request reads its prefix by itself: behind prefixes too short
+ * for it, and where its own rows fill half a matrix tile (chunk_len * n_q_heads /
+ * n_kv_heads >= 64).
  *   groups  host [n_groups], ascending and disjoint; prefix_len a multiple of
  *           16, at most the context_len of every request of the group
  * No window. Errors: those of hb_plan_attention; HB_ERR_INVALID (null groups,

@@ -211,6 +211,7 @@ hb_status hb_create_attention(const hb_layer_config* cfg, int32_t num_blocks, vo
     if (const char* e = std::getenv("HB_ATTN_SPLIT_TILE")) a->opt.split_tile = std::atoi(e);
     if (const char* e = std::getenv("HB_ATTN_SPLIT_ITEM")) a->opt.split_item = std::atoi(e);
     if (const char* e = std::getenv("HB_ATTN_UNIT_BLOCK")) a->opt.unit_block = std::atoi(e);
+    if (const char* e = std::getenv("HB_ATTN_SHARE_ALL")) a->opt.share_all = std::atoi(e) != 0;
     for (PlanStage& s : a->stage)
       if (hipEventCreateWithFlags(&s.copied, hipEventDisableTiming) != hipSuccess)
         return bail(fail(HB_ERR_HIP, "hipEventCreate failed"));

@@ -426,38 +426,36 @@ static int fit_tile_split(const std::vector<int>& lengths, int nkv, int64_t slot
 // rest of it to the next. (Tiles share a key range four times less often: even
 // with cold caches, 19.8 -> 23.2 us with warm ones, 64 tiles of 1000 keys.)
 constexpr int kDies = 8;
+// units[at[i]] are dealt anew over the places `at`.
 template <typename F>
-static std::vector<int32_t> by_die(const std::vector<int32_t>& units, F&& item_of) {
-  const int n = (int)units.size();
+static void by_die(std::vector<int32_t>* units, const std::vector<int>& at, F&& item_of) {
   std::map<std::tuple<int, int, int>, int> known;
   std::vector<std::vector<int32_t>> groups;
-  for (const int32_t u : units) {
+  std::vector<int> places[kDies];
+  for (const int i : at) {
+    const int32_t u = (*units)[i];
     const AttnItem it = item_of(u);
-    const auto at = known.insert({{it.req, it.kv_head, it.kv_begin}, (int)groups.size()}).first;
-    if (at->second == (int)groups.size()) groups.emplace_back();
-    groups[at->second].push_back(u);
+    const auto found = known.insert({{it.req, it.kv_head, it.kv_begin}, (int)groups.size()}).first;
+    if (found->second == (int)groups.size()) groups.emplace_back();
+    groups[found->second].push_back(u);
+    places[i % kDies].push_back(i);
   }
   std::stable_sort(groups.begin(), groups.end(), [](const auto& a, const auto& b) { return a.size() > b.size(); });
-  int next[kDies], room[kDies];
-  for (int x = 0; x < kDies; ++x) {
-    next[x] = x;
-    room[x] = (n - x + kDies - 1) / kDies;
-  }
-  std::vector<int32_t> order(n);
+  size_t next[kDies] = {}, room[kDies];
+  for (int x = 0; x < kDies; ++x) room[x] = places[x].size();
   for (const auto& group : groups) {
-    int x = 0, left = 0;
+    int x = 0;
+    size_t left = 0;
     for (const int32_t u : group) {
       if (left == 0) {
         x = (int)(std::max_element(room, room + kDies) - room);
         left = room[x];
       }
-      order[next[x]] = u;
-      next[x] += kDies;
+      (*units)[places[x][next[x]++]] = u;
       --room[x];
       --left;
     }
   }
-  return order;
 }
 
 namespace {
@@ -479,14 +477,24 @@ struct Run {
   int64_t base = 0;
 };
 
-// The requests of a group that are joined, as runs of consecutive ones.
+// The requests of a group that are joined, as runs of consecutive ones. Joined rows
+// need the merge kernel (2.5 to 3 us); requests alone need it from some 600 keys on, or
+// where launches are large. So joining pays from 1024 shared keys on (cold caches, one
+// call, alone / joined: 2 decodes of 8B heads behind 512 keys 6.9 / 9.6 us, 1024 10.3 /
+// 9.1, 8192 13.8 / 12.6; 64 behind 1024 19.2 / 16.2, 8192 137 / 24) or where it saves
+// as many K and V bytes as these take to read (64 behind 512: eight kv heads, 132 MB,
+// 13.3 / 15.3; sixteen, 264 MB, 19.3 / 16.6).
+constexpr int kSharedKeys = 1024;
+constexpr double kSharedBytes = 192e6;
 std::vector<Run> shared_runs(const Dims& d, const hb_request* rq, const PlanOptions& opt) {
   std::vector<Run> runs;
   for (int i = 0; i < opt.n_groups; ++i) {
     const hb_prefix_group& g = opt.groups[i];
     int rows = 0, first = g.first;
     auto close = [&](int end) {
-      if (end - first > 1 && g.prefix_len > 0) runs.push_back({first, end - first, g.prefix_len, rows});
+      const double saved = (end - first - 1.0) * g.prefix_len * 4 * d.nkv * d.hd;
+      if (end - first > 1 && g.prefix_len > 0 && (opt.share_all || g.prefix_len >= kSharedKeys || saved >= kSharedBytes))
+        runs.push_back({first, end - first, g.prefix_len, rows});
       first = end + 1;
       rows = 0;
     };
@@ -658,6 +666,19 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   const int S_t = opt.split_tile > 0 ? round_up(opt.split_tile, 64) : S_t_fit > 0 ? S_t_fit : S_t_auto;
   p->split_tile = S_t;
   p->split_item = S_i;
+  // A shared prefix's tiles: as many pieces as make one for each CU, all tiles taken
+  // together (cold caches, 8B heads: 64 decodes behind 8192 shared keys, 16 tiles, 16
+  // pieces each 24.3 us, 8 29.6, 32 29.3; 256 behind 16384 and up to 1000 of their own,
+  // 64 tiles, 4 pieces 127, 8 140, 6 146, 16 167), but, beside items, none shorter than
+  // what takes 0.6 of their time (64 behind 8192 and up to 2000 of their own: 6 pieces
+  // 55.2, 5 63.5, 8 58.5, 16 65.9), and no finer than other tiles' parts (fit_tile_split).
+  auto prefix_split = [&](int keys) {
+    const double finest = std::max(3.0 * std::sqrt((double)keys), tile_keys / cus);
+    const double least = item_keys * 4.0 * d.hd / kItemBytesPerUs * 32.0;
+    const int n = (int)std::max(1.0, std::min(std::floor(keys / finest + 1e-6), std::ceil(keys / std::max(least, 64.0))));
+    return round_up((keys + n - 1) / n, 64);
+  };
+  auto tile_split = [&](const Span& s) { return s.end >= 0 && opt.split_tile <= 0 ? prefix_split(s.end - s.lo) : S_t; };
 
   // Tiles: one work unit per (request, kv head, position block, key split).
   // Items: a (request, kv head, position group) whose keys fit one split
@@ -677,13 +698,14 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   std::vector<Unit> merged_units;
   struct SplitTile {
     int first, n, begin, end;  // its pieces are tiles[first .. first + n), over these keys
+    bool shared;
   };
   std::vector<SplitTile> split_tiles;
   std::vector<MergeGroup> groups;
   int slots = 0;
   // units that a range of `len` keys takes one after the other (for a wave alone: one)
-  auto parts_of = [&](bool tile, int len) {
-    const int nspl = (len + (tile ? S_t : S_i) - 1) / (tile ? S_t : S_i);
+  auto parts_of = [&](bool tile, int len, int split) {
+    const int nspl = (len + split - 1) / split;
     return tile ? nspl : len <= S_1 ? 1 : (nspl + kItemsPerUnit - 1) / kItemsPerUnit;
   };
   // slots of the shared runs, every unit of which leaves parts
@@ -691,8 +713,8 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   for (const Span& s : spans) {
     if (s.run < 0) continue;
     Run& u = runs[s.run];
-    if (s.end >= 0) u.parts = u.prefix_parts = parts_of(is_tile(s), s.end - s.lo);
-    else u.parts = std::max(u.parts, u.prefix_parts + parts_of(false, range_len(s, s.rows - 1, 1)));
+    if (s.end >= 0) u.parts = u.prefix_parts = parts_of(is_tile(s), s.end - s.lo, is_tile(s) ? tile_split(s) : S_i);
+    else u.parts = std::max(u.parts, u.prefix_parts + parts_of(false, range_len(s, s.rows - 1, 1), S_i));
   }
   int64_t run_rows = 0;
   for (Run& u : runs) {
@@ -709,14 +731,14 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   for (const Span& sp : spans) {
     const int r = sp.r, c = sp.rows, x = sp.x;
     const bool tile = is_tile(sp);
-    const int w = !tile ? d.P : p->half_tiles ? d.BQ / 2 : d.BQ, S = tile ? S_t : S_i;
+    const int w = !tile ? d.P : p->half_tiles ? d.BQ / 2 : d.BQ, S = tile ? tile_split(sp) : S_i;
     for (int g = 0; g < d.nkv; ++g) {
       for (int i0 = 0; i0 < c; i0 += w) {
         const int npos = std::min(w, c - i0), tok0 = sp.tok0 + i0;
         const int gap = 16 * dead_blocks(win, x + i0).count;
         const int pos0 = sp.end >= 0 ? x : x + i0 - gap, kv_end = sp.end >= 0 ? sp.end : pos0 + npos;
         const int kv_len = kv_end - sp.lo;
-        const int nspl = (kv_len + S - 1) / S, k = parts_of(tile, kv_len);
+        const int nspl = (kv_len + S - 1) / S, k = parts_of(tile, kv_len, S);
         // where the unit's parts go: the first one's slots, and those between two of them
         int part0 = -1, stride = 0;
         if (sp.run >= 0) {
@@ -735,7 +757,7 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
           slots += k * stride;
         }
         if (tile) {
-          if (nspl > 1) split_tiles.push_back({(int)tiles.size(), nspl, sp.lo, kv_end});
+          if (nspl > 1) split_tiles.push_back({(int)tiles.size(), nspl, sp.lo, kv_end, sp.end >= 0});
           for (int s = 0; s < nspl; ++s)
             tiles.push_back({r, g, tok0, pos0, npos, sp.lo + s * S, std::min(kv_end, sp.lo + (s + 1) * S),
                              part0 < 0 ? -1 : part0 + s * stride});
@@ -766,8 +788,11 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
   // than slots, even pieces would add long units to the queue; the short
   // last pieces fill gaps there.
   const int64_t item_unit_count = (int64_t)merged_units.size() + ((int64_t)singles.size() + kItemsPerUnit - 1) / kItemsPerUnit;
-  if ((int64_t)tiles.size() + item_unit_count <= 2 * (int64_t)std::max(1, cu_count)) {
-    for (const SplitTile& st : split_tiles) {
+  // (A shared prefix's pieces are even always: pieces of one length keep their order,
+  // in which those of the same keys go to one die.)
+  const bool one_round = (int64_t)tiles.size() + item_unit_count <= 2 * (int64_t)std::max(1, cu_count);
+  for (const SplitTile& st : split_tiles) {
+    if (one_round || st.shared) {
       const int piece = round_up((st.end - st.begin + st.n - 1) / st.n, 64);
       for (int s = 0; s < st.n; ++s) {
         tiles[st.first + s].kv_begin = st.begin + s * piece;
@@ -832,8 +857,13 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
       else units.push_back(item_unit_codes[b++]);
     }
   }
-  if (items_only)
-    units = by_die(units, [&](int32_t u) { return items[((-1 - u) & ~kUnitMerged) * kItemsPerUnit]; });
+  if (items_only || !runs.empty()) {
+    // all item units; or the tiles of the shared prefixes, whose keys many tiles read
+    std::vector<int> at;
+    for (int i = 0; i < (int)units.size(); ++i)
+      if (items_only || (units[i] >= 0 && tiles[units[i]].part >= 0)) at.push_back(i);
+    by_die(&units, at, [&](int32_t u) { return u >= 0 ? tiles[u] : items[((-1 - u) & ~kUnitMerged) * kItemsPerUnit]; });
+  }
   p->n_tiles = nt;
   p->n_items = (int)items.size();
   p->n_units = (int)units.size();

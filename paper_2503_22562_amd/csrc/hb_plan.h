@@ -183,6 +183,7 @@ struct PlanOptions {
   // groups of requests that share a prefix (checked; no window then)
   const hb_prefix_group* groups = nullptr;
   int n_groups = 0;
+  bool share_all = false;  // join however short a prefix is (testing)
 };
 
 // Build the plan of a validated batch for a GPU with cu_count compute units.

@@ -61,7 +61,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int q_pa
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
         r[t] = u32x4{0u, 0u, 0u, 0u};
-        if (t0 + t >= 0 && t0 + t < u.n) r[t] = ld16(a.v + (int64_t)(u.tok0 + t0 + t) * a.v_stride + g * HD + 8 * c);
+        if (t0 + t >= 0 && t0 + t < u.n) r[t] = ld16_stream(a.v + (int64_t)(u.tok0 + t0 + t) * a.v_stride + g * HD + 8 * c);
       }
       uint16_t* vb = a.v_pool + block + (size_t)g * 16 * HD + (half * HD + 8 * c) * 8;
       const bool whole = t0 >= 0 && t0 + 8 <= u.n;
@@ -103,8 +103,8 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int q_pa
     if (!place(i, h, t)) continue;
     const uint16_t* row = h < a.nq ? a.q + (int64_t)(u.tok0 + t) * a.q_stride + h * HD
                                    : a.k + (int64_t)(u.tok0 + t) * a.k_stride + (h - a.nq) * HD;
-    x0[i] = ld16(row + d0);
-    x1[i] = ld16(row + d1);
+    x0[i] = ld16_stream(row + d0);
+    x1[i] = ld16_stream(row + d1);
   }
   const int pairs = rot / 2;
   for (int i = tid; i < u.n * pairs; i += kThreads) {
@@ -141,8 +141,8 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int q_pa
     }
     if (h < a.nq) {
       uint16_t* row = a.q_out + (int64_t)(u.tok0 + t) * a.q_out_stride + h * HD;
-      st16(row + d0, y0);
-      st16(row + d1, y1);
+      st16_stream(row + d0, y0);
+      st16_stream(row + d1, y1);
     } else {
       uint16_t* kb = a.k_pool + block + (size_t)(h - a.nq) * 16 * HD;
       const int slot = (u.pos0 + t) & 15;

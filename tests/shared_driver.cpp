@@ -1,7 +1,7 @@
 // Prints the plan of a batch whose groups share prefixes: the records that a
 // handle uploads, with the block ids of their ranges looked up as the kernels
 // do, its merge records and its append units.
-// Input: "nq nkv hd cu split_tile split_item check R NG", then R lines "chunk context
+// Input: "nq nkv hd cu split_tile split_item share_all check R NG", then R lines "chunk context
 // n_blocks id ...", then NG lines "first count prefix_len". check 1: check_shared only.
 #include <algorithm>
 #include <cstdio>
@@ -13,11 +13,12 @@ using namespace hb;
 
 int main() {
   hb_layer_config c{};
-  int cu, check, n, ng;
+  int cu, all, check, n, ng;
   PlanOptions opt;
-  if (scanf("%d %d %d %d %d %d %d %d %d", &c.n_q_heads, &c.n_kv_heads, &c.head_dim, &cu, &opt.split_tile, &opt.split_item,
-            &check, &n, &ng) != 9)
+  if (scanf("%d %d %d %d %d %d %d %d %d %d", &c.n_q_heads, &c.n_kv_heads, &c.head_dim, &cu, &opt.split_tile,
+            &opt.split_item, &all, &check, &n, &ng) != 10)
     return 2;
+  opt.share_all = all;
   c.hidden = 64;
   c.ffn_dim = 16;
   c.kv_block_size = 16;

@@ -9,6 +9,12 @@ from hb_workloads import LayerShape, bf16_bits_to_f32
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture(autouse=True)
+def join_them_all(monkeypatch):
+    """Prefixes are joined however short they are."""
+    monkeypatch.setenv("HB_ATTN_SHARE_ALL", "1")
+
+
 def heads(nq, nkv, hd):
     return LayerShape(f"{nq}q{nkv}kv{hd}", 64, nq, nkv, hd, 16, weight_seed=7)
 
@@ -93,6 +99,16 @@ def test_splits(hb, monkeypatch, nqkvhd, name, split_tile, split_item):
 def test_many_rows_behind_a_long_prefix(hb):
     r = Run(heads(16, 4, 128), [(1, 5008 + 9 * i) for i in range(100)], [(0, 100, 5008)], seed=22)
     r.check(r.run())
+
+
+@pytest.mark.parametrize("lens,groups", [CASES["odd lengths"], ([(1, 1040 + 9 * i) for i in range(30)], [(0, 30, 1040)]),
+                                         ([(1, 2060), (2, 2050), (1, 600), (1, 600)], [(0, 2, 2048), (2, 2, 592)])])
+def test_as_the_planner_chooses(hb, monkeypatch, lens, groups):
+    """Short prefixes apart, long ones joined."""
+    monkeypatch.delenv("HB_ATTN_SHARE_ALL")
+    for nqkvhd in ((8, 2, 128), (4, 4, 64)):
+        r = Run(heads(*nqkvhd), lens, groups, seed=28)
+        r.check(r.run())
 
 
 def test_keys_that_dominate(hb):

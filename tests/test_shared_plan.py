@@ -26,9 +26,9 @@ def driver(tmp_path_factory):
     return exe
 
 
-def run(exe, heads, reqs, groups, cu=256, split_tile=0, split_item=0, check=0):
+def run(exe, heads, reqs, groups, cu=256, split_tile=0, split_item=0, check=0, share_all=1):
     """reqs: (chunk, context, table)."""
-    lines = [" ".join(map(str, (*heads, cu, split_tile, split_item, check, len(reqs), len(groups))))]
+    lines = [" ".join(map(str, (*heads, cu, split_tile, split_item, share_all, check, len(reqs), len(groups))))]
     lines += [f"{c} {x} {len(t)} " + " ".join(map(str, t)) for c, x, t in reqs]
     lines += [" ".join(map(str, g)) for g in groups]
     env = dict(os.environ, ASAN_OPTIONS="detect_leaks=0")
@@ -143,10 +143,11 @@ CASES = [
 def test_every_key_once(driver, heads, i, cu, split_tile, split_item):
     lens, groups = CASES[i]
     reqs = batch(lens, groups)
-    plan = run(driver, heads, reqs, groups, cu, split_tile, split_item)
-    assert plan["status"] == [[OK]]
-    check(plan, heads, reqs)
-    check_append(plan, reqs)
+    for share_all in (1, 0):
+        plan = run(driver, heads, reqs, groups, cu, split_tile, split_item, share_all=share_all)
+        assert plan["status"] == [[OK]]
+        check(plan, heads, reqs)
+        check_append(plan, reqs)
 
 
 @pytest.mark.parametrize("seed", range(30))
@@ -176,6 +177,40 @@ def test_prefixes_that_are_read_once(driver):
         units = plan["wave"][u:u + 1] if plan["wave"][u][0] == 0 else plan["wave"][u:u + 4]
         read += sum(max(0, w[6] - w[5]) for w in units)
     assert read == 2 * (64 // 4 * 4096 + 64 * 51)  # per kv head, and each request's own
+
+
+@pytest.mark.parametrize("n,prefix,nkv,joined", [(2, 1008, 8, False), (2, 1024, 8, True), (64, 512, 8, False), (64, 512, 16, True),
+                                                 (90, 512, 8, False), (93, 512, 8, True)])
+def test_prefixes_that_are_too_short(driver, n, prefix, nkv, joined):
+    """192 MB of K and V saved, or 1024 keys."""
+    groups = [(0, n, prefix)]
+    reqs = batch([(1, prefix + 20)] * n, groups)
+    plan = run(driver, (nkv, nkv, 128), reqs, groups, share_all=0)
+    seen = any(w[4] > 1 for w in plan["wave"])  # units whose rows are several requests'
+    assert seen == joined
+    check(plan, (nkv, nkv, 128), reqs)
+
+
+@pytest.mark.parametrize("heads,n,prefix,own,pieces", [((32, 8, 128), 64, 8192, 31, 16), ((32, 8, 128), 256, 16384, 500, 4),
+                                                       ((32, 8, 128), 64, 8192, 1000, 6), ((64, 8, 128), 64, 8192, 31, 8),
+                                                       ((8, 1, 128), 256, 8192, 450, 16), ((16, 4, 64), 300, 4096, 20, 6)])
+def test_pieces_of_a_prefix(driver, heads, n, prefix, own, pieces):
+    """Even pieces of a prefix's tiles, and the tiles of one piece on one of the eight dies (workgroup index modulo 8)."""
+    groups = [(0, n, prefix)]
+    reqs = batch([(1, prefix + own)] * n, groups)
+    plan = run(driver, heads, reqs, groups, share_all=0)
+    tiles = defaultdict(set)
+    for u in range(0, len(plan["wave"]), 4):
+        kind, g, tok0, pos0, npos, b, e, part = plan["wave"][u][:8]
+        if kind == 0:
+            tiles[g, b, e].add((tok0, u // 4 % 8))
+    assert len({(b, e) for _, b, e in tiles}) == pieces
+    assert max(e - b for _, b, e in tiles) - min(e - b for _, b, e in tiles) < 64 * pieces
+    rows = {t for t, _ in next(iter(tiles.values()))}
+    for key, at in tiles.items():
+        assert {t for t, _ in at} == rows
+    spread = [len({die for _, die in at}) for at in tiles.values()]
+    assert sum(spread) <= len(spread) + 8  # a die's last places may have to take a part of one more
 
 
 def test_refusals(driver):
