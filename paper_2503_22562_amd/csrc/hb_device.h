@@ -76,6 +76,29 @@ __device__ __forceinline__ float rows_sum(float v) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// v of lane (this lane ^ X), X a power of two below 64: quad permutations, mirrors of 8-
+// and 16-lane rows (lane ^ 7, lane ^ 15) and the row swaps above, VALU only. (A swap's
+// first result is the partner's in the upper of two rows, the second in the lower.)
+template <int X>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t v) {
+  if constexpr (X == 1) return __builtin_amdgcn_mov_dpp(v, 0xB1, 0xF, 0xF, false);
+  if constexpr (X == 2) return __builtin_amdgcn_mov_dpp(v, 0x4E, 0xF, 0xF, false);
+  if constexpr (X == 4) return __builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp(v, 0x141, 0xF, 0xF, false), 0x1B, 0xF, 0xF, false);
+  if constexpr (X == 8) return __builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp(v, 0x140, 0xF, 0xF, false), 0x141, 0xF, 0xF, false);
+  if constexpr (X == 16) {
+    const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return (threadIdx.x & 16) ? a[0] : a[1];
+  }
+  if constexpr (X == 32) {
+    const auto a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return (threadIdx.x & 32) ? a[0] : a[1];
+  }
+}
+template <int X>
+__device__ __forceinline__ uint64_t lane_xor64(uint64_t v) {
+  return (uint64_t)lane_xor<X>((uint32_t)(v >> 32)) << 32 | lane_xor<X>((uint32_t)v);
+}
+
 // Load from memory that no kernel of the launch writes (the per-iteration
 // metadata): read through the constant address space so that wave-uniform
 // addresses become scalar loads, which do not wait on outstanding vector

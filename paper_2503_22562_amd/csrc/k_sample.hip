@@ -152,9 +152,12 @@ struct Largest {
 };
 template <typename F>
 __device__ __forceinline__ u64 wave_reduce(u64 v, F&& f) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) v = f(v, (u64)__shfl_xor(v, d));
-  return v;
+  v = f(v, (u64)lane_xor64<32>(v));
+  v = f(v, (u64)lane_xor64<16>(v));
+  v = f(v, (u64)lane_xor64<8>(v));
+  v = f(v, (u64)lane_xor64<4>(v));
+  v = f(v, (u64)lane_xor64<2>(v));
+  return f(v, (u64)lane_xor64<1>(v));
 }
 
 // Running sums, over all threads, of a value of each. red: a word per wave, free again after the next barrier.
@@ -234,9 +237,8 @@ struct Scale {
     return FAR && !(v > -INFINITY) ? 0 : w;
   }
   __device__ __forceinline__ u64 weight_of(float v) const { return far ? weight<true>(v) : weight<false>(v); }
-  __device__ __forceinline__ int bin_of(float v) const {
-    return (int)fminf((max - clamp(v)) * per, (float)(kBins - 1));
-  }
+  __device__ __forceinline__ float distance(float v) const { return fminf((max - clamp(v)) * per, kBins - 0.5f); }
+  __device__ __forceinline__ int bin_of(float v) const { return (int)distance(v); }
 };
 __device__ __forceinline__ Scale scale_of(const Setting& g, const Extent& e, int shift, const double* pow2) {
   Scale c;
@@ -361,120 +363,89 @@ __device__ __forceinline__ void scan_bins(Bins& s, u64 (&w)[kOwnBins], uint32_t 
 template <int SIZE>
 struct List {
   u64 key[SIZE], sum[SIZE];
+  uint32_t at[SIZE];
+  uint32_t lo, hi;
 };
 
-// A wave's 64 E places, element lane E + e of them in v[e], into descending order: a
-// bitonic network, by lane swaps down to a distance of E and in registers below. (The
-// loops stay rolled: such code runs once, at the rate at which it is fetched. 20 us
-// unrolled, E = 8.)
-template <int E>
-__device__ __forceinline__ void wave_sort(u64 (&v)[E]) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll 1
-  for (int size = 2; size <= 64 * E; size *= 2) {
-#pragma unroll 1
-    for (int d = size / 2; d >= E; d /= 2) {
-      const bool lower = (lane & (d / E)) == 0;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const u64 o = __shfl_xor(v[e], d / E);
-        const bool down = ((lane * E + e) & size) == 0;
-        if ((v[e] < o) == (lower == down)) v[e] = o;
-      }
-    }
-#pragma unroll
-    for (int d = E / 2; d >= 1; d /= 2) {
-      if (d >= size) continue;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        if (e & d) continue;
-        const bool down = ((lane * E + e) & size) == 0;
-        if ((v[e] < v[e | d]) == down) {
-          const u64 o = v[e];
-          v[e] = v[e | d];
-          v[e | d] = o;
-        }
-      }
-    }
+// The n <= SIZE listed places (no two the same) into descending order: counted into SIZE
+// even parts of the range of distance(logit) (which grows as the logit falls), dealt to
+// their parts' places, and ranked within a part, which few share (equal logits aside). A network over the same 518
+// places took 16 us with a barrier a step, 11 us by waves and a merge of theirs.
+template <int SIZE, typename D>
+__device__ __forceinline__ void sort_list(List<SIZE>& s, int n, u64 (*red)[kWaves], D&& distance) {
+  constexpr int PER = SIZE / kThreads;
+  const int tid = threadIdx.x;
+  if (tid == 0) {
+    s.lo = __float_as_uint(INFINITY);
+    s.hi = 0;
   }
-}
-// The n <= 256 E listed places (no two the same) into descending order: each wave sorts a
-// quarter, and every element goes to its place in the four quarters' order, which
-// binary searches in the others tell. (No barrier within a sort: 518 places 16 us as
-// one network over LDS.)
-template <int E, int SIZE>
-__device__ __forceinline__ void sort_list(List<SIZE>& s, int n) {
-  constexpr int N = 64 * E;
-  static_assert(kWaves * N <= SIZE, "a quarter a wave");
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  u64 v[E];
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    const int i = wave * N + e * 64 + lane;
-    v[e] = i < n ? s.key[i] : 0;
+  for (int k = 0; k < PER; ++k) s.at[tid + k * kThreads] = 0;
+  __syncthreads();
+  u64 v[PER];
+  float f[PER], lo = INFINITY, hi = 0.f;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const int i = tid + k * kThreads;
+    if (i >= n) continue;
+    v[k] = s.key[i];
+    f[k] = distance(value_of(v[k]));
+    lo = fminf(lo, f[k]);
+    hi = fmaxf(hi, f[k]);
   }
-  wave_sort<E>(v);
-  __syncthreads();
-#pragma unroll
-  for (int e = 0; e < E; ++e) s.key[wave * N + lane * E + e] = v[e];
-  __syncthreads();
-  // of each other quarter: how many are larger
-  int above[kWaves - 1][E] = {};
-#pragma unroll 1
-  for (int step = N; step >= 1; step /= 2)
-#pragma unroll
-    for (int o = 0; o < kWaves - 1; ++o)
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const int to = above[o][e] + step;
-        if (to <= N && s.key[(wave + 1 + o) % kWaves * N + to - 1] > v[e]) above[o][e] = to;
-      }
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    int at = lane * E + e;
-#pragma unroll
-    for (int o = 0; o < kWaves - 1; ++o) at += above[o][e];
-    if (v[e]) s.sum[at] = v[e];
+  if (tid < n) {  // (none is negative: their bits are in their order)
+    atomicMin(&s.lo, __float_as_uint(lo));
+    atomicMax(&s.hi, __float_as_uint(hi));
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < n; i += kThreads) s.key[i] = s.sum[i];
+  lo = __uint_as_float(s.lo);
+  const float range = __uint_as_float(s.hi) - lo, per = range > 1e-20f ? SIZE / range : 0.f;
+  int part[PER];
+  uint32_t slot[PER];
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    if (tid + k * kThreads >= n) continue;
+    part[k] = min((int)((f[k] - lo) * per), SIZE - 1);
+    slot[k] = atomicAdd(&s.at[part[k]], 1u);
+  }
+  __syncthreads();
+  uint32_t own[PER], sum = 0;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    own[k] = sum;
+    sum += s.at[tid * PER + k];
+  }
+  const uint32_t before = block_scan(sum, red[0]) - sum;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) s.at[tid * PER + k] = before + own[k];
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < PER; ++k)
+    if (tid + k * kThreads < n) s.sum[s.at[part[k]] + slot[k]] = v[k];
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    if (tid + k * kThreads >= n) continue;
+    const int first = (int)s.at[part[k]], end = part[k] + 1 < SIZE ? (int)s.at[part[k] + 1] : n;
+    int rank = first;
+#pragma unroll 4
+    for (int i = first; i < end; ++i) rank += s.sum[i] > v[k];
+    s.key[rank] = v[k];
+  }
   __syncthreads();
 }
-template <int SIZE>
-__device__ __forceinline__ void sort_any(List<SIZE>& s, int n) {
-  if (n <= kThreads) return sort_list<1>(s, n);
-  if constexpr (SIZE > kThreads) {
-    if (n <= 2 * kThreads) sort_list<2>(s, n);
-    else if (n <= 4 * kThreads) sort_list<4>(s, n);
-    else sort_list<SIZE / kThreads>(s, n);
-  }
-}
-// Running weights of the sorted list into s.sum; gap(i, w, c) adds what stands between
-// element i and the one listed before it. found: the first element whose running count
-// reaches `count`, n where there is none.
+// Running weights of the sorted list into s.sum; gap(i) is what stands between element i
+// and the one listed before it.
 template <int SIZE, typename G>
-__device__ __forceinline__ void scan_list(List<SIZE>& s, int n, const Scale& c, uint32_t count, uint32_t& found,
-                                          u64 (*red)[kWaves], G&& gap) {
+__device__ __forceinline__ void scan_list(List<SIZE>& s, int n, const Scale& c, u64 (*red)[kWaves], G&& gap) {
   const int per = (n + kThreads - 1) / kThreads, i0 = threadIdx.x * per, i1 = min(n, i0 + per);
-  if (threadIdx.x == 0) found = (uint32_t)n;
   u64 sum = 0;
-  uint32_t cnt = 0;
   for (int i = i0; i < i1; ++i) {
-    gap(i, sum, cnt);
-    sum += c.weight_of(value_of(s.key[i]));
-    ++cnt;
+    sum += gap(i) + c.weight_of(value_of(s.key[i]));
     s.sum[i] = sum;
   }
-  const u64 w0 = block_scan(sum, red[0]) - sum;
-  uint32_t c0 = block_scan(cnt, red[1]) - cnt;
-  for (int i = i0; i < i1; ++i) {
-    s.sum[i] += w0;
-    if (count) {
-      u64 none = 0;
-      gap(i, none, c0);
-      if (++c0 >= count) atomicMin(&found, (uint32_t)i);
-    }
-  }
+  const u64 w0 = block_scan(sum, red[1]) - sum;
+  for (int i = i0; i < i1; ++i) s.sum[i] += w0;
   __syncthreads();
 }
 
@@ -482,16 +453,18 @@ __device__ __forceinline__ void scan_list(List<SIZE>& s, int n, const Scale& c, 
 // bins of the searches before: bins [from, to] each, none if to < from.
 struct Search {
   int k_bin, p_from, p_to, m_from, m_to, u_from, u_to;
+  int k_rank;  // which of its bin's elements is the k-th, from 0
   __device__ __forceinline__ int last() const { return max(max(k_bin, p_to), max(m_to, u_to)); }
   __device__ __forceinline__ bool wanted(int b) const {
     return b == k_bin || (b >= p_from && b <= p_to) || (b >= m_from && b <= m_to) || (b >= u_from && b <= u_to);
   }
 };
 __device__ __forceinline__ Search search_of(const Setting& g, const Scale& c, const Bins& s) {
-  Search h = {-1, 0, -1, 0, -1, 0, -1};
+  Search h = {-1, 0, -1, 0, -1, 0, -1, 0};
   u64 lo = s.w[kBins - 1], hi = lo;  // of the kept weight
   if (g.k > 0 && (uint32_t)g.k < s.c[kBins - 1]) {
     h.k_bin = s.met({(uint32_t)g.k, 0.0, false});
+    h.k_rank = g.k - 1 - (int)s.c_before(h.k_bin);
     lo = s.w_before(h.k_bin);
     hi = s.w[h.k_bin];
   }
@@ -534,17 +507,16 @@ __device__ __forceinline__ void answer(const SampleArgs& a, int r, const Scale& 
   if (a.probs) a.probs[r] = f.some ? (float)(c.weights.scaled(c.clamp(value_of(f.place))) / (double)f.kept_w) : 1.f;
 }
 // As pick_listed, of at most 64 elements: all in the registers of a wave (every wave does
-// the same), with no barrier.
-template <int SIZE, typename W, typename C>
-__device__ __forceinline__ Pick pick_few(List<SIZE>& s, int n, const Setting& g, const Scale& c, const Search& h,
-                                         W&& w_before, C&& c_before) {
+// the same).
+template <int SIZE, typename W>
+__device__ __forceinline__ Pick pick_few(List<SIZE>& s, int n, const Setting& g, const Scale& c, const Search& h, W&& w_before) {
   const int lane = threadIdx.x & 63;
   u64 place = lane < n ? s.key[lane] : 0;
   int rank = 0;
-#pragma unroll 1
+#pragma unroll 4
   for (int j = 0; j < n; ++j) rank += s.key[j] > place;
   __syncthreads();
-  if (threadIdx.x < n) s.key[rank] = place;
+  if ((int)threadIdx.x < n) s.key[rank] = place;
   __syncthreads();
   place = s.key[min(lane, n - 1)];
   const float x = value_of(place);
@@ -553,19 +525,11 @@ __device__ __forceinline__ Pick pick_few(List<SIZE>& s, int n, const Setting& g,
   if (lane == 0) before = -1;
   const u64 own = lane < n ? c.weight_of(x) : 0;
   u64 sum = own;
-  uint32_t cnt = lane < n;
-  if (b != before) {
-    sum += w_before(b) - w_before(before + 1);
-    cnt += c_before(b) - c_before(before + 1);
-  }
+  if (b != before) sum += w_before(b) - w_before(before + 1);
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
     const u64 w = __shfl_up(sum, d);
-    const uint32_t k = __shfl_up(cnt, d);
-    if (lane >= d) {
-      sum += w;
-      cnt += k;
-    }
+    if (lane >= d) sum += w;
   }
   // the first of the elements that does, the last where none does
   auto first = [&](bool does) {
@@ -573,7 +537,7 @@ __device__ __forceinline__ Pick pick_few(List<SIZE>& s, int n, const Setting& g,
     return m ? __ffsll(m) - 1 : n - 1;
   };
   Pick f = {0, w_before(kBins), true};
-  if (h.k_bin >= 0) f.kept_w = __shfl(sum, first(cnt >= (uint32_t)g.k));
+  if (h.k_bin >= 0) f.kept_w = __shfl(sum, min(first(b >= h.k_bin) + h.k_rank, n - 1));
   if (h.p_to >= h.p_from) f.kept_w = __shfl(sum, first((double)sum >= (double)g.p * (double)f.kept_w));
   if (h.m_to >= h.m_from) {
     const bool keeps = c.weights.scaled(c.clamp(x)) >= ldexp((double)g.min_p, c.shift);
@@ -585,22 +549,21 @@ __device__ __forceinline__ Pick pick_few(List<SIZE>& s, int n, const Setting& g,
   f.place = __shfl(place, first((double)sum > (double)g.u * (double)f.kept_w));
   return f;
 }
-// The token, from the n listed elements of the wanted bins. w_before, c_before(b): running sums.
-template <int SIZE, typename W, typename C>
+// The token, from the n listed elements, all of the wanted bins' among them.
+// w_before(b): running weights; distance: as sort_list takes it.
+template <int SIZE, typename W, typename D>
 __device__ __forceinline__ Pick pick_listed(List<SIZE>& s, int n, const Setting& g, const Scale& c, const Search& h,
-                                            uint32_t& found, u64 (*red)[kWaves], W&& w_before, C&& c_before) {
+                                            u64 (*red)[kWaves], W&& w_before, D&& distance) {
   n = max(n, 1);  // (the element drawn is always there)
-  if (n <= 64) return pick_few(s, n, g, c, h, w_before, c_before);
-  sort_any(s, n);
+  if (n <= 64) return pick_few(s, n, g, c, h, w_before);
+  sort_list(s, n, red, distance);
   auto bin_at = [&](int i) { return c.bin_of(value_of(s.key[i])); };
-  scan_list(s, n, c, h.k_bin >= 0 ? (uint32_t)g.k : 0u, found, red, [&](int i, u64& w, uint32_t& cnt) {
+  scan_list(s, n, c, red, [&](int i) -> u64 {
     const int b = bin_at(i), before = i ? bin_at(i - 1) : -1;
-    if (b == before) return;
-    w += w_before(b) - w_before(before + 1);
-    cnt += c_before(b) - c_before(before + 1);
+    return b == before ? 0 : w_before(b) - w_before(before + 1);
   });
   Pick f = {0, w_before(kBins), true};
-  if (h.k_bin >= 0) f.kept_w = s.sum[min((int)found, n - 1)];
+  if (h.k_bin >= 0) f.kept_w = s.sum[min(first_met(n, [&](int i) { return bin_at(i) >= h.k_bin; }) + h.k_rank, n - 1)];
   if (h.p_to >= h.p_from) {
     const double want = (double)g.p * (double)f.kept_w;
     f.kept_w = s.sum[first_met(n, [&](int i) { return (double)s.sum[i] >= want; })];
@@ -664,6 +627,7 @@ __global__ __launch_bounds__(kThreads) void sample_weights_kernel(SampleArgs a) 
   __syncthreads();
   const int first = slice * a.slice_len;
   const Logits<BF16> x(a.logits, (int64_t)out * a.stride, first, min(a.slice_len, a.vocab - first));
+  bool listing = true;  // the list has room yet
   // (a run's weights are formed together, with their reads of the table in flight together)
   auto add = [&](auto far, const auto& v) {
     constexpr int N = sizeof v.x / 4;
@@ -684,7 +648,10 @@ __global__ __launch_bounds__(kThreads) void sample_weights_kernel(SampleArgs a) 
       for (int j = 0; j < N; ++j)
         if (w[j]) atomicAdd(&bins.c[b[j]], 1u);
     }
-    if (least < c.near && n < kNearList) {
+    if (least < c.near && listing) {
+      asm volatile("" ::: "memory");  // (keeps the read of n, which waits for the additions above, in here)
+      listing = n < kNearList;
+      if (!listing) return;
 #pragma unroll
       for (int j = 0; j < N; ++j)
         if (w[j] && b[j] < c.near) {
@@ -715,7 +682,7 @@ __global__ __launch_bounds__(kThreads) void sample_weights_kernel(SampleArgs a) 
 #pragma unroll
   for (int k = 0; k < kOwnBins; ++k) {
     own_w[k] = get(&st.w[tid * kOwnBins + k]);
-    own_c[k] = get(&st.c[tid * kOwnBins + k]);
+    own_c[k] = count ? get(&st.c[tid * kOwnBins + k]) : 0;
   }
   const uint32_t listed = get(&st.n_near);
   if (tid == 0) n = 0;
@@ -724,13 +691,11 @@ __global__ __launch_bounds__(kThreads) void sample_weights_kernel(SampleArgs a) 
   if (listed > kNearList || h.last() >= c.near) {
     // running sums, for the next kernel, and where to look
 #pragma unroll
-    for (int k = 0; k < kOwnBins; ++k) {
-      st.w[tid * kOwnBins + k] = bins.w[tid * kOwnBins + k];
-      st.c[tid * kOwnBins + k] = bins.c[tid * kOwnBins + k];
-    }
+    for (int k = 0; k < kOwnBins; ++k) st.w[tid * kOwnBins + k] = bins.w[tid * kOwnBins + k];
     if (tid == 0) {
       st.search[0] = h.k_bin; st.search[1] = h.p_from; st.search[2] = h.p_to; st.search[3] = h.m_from;
-      st.search[4] = h.m_to;  st.search[5] = h.u_from; st.search[6] = h.u_to;
+      st.search[4] = h.m_to;  st.search[5] = h.u_from; st.search[6] = h.u_to;  st.search[7] = h.k_rank;
+      st.counted = bins.c[kBins - 1];
       st.pending = 1;
     }
     return;
@@ -741,7 +706,7 @@ __global__ __launch_bounds__(kThreads) void sample_weights_kernel(SampleArgs a) 
   }
   __syncthreads();
   const Pick f = pick_listed(
-      list, (int)n, g, c, h, base, red, [&](int b) { return bins.w_before(b); }, [&](int b) { return bins.c_before(b); });
+      list, (int)n, g, c, h, red, [&](int b) { return bins.w_before(b); }, [&](float v) { return c.distance(v); });
   answer(a, out, c, f);
 }
 
@@ -753,22 +718,36 @@ __global__ __launch_bounds__(kThreads) void sample_rest_kernel(SampleArgs a) {
     List<kList> list;
     Bins bins;
   } s;
+  // 0, or of which wanted bin it is, from 1 to 255 and no further. (A look-up per element,
+  // in place of four ranges: half the time.)
+  __shared__ uint8_t wanted[kBins];
   __shared__ u64 red[2][kWaves];
   __shared__ double pow2[kSteps];
   __shared__ uint32_t n, base;
   const int r = blockIdx.x / a.parts, out = a.row0 + r, tid = threadIdx.x;
   SampleState& st = a.state[r];
   if (!const_load(&st.pending)) return;
-  const Search h = {st.search[0], st.search[1], st.search[2], st.search[3], st.search[4], st.search[5], st.search[6]};
+  const Search h = {st.search[0], st.search[1], st.search[2], st.search[3], st.search[4], st.search[5], st.search[6], st.search[7]};
   const Setting g = setting_of(a, out);
   const Extent e = row_extent(a, r);
   fill_table(pow2, a.shift);
   const Scale c = scale_of(g, e, a.shift, pow2);
   if (tid == 0) n = 0;
+  uint32_t bits = 0;
+  static_assert(kOwnBins <= 32, "a bit each");
+#pragma unroll
+  for (int k = 0; k < kOwnBins; ++k) bits |= (uint32_t)h.wanted(tid * kOwnBins + k) << k;
+  uint32_t ordinal = block_scan((uint32_t)__popc(bits), red[0]) - __popc(bits);
+#pragma unroll
+  for (int k = 0; k < kOwnBins; ++k) {
+    const bool is = bits >> k & 1;
+    ordinal += is;
+    wanted[tid * kOwnBins + k] = is ? (uint8_t)min(ordinal, 255u) : 0;
+  }
   __syncthreads();
-  // List the elements that take(value, index) wants; n (0 before) counts all of them, and
-  // the first kList to arrive are there.
-  auto gather = [&](const Logits<BF16>& x, auto&& take) {
+  // List the elements that take(value, index) and also(value) want; n (0 before) counts
+  // all of them, and the first kList to arrive are there.
+  auto gather = [&](const Logits<BF16>& x, auto&& take, auto&& also) {
     x.template each<8>([&](const auto& v) {
       constexpr int N = sizeof v.x / 4;
       bool any = false, takes[N];
@@ -777,25 +756,18 @@ __global__ __launch_bounds__(kThreads) void sample_rest_kernel(SampleArgs a) {
       if (!any) return;
 #pragma unroll
       for (int j = 0; j < N; ++j)
-        if (takes[j]) {
+        if (takes[j] && also(v.x[j])) {
           const uint32_t at = atomicAdd(&n, 1u);
           if (at < kList) s.list.key[at] = place_of(clean(v.x[j]), v.first + j);
         }
     });
     __syncthreads();
   };
-  // Of the part: wanted(bin_of(v)), as ranges of what bin_of rounds down. The elements at
-  // the cut have no weight.
+  // (The elements at the cut have no weight.)
   const int first = (blockIdx.x - r * a.parts) * a.part_len;
-  const float least_v = c.far ? -INFINITY : c.cut, end = INFINITY;
-  auto above = [&](int to) { return to == kBins - 1 ? end : (float)(to + 1); };  // (the last bin holds all that is further away)
-  const float f0 = h.k_bin < 0 ? end : h.k_bin, f1 = above(h.k_bin), f2 = h.p_to < h.p_from ? end : h.p_from;
-  const float f3 = above(h.p_to), f4 = h.m_to < h.m_from ? end : h.m_from, f5 = above(h.m_to);
-  const float f6 = h.u_from, f7 = above(h.u_to);
-  gather(Logits<BF16>(a.logits, (int64_t)out * a.stride, first, max(0, min(a.part_len, a.vocab - first))), [&](float v, int) {
-    const float b = (c.max - c.clamp(v)) * c.per;
-    return (v > least_v) & (((b >= f0) & (b < f1)) | ((b >= f2) & (b < f3)) | ((b >= f4) & (b < f5)) | ((b >= f6) & (b < f7)));
-  });
+  const float least_v = c.far ? -INFINITY : c.cut;
+  gather(Logits<BF16>(a.logits, (int64_t)out * a.stride, first, max(0, min(a.part_len, a.vocab - first))),
+         [&](float v, int) { return wanted[c.bin_of(v)] != 0; }, [&](float v) { return v > least_v; });
   const uint32_t mine = n;
   if (tid == 0) base = mine ? atomicAdd(&st.n_list, mine) : 0;
   __syncthreads();
@@ -806,9 +778,11 @@ __global__ __launch_bounds__(kThreads) void sample_rest_kernel(SampleArgs a) {
   if (all <= kList) {
     for (int i = tid; i < (int)all; i += kThreads) s.list.key[i] = get(&st.list[i]);
     __syncthreads();
-    const Pick f = pick_listed(
-        s.list, (int)all, g, c, h, base, red, [&](int b) { return b ? st.w[b - 1] : 0; },
-        [&](int b) { return b ? st.c[b - 1] : 0; });
+    // (distances without the bins between that are not wanted)
+    const Pick f = pick_listed(s.list, (int)all, g, c, h, red, [&](int b) { return b ? st.w[b - 1] : 0; }, [&](float v) {
+      const float d = c.distance(v);
+      return wanted[(int)d] + (d - truncf(d));
+    });
     answer(a, out, c, f);
     return;
   }
@@ -816,7 +790,7 @@ __global__ __launch_bounds__(kThreads) void sample_rest_kernel(SampleArgs a) {
   // places by histograms of its own until the list holds what is left.
   const Logits<BF16> x(a.logits, (int64_t)out * a.stride, 0, a.vocab);
   const double least = ldexp((double)g.min_p, a.shift);
-  const bool by_k = g.k > 0 && (uint32_t)g.k < st.c[kBins - 1], by_p = g.p < 1.f, by_m = g.min_p > 0.f;
+  const bool by_k = g.k > 0 && (uint32_t)g.k < st.counted, by_p = g.p < 1.f, by_m = g.min_p > 0.f;
   Pick f = {0, st.w[kBins - 1], true};
   u64 min_w = f.kept_w;
   if (by_m) {
@@ -878,12 +852,12 @@ __global__ __launch_bounds__(kThreads) void sample_rest_kernel(SampleArgs a) {
     __syncthreads();
     gather(x, [&](float v, int i) {
       const u64 q = place_of(clean(v), i);
-      return q >= from && q <= to && c.weight_of(v) != 0;
-    });
-    const int m = (int)min(n, (uint32_t)kList);
-    sort_any(s.list, m);
-    scan_list(s.list, m, c, stage == 0 ? (uint32_t)g.k - c0 : 0u, base, red, [](int, u64&, uint32_t&) {});
-    const int j = stage == 0 ? min((int)base, m - 1) : first_met(m, [&](int i) { return t.met(0, w0 + s.list.sum[i]); });
+      return q >= from && q <= to;
+    }, [&](float v) { return c.weight_of(v) != 0; });
+    const int m = max(1, (int)min(n, (uint32_t)kList));
+    sort_list(s.list, m, red, [&](float v) { return c.distance(v); });
+    scan_list(s.list, m, c, red, [](int) -> u64 { return 0; });
+    const int j = first_met(m, [&](int i) { return t.met(c0 + i + 1, w0 + s.list.sum[i]); });
     f.place = s.list.key[j];
     if (stage < 2) f.kept_w = w0 + s.list.sum[j];
   }
