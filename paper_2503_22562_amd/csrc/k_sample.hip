@@ -5,14 +5,25 @@
 // first at which the running weight passes u times the kept weight. All of it is the
 // same search -- for the k-th token, for the one that reaches p of the weight, for the
 // one drawn -- in one cumulative distribution, so no row is sorted: a histogram over
-// the logits' distances to their maximum tells the bin that holds an element searched
-// for, and only the bins' elements (at most kList of them at a time) are sorted.
+// the logits' distances to their maximum tells the bins that may hold an element searched
+// for, and only their elements (kList at most, or the search is narrowed) are sorted.
 //
 // Weights w = exp((x - max) / t) are formed in fp64 and summed as integers, w 2^shift
 // rounded to the nearest, with a shift that keeps the sum of a row below 2^63: sums then
 // do not depend on their order, and two programs that use 64 bits agree on every token
-// unless u falls within some 2^-40 of a border. In fp32 they would not: 128256 even
-// weights, each off by 2^-25, move some border past u in one row of 10^4 to 10^5.
+// unless u falls within some 2^-29 of a border (V roundings of 2^-46). In fp32 they would
+// disagree more often: 128256 even weights, each off by 2^-25, move some border past u in
+// one row of 10^4 to 10^5.
+//
+// Three launches: the rows' extents (the bins and weights need the maximum); the
+// histograms, with the likely tokens listed on the way, which tell the token of most
+// rows; and a second look at the rows where they do not. Rows are cut into slices so that
+// few rows fill the card, and the last workgroup of a row to finish draws its token: no
+// launch of its own for that. Few rows are bound by the launches and by chains of
+// barriers (one row of 128256: 15.4 us, 4.2, 6.5 and 3 us of kernels), many by the vector
+// instructions of the weights (256 rows, 131 MB: 27 us extents, 49 weights, of which some
+// 35 instructions an element make 29, 30 the second look at the rows whose limits lie
+// among unlikely tokens; 104 us a call, and 19 to read the logits once).
 #include <algorithm>
 #include <cfloat>
 #include <cstddef>
@@ -778,10 +789,10 @@ __global__ __launch_bounds__(kThreads) void sample_rest_kernel(SampleArgs a) {
   if (all <= kList) {
     for (int i = tid; i < (int)all; i += kThreads) s.list.key[i] = get(&st.list[i]);
     __syncthreads();
-    // (distances without the bins between that are not wanted)
+    // (distances without the bins between that are not wanted; as they are from the 255th wanted one on)
     const Pick f = pick_listed(s.list, (int)all, g, c, h, red, [&](int b) { return b ? st.w[b - 1] : 0; }, [&](float v) {
       const float d = c.distance(v);
-      return wanted[(int)d] + (d - truncf(d));
+      return wanted[(int)d] + (wanted[(int)d] < 255 ? d - truncf(d) : d);
     });
     answer(a, out, c, f);
     return;

@@ -315,3 +315,24 @@ def test_calls_that_are_refused(hb):
     assert (tokens == -7).all()
     hb.hb_destroy_sampler(s)
     hb.hb_destroy_sampler(s)
+
+
+def crowded():
+    """Rows whose k-th token stands in a crowd of equal ones that weighs as much as all before it, so that top_p and u
+    may end at any of hundreds of distinct logits before it."""
+    rng = np.random.default_rng(31)
+    rows, vocab = 60, 6000
+    x = np.full((rows, vocab), -1.5, np.float32)
+    k = np.zeros(rows, np.int32)
+    for r in range(rows):
+        spread = rng.integers(500, 900)
+        x[r, :spread] = -1.4 * rng.random(spread)
+        x[r, spread + 1100:] = -2.0 - 2.0 * rng.random(vocab - spread - 1100)
+        k[r] = spread + rng.integers(300, 900)
+        x[r] = rng.permutation(x[r])
+    return x, rng.random(rows), dict(top_k=k, top_p=rng.choice([0.2, 0.4, 0.5, 0.7], rows))
+
+
+def test_many_tokens_among_which_a_limit_may_lie(hb):
+    x, u, limits = crowded()
+    check(hb, x, u, **limits)
