@@ -1,5 +1,19 @@
 // Append of a planned batch: new queries and keys rotated to their positions, new
 // keys and values put into the pool's layouts.
+//
+// Pair j at position p turns by p f_j: (a, b) -> m (a cos - b sin, b cos + a sin). Bytes
+// bound it: each row is read once and written once, 165 MB for four prompts of 777 to
+// 1500 tokens beside 8 decodes with 70B heads, 23 us at a copy's rate, in 33 us. Decodes
+// are a launch and one chain of loads: 3.3 us of kernel for one, 3.6 for 64.
+//
+// The work is cut by pool blocks, so that a block's 128-byte lines are written by one
+// workgroup, together; and by eight heads, so that one token's heads share its cosines and a
+// batch of a few decodes still has a workgroup for every few heads (4 or 16 heads, 128 or
+// 512 threads: no faster at any of 1 decode, 64 decodes and the 70B case). Rows and q_out
+// are read and written past the caches: nothing reads them again before megabytes of others
+// have passed (70B case, before the values' two ways below: neither 45 us, reads 38.6, both
+// 35.2; keys stored that way too 64: a line of the pool is put together in L2 from several
+// stores).
 #include <algorithm>
 #include <type_traits>
 
@@ -40,31 +54,49 @@ __device__ __forceinline__ void cos_sin_turns(double turns, float& c, float& s) 
 // unrotated dimensions: 16c .. and 16c + 8 ..): both are read before either is
 // written, so q_out may be q. The cosines and sines are formed once per token and
 // pair, one a thread, while the rows are on their way, and shared through LDS.
-// Values: a thread moves eight dimensions of one head for eight slots, transposed
-// in registers; slots outside the unit are not touched.
+// Values of a whole block: a thread moves eight dimensions of one head for eight slots,
+// transposed in registers. Of a part of one, whose other slots are not touched: of one
+// token, value by value. (Units of both kinds through the transposition, with a test of
+// each slot: 10.4 us of kernel, with this 6.2, for a chunk of 777 tokens behind 5234 and 45
+// decodes with 16 and 4 heads; so much code is read for the few units that need it. With
+// the workgroups of values before the others 5.6: theirs is the longer chain.)
 template <int HD, bool INTERLEAVED>
-__global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int q_parts) {
+__global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int v_parts) {
   __shared__ __attribute__((aligned(16))) float cs[2][kTokens][HD / 2];
   constexpr int CH = HD / 16;  // threads of one head of one token
   const AppendUnit u = const_load(reinterpret_cast<const AppendUnit*>(a.units) + blockIdx.x / a.parts);
   const int part = blockIdx.x % a.parts, tid = threadIdx.x;
   const size_t block = (size_t)u.block * a.nkv * 16 * HD;
-  if (part >= q_parts) {  // values
-    constexpr int VC = HD / 8;
-    const int c = tid % VC, half = (tid / VC) & 1;
-    for (int hi = tid / (2 * VC); hi < kHeads; hi += kThreads / (2 * VC)) {
-      const int g = (part - q_parts) * kHeads + hi;
-      if (g >= a.nkv) return;
-      const int t0 = 8 * half - (u.pos0 & 15);  // token of the half's first slot (may lie outside [0, n))
-      if (t0 + 8 <= 0 || t0 >= u.n) return;
+  if (part < v_parts) {  // values
+    constexpr int VC = HD / 8, STEP = kThreads / VC;
+    const int c = tid % VC, g0 = part * kHeads, heads = min(kHeads, a.nkv - g0);
+    if (u.n < 16) {
+      constexpr int LOADS = 4;
+      for (int e0 = tid / VC; e0 < u.n * heads; e0 += LOADS * STEP) {
+        u32x4 r[LOADS];
+        uint16_t* to[LOADS];
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+          const int e = e0 + i * STEP, h = e / u.n, t = e - h * u.n, slot = (u.pos0 & 15) + t;
+          to[i] = a.v_pool + block + (size_t)(g0 + h) * 16 * HD + ((slot >> 3) * HD + 8 * c) * 8 + (slot & 7);
+          if (e < u.n * heads) r[i] = ld16_stream(a.v + (int64_t)(u.tok0 + t) * a.v_stride + (g0 + h) * HD + 8 * c);
+        }
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+          if (e0 + i * STEP >= u.n * heads) break;
+#pragma unroll
+          for (int d = 0; d < 8; ++d) to[i][8 * d] = (uint16_t)(r[i][d >> 1] >> (16 * (d & 1)));
+        }
+      }
+      return;
+    }
+    const int half = (tid / VC) & 1;
+    for (int h = tid / (2 * VC); h < heads; h += STEP / 2) {
+      const uint16_t* row = a.v + (int64_t)(u.tok0 + 8 * half) * a.v_stride + (g0 + h) * HD + 8 * c;
       u32x4 r[8];
 #pragma unroll
-      for (int t = 0; t < 8; ++t) {
-        r[t] = u32x4{0u, 0u, 0u, 0u};
-        if (t0 + t >= 0 && t0 + t < u.n) r[t] = ld16_stream(a.v + (int64_t)(u.tok0 + t0 + t) * a.v_stride + g * HD + 8 * c);
-      }
-      uint16_t* vb = a.v_pool + block + (size_t)g * 16 * HD + (half * HD + 8 * c) * 8;
-      const bool whole = t0 >= 0 && t0 + 8 <= u.n;
+      for (int t = 0; t < 8; ++t) r[t] = ld16_stream(row + t * a.v_stride);
+      uint16_t* vb = a.v_pool + block + (size_t)(g0 + h) * 16 * HD + (half * HD + 8 * c) * 8;
 #pragma unroll
       for (int d = 0; d < 8; ++d) {
         u32x4 o;
@@ -73,13 +105,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int q_pa
           const uint32_t x = r[2 * w][d >> 1], y = r[2 * w + 1][d >> 1];
           o[w] = (d & 1) ? (x >> 16) | (y & 0xFFFF0000u) : (x & 0xFFFFu) | (y << 16);
         }
-        if (whole) {
-          st16(vb + 8 * d, o);
-        } else {
-#pragma unroll
-          for (int t = 0; t < 8; ++t)
-            if (t0 + t >= 0 && t0 + t < u.n) vb[8 * d + t] = (uint16_t)(o[t >> 1] >> (16 * (t & 1)));
-        }
+        st16(vb + 8 * d, o);
       }
     }
     return;
@@ -93,7 +119,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int q_pa
   // item i of a thread: head hi, token t (heads of one token first)
   auto place = [&](int i, int& h, int& t) {
     const int e = (tid + i * kThreads) / CH;
-    h = part * kHeads + e % kHeads;
+    h = (part - v_parts) * kHeads + e % kHeads;
     t = e / kHeads;
     return t < u.n && h < a.nq + a.nkv;
   };
@@ -156,14 +182,14 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int q_pa
 
 void launch_append(hipStream_t s, AppendArgs a) {
   if (a.n_units <= 0) return;
-  const int q_parts = (a.nq + a.nkv + kHeads - 1) / kHeads;
-  a.parts = q_parts + (a.nkv + kHeads - 1) / kHeads;
+  const int v_parts = (a.nkv + kHeads - 1) / kHeads;
+  a.parts = v_parts + (a.nq + a.nkv + kHeads - 1) / kHeads;
   // a grid holds fewer than 2^32 threads
   const int most = (1 << 23) / a.parts;
   for (int left = a.n_units; left > 0; left -= most, a.units += 4 * (size_t)most) {
     const int groups = std::min(left, most) * a.parts;
     auto go = [&](auto hd, auto inter) {
-      append_kernel<decltype(hd)::value, decltype(inter)::value><<<groups, kThreads, 0, s>>>(a, q_parts);
+      append_kernel<decltype(hd)::value, decltype(inter)::value><<<groups, kThreads, 0, s>>>(a, v_parts);
     };
     auto layout = [&](auto hd) { a.interleaved ? go(hd, std::true_type{}) : go(hd, std::false_type{}); };
     if (a.hd == 128) layout(std::integral_constant<int, 128>{});
