@@ -220,8 +220,7 @@ struct SampleState {
   uint32_t n_near, n_list;  // elements found, of which the lists hold the first ones
   uint32_t slices_done, parts_done;
   int32_t pending, search[8];  // a row whose likely tokens do not tell, and the bins to look into
-  uint32_t counted;            // elements with weight, where top_k counts them
-  uint32_t pad[2];
+  uint32_t pad[3];
   unsigned long long near[kSampleNear], list[kSampleList];
 };
 // Slices of a row (all of slice_len elements but the last): few rows in as many as

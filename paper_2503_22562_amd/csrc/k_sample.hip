@@ -706,7 +706,6 @@ __global__ __launch_bounds__(kThreads) void sample_weights_kernel(SampleArgs a) 
     if (tid == 0) {
       st.search[0] = h.k_bin; st.search[1] = h.p_from; st.search[2] = h.p_to; st.search[3] = h.m_from;
       st.search[4] = h.m_to;  st.search[5] = h.u_from; st.search[6] = h.u_to;  st.search[7] = h.k_rank;
-      st.counted = bins.c[kBins - 1];
       st.pending = 1;
     }
     return;
@@ -797,17 +796,20 @@ __global__ __launch_bounds__(kThreads) void sample_rest_kernel(SampleArgs a) {
     answer(a, out, c, f);
     return;
   }
-  // Bins that hold more than the list (many equal logits): each search narrows the
-  // places by histograms of its own until the list holds what is left.
+  // Bins that hold more than the list (many equal logits): each search goes to its bin by
+  // the running sums, and narrows the places of that by histograms of its own until the
+  // list holds what is left.
   const Logits<BF16> x(a.logits, (int64_t)out * a.stride, 0, a.vocab);
-  const double least = ldexp((double)g.min_p, a.shift);
-  const bool by_k = g.k > 0 && (uint32_t)g.k < st.counted, by_p = g.p < 1.f, by_m = g.min_p > 0.f;
-  Pick f = {0, st.w[kBins - 1], true};
+  auto w_before = [&](int b) { return b ? st.w[b - 1] : 0; };
+  Pick f = {0, w_before(kBins), true};
   u64 min_w = f.kept_w;
-  if (by_m) {
+  if (h.m_to >= h.m_from) {
+    const double least = ldexp((double)g.min_p, a.shift);
     u64 sum = 0;
-    x.template each<2>([&](const auto& v) {
+    x.template each<4>([&](const auto& v) {
       for (const float y : v.x) {
+        const int b = c.bin_of(y);
+        if (b < h.m_from || b > h.m_to) continue;
         const u64 w = c.weight_of(y);
         if (w && c.weights.scaled(c.clamp(y)) >= least) sum += w;
       }
@@ -815,31 +817,68 @@ __global__ __launch_bounds__(kThreads) void sample_rest_kernel(SampleArgs a) {
     sum = wave_reduce(sum, Sum());
     if ((tid & 63) == 0) red[0][tid >> 6] = sum;
     __syncthreads();
-    min_w = red[0][0] + red[0][1] + red[0][2] + red[0][3];
+    min_w = w_before(h.m_from) + red[0][0] + red[0][1] + red[0][2] + red[0][3];
     f.some = min_w > 0;
   }
-  for (int stage = by_k ? 0 : by_p ? 1 : 2; stage < 3; ++stage) {
-    if (stage == 1 && !by_p) continue;
+  for (int stage = 0; stage < 3; ++stage) {
+    if (stage == 0 ? h.k_bin < 0 : stage == 1 && h.p_to < h.p_from) continue;
     if (stage == 2) f.kept_w = Least()(f.kept_w, min_w);
     const Target t = {stage == 0 ? (uint32_t)g.k : 0u, (double)(stage == 1 ? g.p : g.u) * (double)f.kept_w, stage == 2};
-    u64 to = e.top, from = place_of(e.lo, 0x7FFFFFFF), w0 = 0;
-    uint32_t c0 = 0, left = kList + 1;
+    const int bin = stage == 0 ? h.k_bin : first_met(kBins, [&](int i) { return t.met(0, st.w[i]); });
+    u64 w0 = w_before(bin), from = ~0ull, to = 0;
+    uint32_t c0 = stage == 0 ? (uint32_t)(g.k - 1 - h.k_rank) : 0u, left = kList + 1;
+    x.template each<4>([&](const auto& v) {
+#pragma unroll
+      for (int j = 0; j < (int)(sizeof v.x / 4); ++j) {
+        if (c.bin_of(v.x[j]) != bin || !(v.x[j] > least_v)) continue;
+        const u64 q = place_of(clean(v.x[j]), v.first + j);
+        from = Least()(from, q);
+        to = Largest()(to, q);
+      }
+    });
+    from = wave_reduce(from, Least());
+    to = wave_reduce(to, Largest());
+    __syncthreads();
+    if ((tid & 63) == 0) {
+      red[0][tid >> 6] = from;
+      red[1][tid >> 6] = to;
+    }
+    __syncthreads();
+    for (int w = 0; w < kWaves; ++w) {
+      from = Least()(from, red[0][w]);
+      to = Largest()(to, red[1][w]);
+    }
     while (left > kList) {
       int sh = 0;
       while (((to - from) >> sh) >= kBins) ++sh;
       __syncthreads();
       s.bins.clear();
       __syncthreads();
-      x.template each<2>([&](const auto& v) {
+      x.template each<4>([&](const auto& v) {
+        // (a run's elements of one bin are added together: equal logits beside each other are)
+        int last = -1;
+        u64 w_sum = 0;
+        uint32_t c_sum = 0;
+        auto add = [&] {
+          atomicAdd(&s.bins.w[last], w_sum);
+          atomicAdd(&s.bins.c[last], c_sum);
+        };
         for (int j = 0; j < (int)(sizeof v.x / 4); ++j) {
           const u64 q = place_of(clean(v.x[j]), v.first + j);
           if (q < from || q > to) continue;
           const u64 w = c.weight_of(v.x[j]);
           if (w == 0) continue;
           const int b = (int)((to - q) >> sh);
-          atomicAdd(&s.bins.w[b], w);
-          atomicAdd(&s.bins.c[b], 1u);
+          if (b != last && last >= 0) {
+            add();
+            w_sum = 0;
+            c_sum = 0;
+          }
+          last = b;
+          w_sum += w;
+          ++c_sum;
         }
+        if (last >= 0) add();
       });
       __syncthreads();
       u64 own_w[kOwnBins];
