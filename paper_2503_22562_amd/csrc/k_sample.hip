@@ -16,14 +16,15 @@
 // one row of 10^4 to 10^5.
 //
 // Three launches: the rows' extents (the bins and weights need the maximum); the
-// histograms, with the likely tokens listed on the way, which tell the token of most
-// rows; and a second look at the rows where they do not. Rows are cut into slices so that
-// few rows fill the card, and the last workgroup of a row to finish draws its token: no
-// launch of its own for that. Few rows are bound by the launches and by chains of
-// barriers (one row of 128256: 15.4 us, 4.2, 6.5 and 3 us of kernels), many by the vector
-// instructions of the weights (256 rows, 131 MB: 27 us extents, 49 weights, of which some
-// 35 instructions an element make 29, 30 the second look at the rows whose limits lie
-// among unlikely tokens; 104 us a call, and 19 to read the logits once).
+// histograms, with the likely tokens listed on the way, which tell the token of most rows;
+// and a second look at the rows where they do not. Rows are cut into slices so that few
+// rows fill the card, and the last workgroup of a row to finish draws its token: no launch
+// of its own for that. Few rows are bound by the launches and by chains of barriers (one
+// row of 128256: 15.4 us a call; kernels 3.6, 11.5 and 0.9, or 3.8 where the row is read
+// again), many by the vector instructions of the weights (256 rows, 131 MB: 27 us extents,
+// 49 weights, of which some 35 instructions an element make 29, 30 the second look at the
+// rows whose limits lie among unlikely tokens; 104 us a call, and 19 to read the logits
+// once).
 #include <algorithm>
 #include <cfloat>
 #include <cstddef>
