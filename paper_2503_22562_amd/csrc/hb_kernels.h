@@ -225,8 +225,9 @@ struct SampleState {
 };
 // Slices of a row (all of slice_len elements but the last): few rows in as many as
 // are worth a workgroup's start, many in about eight per CU, of which each adds its
-// histogram to the row's once (64 rows of 128256, weights: 8K elements 17.6 us, 4K
-// 22.8, 16K 20.1; 256 rows: 16K 40.6, 32K 42.8).
+// histogram to the row's once, some 2000 atomics (the weights' kernel, 64 rows of 128256:
+// slices of 4K elements 32 us, 8K 27, 16K 26, 32K 33; 256 rows: 8K 57, 16K 47, 32K 49;
+// 33 rows of 32003: 2K 16, 4K 15, 8K 17, 16K 22).
 inline void sample_slices(int rows, int vocab, int* slices, int* slice_len) {
   const int want = std::max(1, std::min(kSampleSlices, 2048 / rows));
   const int least = (int64_t)rows * ((vocab + 2047) / 2048) > 1024 ? 8192 : 2048;
@@ -234,7 +235,8 @@ inline void sample_slices(int rows, int vocab, int* slices, int* slice_len) {
   *slices = (vocab + *slice_len - 1) / *slice_len;
 }
 // Parts of a row (of part_len elements) where it has to be read again: as many as are
-// worth a workgroup's start, for few rows and where all rows are (about eight per CU).
+// worth a workgroup's start, for few rows and where all rows are (about eight per CU; 64 rows
+// of 128256: parts of 2K elements 22 us, 4K 19, 8K 19, 16K 22; 256 rows: 4K 43, 8K 34, 16K 28).
 inline void sample_parts(int rows, int vocab, int* parts, int* part_len) {
   const int want = std::max(1, std::min(32, 2048 / rows));
   *part_len = std::max(4096, ((vocab + want - 1) / want + 7) / 8 * 8);
