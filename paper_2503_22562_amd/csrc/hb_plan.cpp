@@ -422,13 +422,14 @@ static int fit_tile_split(const std::vector<int>& lengths, int nkv, int64_t slot
 // one die: workgroups go to the kDies dies in turn, each with an L2 of its own,
 // and every die would fetch all of K and V otherwise (cold caches, 64 tokens
 // behind 500 cached, eight kv heads, 128 units 13.1 -> 10.0 us; 70B heads behind
-// 900 17.4 -> 12.6). Larger groups first, each to the die with the most room, the
-// rest of it to the next. (Tiles share a key range four times less often: even
+// 900 17.4 -> 12.6). Each group goes to the die with the most room, the rest of it to
+// the next. (Tiles share a key range four times less often: even
 // with cold caches, 19.8 -> 23.2 us with warm ones, 64 tiles of 1000 keys.)
 constexpr int kDies = 8;
-// units[at[i]] are dealt anew over the places `at`.
+// units[at[i]] are dealt anew over the places `at`, group by group: the largest first,
+// which then lie whole on one die, or in the order in which they stand.
 template <typename F>
-static void by_die(std::vector<int32_t>* units, const std::vector<int>& at, F&& item_of) {
+static void by_die(std::vector<int32_t>* units, const std::vector<int>& at, bool largest_first, F&& item_of) {
   std::map<std::tuple<int, int, int>, int> known;
   std::vector<std::vector<int32_t>> groups;
   std::vector<int> places[kDies];
@@ -440,7 +441,8 @@ static void by_die(std::vector<int32_t>* units, const std::vector<int>& at, F&& 
     groups[found->second].push_back(u);
     places[i % kDies].push_back(i);
   }
-  std::stable_sort(groups.begin(), groups.end(), [](const auto& a, const auto& b) { return a.size() > b.size(); });
+  if (largest_first)
+    std::stable_sort(groups.begin(), groups.end(), [](const auto& a, const auto& b) { return a.size() > b.size(); });
   size_t next[kDies] = {}, room[kDies];
   for (int x = 0; x < kDies; ++x) room[x] = places[x].size();
   for (const auto& group : groups) {
@@ -858,11 +860,16 @@ void build_plan(const Dims& d, const hb_batch_desc* desc, int cu_count, Plan* p,
     }
   }
   if (items_only || !runs.empty()) {
-    // all item units; or the tiles of the shared prefixes, whose keys many tiles read
+    // All item units, which are one round. Or the tiles of the shared prefixes, whose keys
+    // many tiles read: among the places that they hold and the longest first as before, since
+    // they are a queue with the other tiles (8B heads, cold caches, 64 decodes behind 8192 shared
+    // keys and a chunk of 777 behind 5234, all split tiles dealt anew, the most read first: 217 us,
+    // so 172; with a fresh chunk of 2048 102, 75).
+    auto of_run = [&](const AttnItem& t) { return t.part >= 0 && t.part < run_slots; };
     std::vector<int> at;
     for (int i = 0; i < (int)units.size(); ++i)
-      if (items_only || (units[i] >= 0 && tiles[units[i]].part >= 0)) at.push_back(i);
-    by_die(&units, at, [&](int32_t u) { return u >= 0 ? tiles[u] : items[((-1 - u) & ~kUnitMerged) * kItemsPerUnit]; });
+      if (items_only || (units[i] >= 0 && of_run(tiles[units[i]]))) at.push_back(i);
+    by_die(&units, at, items_only, [&](int32_t u) { return u >= 0 ? tiles[u] : items[((-1 - u) & ~kUnitMerged) * kItemsPerUnit]; });
   }
   p->n_tiles = nt;
   p->n_items = (int)items.size();

@@ -213,6 +213,68 @@ def test_pieces_of_a_prefix(driver, heads, n, prefix, own, pieces):
     assert sum(spread) <= len(spread) + 8  # a die's last places may have to take a part of one more
 
 
+def tiles_in_order(plan, heads, reqs):
+    """(place, kv head, first key, keys, rows, whether it is a shared prefix's) of each tile."""
+    request_of = [r for r, (c, _, _) in enumerate(reqs) for _ in range(c)]
+    out = []
+    for u in range(0, len(plan["wave"]), 4):
+        kind, g, tok0, _, npos, b, e, _ = plan["wave"][u][:8]
+        if kind == 0:
+            c = reqs[request_of[tok0]][0]
+            out.append((u // 4, g, b, e - b, npos, c * heads[0] // heads[1] < 64))  # (such requests fill no tile alone)
+    return out
+
+
+@pytest.mark.parametrize("lens,groups", [([(1, 8242)] * 64 + [(2048, 0)], [(0, 64, 8192)]),
+                                         ([(1, 4146)] * 64 + [(2048, 0)], [(0, 64, 4096)]),
+                                         ([(1, 8242)] * 64 + [(777, 5234)], [(0, 64, 8192)]),
+                                         ([(1500, 300)] + [(1, 2098)] * 32 + [(777, 0), (900, 2000)], [(1, 32, 2048)])])
+def test_chunks_beside_a_prefix(driver, lens, groups):
+    """Tiles are handed out the longest first, a prefix's pieces too: none of the longest stands behind a shorter one of
+    a chunk."""
+    heads = (32, 8, 128)
+    reqs = batch(lens, groups)
+    plan = run(driver, heads, reqs, groups, share_all=0)
+    check(plan, heads, reqs)
+    tiles = tiles_in_order(plan, heads, reqs)
+    assert any(t[5] for t in tiles) and any(not t[5] for t in tiles)
+    own = [keys * rows for _, _, _, keys, rows, shared in tiles if not shared]
+    assert own == sorted(own, reverse=True)
+    longest = max(keys * rows for _, _, _, keys, rows, _ in tiles)
+    last = max(i for i, t in enumerate(tiles) if t[3] * t[4] == longest)
+    first = min(i for i, t in enumerate(tiles) if t[3] * t[4] < longest and not t[5])
+    assert last < first
+
+
+@pytest.mark.parametrize("sizes", [[(112, 12704), (17, 2224), (148, 2272), (50, 6416)], [(95, 5392), (96, 1056), (33, 4768)],
+                                   [(141, 2448), (23, 4704)], [(107, 5104), (90, 1136), (21, 4704)]])
+def test_prefixes_of_different_lengths(driver, sizes):
+    """A die's tiles stand the longest first, however many rows read a prefix."""
+    heads = (32, 8, 128)
+    lens, groups = [], []
+    for n, p in sizes:
+        groups.append((len(lens), n, p))
+        lens += [(1, p + 20)] * n
+    lens.append((1000, 500))
+    reqs = batch(lens, groups)
+    plan = run(driver, heads, reqs, groups, share_all=0)
+    check(plan, heads, reqs)
+    ranges = defaultdict(list)  # key range -> (place, keys, rows) of the tiles that read it
+    member = [i for i, (n, _) in enumerate(sizes) for _ in range(n)]
+    for u in range(0, len(plan["wave"]), 4):
+        kind, g, tok0, _, npos, b, e, _ = plan["wave"][u][:8]
+        if kind == 0 and tok0 < len(member):
+            ranges[member[tok0], g, b].append((u // 4, e - b, npos))
+    for die in range(8):
+        size = {}
+        for tiles in ranges.values():
+            for place, _, _ in tiles:
+                if place % 8 == die:
+                    size[place] = max(keys * rows for _, keys, rows in tiles)
+        order = [size[place] for place in sorted(size)]
+        assert order == sorted(order, reverse=True)
+
+
 def test_refusals(driver):
     heads, lens = (4, 2, 64), [(1, 40), (1, 50), (1, 60)]
     good = [(0, 2, 32)]
