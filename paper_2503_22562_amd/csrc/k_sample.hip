@@ -209,7 +209,8 @@ struct Setting {
 __device__ __forceinline__ Setting setting_of(const SampleArgs& a, int r) {
   Setting g;
   g.t = a.temperature ? a.temperature[r] : 1.f;
-  g.p = a.top_p ? a.top_p[r] : 1.f;
+  const float p = a.top_p ? a.top_p[r] : 1.f;
+  g.p = p < 0.f ? 0.f : p;  // (-infinity times a sum of 0 would be no number)
   g.min_p = a.min_p ? a.min_p[r] : 0.f;
   g.k = a.top_k ? a.top_k[r] : 0;
   const float u = a.u[r];

@@ -336,3 +336,14 @@ def crowded():
 def test_many_tokens_among_which_a_limit_may_lie(hb):
     x, u, limits = crowded()
     check(hb, x, u, **limits)
+
+
+@pytest.mark.parametrize("vocab", [5, 999, 30000])
+@pytest.mark.parametrize("k", [2, 3, 50])
+def test_top_p_of_minus_infinity_among_few_tokens(hb, vocab, k):
+    """Nothing but the first token, also where the first k all stand at the top."""
+    rng = np.random.default_rng(vocab + k)
+    x = np.concatenate([np.full((4, vocab), 0.5), 1e-3 * rng.standard_normal((4, vocab)), peaked(rng, 4, vocab)])
+    u = np.tile([0.0, 0.3, 0.7, 1.0], 3)
+    tokens = check(hb, x.astype(np.float32), u, top_k=np.full(12, k), top_p=np.full(12, -INF))
+    assert np.array_equal(tokens, x.astype(np.float32).argmax(1))
