@@ -489,7 +489,9 @@ __device__ __forceinline__ Search search_of(const Setting& g, const Scale& c, co
   }
   if (g.min_p > 0.f) {
     // the logit at which a weight is min_p: its bin, and the next ones for what rounding does
-    const int b = g.min_p < 1.f ? c.bin_of(fmaxf(c.max + g.t * logf(g.min_p), -FLT_MAX)) : 0;
+    // (a weight is 1 in fp64 down to a distance of 2^-54 t; none is above 1)
+    const float ends = g.min_p < 1.f ? logf(g.min_p) : g.min_p > 1.f ? 0.f : -0x1p-54f;
+    const int b = ends < 0.f ? c.bin_of(fmaxf(c.max + g.t * ends, -FLT_MAX)) : 0;
     h.m_from = max(0, b - 1);
     h.m_to = min(kBins - 1, b + 1);
     if (s.w[h.m_to] <= lo) {  // min_p ends before the others

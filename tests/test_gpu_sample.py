@@ -347,3 +347,25 @@ def test_top_p_of_minus_infinity_among_few_tokens(hb, vocab, k):
     u = np.tile([0.0, 0.3, 0.7, 1.0], 3)
     tokens = check(hb, x.astype(np.float32), u, top_k=np.full(12, k), top_p=np.full(12, -INF))
     assert np.array_equal(tokens, x.astype(np.float32).argmax(1))
+
+
+@pytest.mark.parametrize("vocab", [5, 999, 30000])
+def test_min_p_of_1_where_every_weight_is_1(hb, vocab):
+    """At temperatures so high that all weights are 1 in fp64, min_p = 1 keeps all; above 1 it keeps the first token."""
+    rng = np.random.default_rng(vocab)
+    x = np.repeat(rng.standard_normal((1, vocab)), 12, 0).astype(np.float32)
+    u = np.tile([0.0, 0.3, 0.7, 0.999], 3)
+    t = np.repeat([INF, 3e38, 1e30], 4)
+    tokens = check(hb, x, u, temperature=t, min_p=np.ones(12))
+    assert len(set(tokens)) == 4
+    check(hb, x, u, temperature=t, min_p=np.ones(12), top_k=np.full(12, max(1, vocab // 3)), top_p=np.full(12, 0.9))
+    tokens = check(hb, x, u, temperature=t, min_p=np.full(12, 1.0 + 2.0 ** -23))
+    assert len(set(tokens)) == 1
+    # exp(-d / t) is 1 in fp64 where d / t <= 2^-54, half its step below 1 (numpy's exp may be off by a step there): of
+    # logits 2^-24 apart, the first t 2^-30 and one, and the token is the first place above u times their number
+    near = np.repeat(np.float32(1) - np.float32(2.0 ** -24) * np.arange(vocab, dtype=np.float32)[None], 4, 0)
+    t = np.array([1.0, 1e9, 2.5 * 2.0 ** 30, 1e13], np.float32)
+    n = np.minimum(vocab, np.floor(t.astype(np.float64) * 2.0 ** -30) + 1)
+    tokens, probs = draw(hb, near, u[:4], min_p=np.ones(4), temperature=t)
+    assert np.array_equal(tokens, np.floor(u[:4].astype(np.float32) * n.astype(np.float64)))
+    assert (np.abs(probs - 1 / n) <= 2.0 ** -24 / n).all()
