@@ -339,8 +339,10 @@ typedef struct {
  * original_context < 1 or not 0 <= low < high < infinity). */
 hb_status hb_rope_frequencies(int32_t rotary_dim, double theta, const hb_rope_scaling* scaling, double* inv_freq);
 
-/* Rotation of the handle's later hb_run_append calls. Plans made from now on hold
- * where a batch's new tokens go in the cache; one made before cannot append.
+/* Rotation of the handle's later hb_run_append calls, those of a plan that stands
+ * among them: a plan holds where its batch's new tokens go in the cache, and no
+ * rotation. Plans hold that from the handle's first call of this on; one made
+ * before it cannot append.
  *   rotary_dim  a multiple of 16 up to head_dim; 0: nothing is rotated
  *   inv_freq    host [rotary_dim / 2], copied (NULL if rotary_dim is 0)
  * Errors: HB_ERR_INVALID (null pointer, a layout that is none, a frequency or
@@ -362,8 +364,8 @@ hb_status hb_set_attention_rope(hb_attention* attention, int32_t rotary_dim, int
  * and reduced in fp64, cosines, sines and products in fp32, rounded once to bf16;
  * v is copied bit by bit, as are the dimensions that are not rotated. Enqueues on
  * the handle's stream and returns; allocates nothing. Errors: HB_ERR_INVALID (null
- * pointer, no plan, a plan made before hb_set_attention_rope or of requests that
- * write one slot twice, a pool of fewer blocks, a stride below the row, no multiple
+ * pointer, no plan, a plan made before the handle's first hb_set_attention_rope or of
+ * requests that write one slot twice, a pool of fewer blocks, a stride below the row, no multiple
  * of 8 or above 2^40, misaligned pointer, an overlap of q_out with k, v or part of q, of a
  * pool with any row or with the other), HB_ERR_HIP (among others: the stream is
  * under graph capture). */

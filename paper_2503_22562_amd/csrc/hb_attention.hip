@@ -252,8 +252,8 @@ hb_status hb_run_append(hb_attention* a, const hb_kv_pool* pool, const void* q, 
   if (!a) return fail(HB_ERR_INVALID, "null attention handle");
   if (!a->planned) return fail(HB_ERR_INVALID, "hb_run_append before a successful plan");
   if (!a->can_append)
-    return fail(HB_ERR_INVALID, "hb_run_append: the plan was made before hb_set_attention_rope, or two of its requests "
-                                "write one slot");
+    return fail(HB_ERR_INVALID, "hb_run_append: the plan was made before the handle's first hb_set_attention_rope, "
+                                "or two of its requests write one slot");
   if (a->plan.T == 0) return HB_OK;
   const int64_t row = (int64_t)a->d.nq * a->d.hd, kv_row = (int64_t)a->d.nkv * a->d.hd;
   return run_append(a, pool, {(uintptr_t)q, q_stride, row}, {(uintptr_t)k, k_stride, kv_row},

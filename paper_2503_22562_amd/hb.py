@@ -517,7 +517,8 @@ def hb_rope_frequencies(rotary_dim: int, theta: float, factor: Optional[float] =
 
 
 def hb_set_attention_rope(attention: Attention, inv_freq, layout: int = HB_ROPE_HALF, magnitude: float = 1.0) -> None:
-    """Rotation of later hb_run_append calls: the first 2 len(inv_freq) dimensions of a head; plan after it."""
+    """Rotation of later hb_run_append calls: the first 2 len(inv_freq) dimensions of a head. The latest one
+    counts, for a plan that stands too; plans made before the first one cannot append."""
     f = np.ascontiguousarray(inv_freq, dtype=np.float64).reshape(-1)
     _check(load().hb_set_attention_rope(attention.handle, 2 * len(f), _int32(layout), f.ctypes.data, magnitude))
 

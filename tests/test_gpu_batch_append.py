@@ -206,6 +206,27 @@ def test_plans_in_turn_and_streams(hb):
     d.check()
 
 
+def test_a_plan_that_stands_takes_the_latest_rotation(hb):
+    """Only a plan made before the handle's first rotation cannot append."""
+    b = Batch(hb, heads(8, 2, 128), [(30, 3), (1, 100)], hb.hb_rope_frequencies(128, 5e5), seed=14)
+    for f, layout, magnitude in ((hb.hb_rope_frequencies(64, 1e4), 1, 1.0), (np.zeros(0), 0, 1.0),
+                                 (hb.hb_rope_frequencies(128, 5e5, 4.0), 0, 1.5)):
+        b.inv_freq, b.layout, b.magnitude = np.asarray(f, np.float64), layout, magnitude
+        hb.hb_set_attention_rope(b.att, f, layout, magnitude)
+        b.run()
+        b.check()
+    late = hb.hb_create_attention(b.att.cfg, b.blocks)
+    hb.hb_plan_attention(late, b.requests)
+    hb.hb_set_attention_rope(late, b.inv_freq)
+    with pytest.raises(hb.HBError, match="before the handle's first hb_set_attention_rope"):
+        hb.hb_run_append(late, *b.slices(), b.k_pool, b.v_pool, b.out)
+    hb.hb_plan_attention(late, b.requests)
+    hb.hb_run_append(late, *b.slices(), b.k_pool, b.v_pool, b.out)
+    b.magnitude = 1.0
+    b.torch.cuda.synchronize()
+    b.check()
+
+
 def test_calls_that_are_refused(hb):
     import torch
     b = Batch(hb, heads(8, 2, 128), [(3, 100), (1, 40)], hb.hb_rope_frequencies(128, 5e5), seed=10)
