@@ -3,8 +3,8 @@ The tolerance is attnref's: sharing changes the order in which fp32 parts are ad
 import numpy as np
 import pytest
 
-from attnref import Cache, assert_close, reference
-from hb_workloads import LayerShape, bf16_bits_to_f32
+from attnref import OUT_REL, Cache, assert_close, reference
+from hb_workloads import LayerShape, bf16_bits_to_f32, f32_to_bf16_bits
 
 pytestmark = pytest.mark.gpu
 
@@ -177,3 +177,42 @@ def test_two_handles_on_two_streams(hb):
         torch.cuda.synchronize()
         for r, w in zip(runs, want):
             assert np.array_equal(r.out.float().cpu().numpy().astype(np.float64), w)
+
+
+COUNTED = [
+    ((8, 2, 128), *CASES["odd lengths"]), ((4, 4, 64), *CASES["drafts"]), ((8, 1, 128), *CASES["two groups and others"]),
+    ((16, 1, 64), *CASES["chunks between"]), ((32, 8, 128), *CASES["long and short"]), ((2, 2, 128), *CASES["more rows than columns"]),
+    ((16, 4, 128), [(1, 5008 + 9 * i) for i in range(40)] + [(777, 3000)], [(0, 40, 5008)]),
+    ((32, 8, 128), [(1, 3100)] * 33 + [(1, 1290 + i) for i in range(90)] + [(1000, 500)], [(0, 33, 3056), (33, 90, 1280)]),
+    ((8, 1, 128), [(1 + i % 4, 6400 + 40 * i) for i in range(20)] + [(1, 9000)], [(0, 20, 6336)]),
+]
+
+
+@pytest.mark.parametrize("share_all", [True, False])
+@pytest.mark.parametrize("i", range(len(COUNTED)))
+def test_every_key_counts_once(hb, monkeypatch, i, share_all):
+    """q is zero, so every key has the weight 1, exactly, and V of key j is the unit vector j / 64 mod hd: the output is
+    the share of the row's keys in those runs of 64. Rounded: the reciprocal of the sum and the product with it (2^-20),
+    the output (2^-8). No row has more than 128 hd keys, so a value counts two runs at most, and one page of 16 keys
+    lost or counted twice is an eighth of it or more."""
+    import torch
+    if not share_all:
+        monkeypatch.delenv("HB_ATTN_SHARE_ALL")
+    nqkvhd, lens, groups = COUNTED[i]
+    nq, nkv, hd = nqkvhd
+    r = Run(heads(*nqkvhd), lens, groups, seed=60 + i)
+    want = []
+    for c, x, table in r.reqs:
+        n = x + c
+        unit = np.zeros((n, hd), np.float32)
+        unit[np.arange(n), np.arange(n) // 64 % hd] = 1.0
+        v = np.broadcast_to(f32_to_bf16_bits(unit)[:, None, :], (n, nkv, hd))
+        r.cache.dl.append_kv(table, 0, r.cache.bits(n, nkv, hd), v.copy())
+        seen = np.cumsum(unit, 0, dtype=np.float64)[x:]
+        want.append(np.repeat((seen / seen.sum(1, keepdims=True))[:, None, :], nq, 1))
+    want = np.concatenate(want)
+    r.q = torch.zeros_like(r.q)
+    for _ in range(2):  # the second over the first one's parts
+        got = r.run()
+        assert np.isfinite(got).all()
+        assert (np.abs(got - want) <= (OUT_REL + 2.0 ** -20) * want).all(), np.abs(got / np.maximum(want, 1e-9) - 1).max()
