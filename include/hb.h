@@ -295,8 +295,11 @@ typedef struct {
 } hb_prefix_group;
 
 /* hb_plan_attention for a batch in which groups of requests share a prefix: runs
- * read a shared prefix's keys and values once for all rows of its group and join
- * that with each row's own keys. The results are those of hb_plan_attention but
+ * read a shared prefix's keys and values for many rows of its group together and
+ * join that with each row's own keys. Read together, once per kv head, are up to 128
+ * columns (a column is one query head of one row); 64 or 16 in small launches, 16
+ * for groups of fewer than 64. Larger groups read the prefix once for each such set
+ * of columns, mostly from the caches. The results are those of hb_plan_attention but
  * for the order in which a row's keys are added up; the same bits every time. Where
  * nothing is gained each request reads its prefix by itself: behind prefixes too short
  * for it, and where its own rows fill half a matrix tile (chunk_len * n_q_heads /
