@@ -594,7 +594,10 @@ hb_status hb_run_model(hb_model* model, const hb_model_batch* batch);
  *   temperature  not above 0 (or not a number): the most likely token, probability 1
  *   u            below 0 or not a number: 0; from 1 on: 1 - 2^-24
  *   logits       not a number, or -infinity: never drawn; +infinity: as the largest
- *                fp32 value; a row of none but the former: token 0, probability 0
+ *                fp32 value; a row of none but the former: token 0, probability 0.
+ *                (A mask of a finite value, -1e4 or the type's lowest, counts as a
+ *                logit. It is drawn as its weight says, but such a row may take
+ *                several times as long: mask with -infinity.)
  * Weights are formed in fp64 and summed as integer multiples of 2^-45 of the largest
  * (2^-44 for a vocabulary above 2^17, 2^-42 at 2^20): the order of additions changes
  * nothing, and two calls give the same tokens. */

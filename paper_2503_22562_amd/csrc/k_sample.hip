@@ -20,10 +20,13 @@
 // and a second look at the rows where they do not. Rows are cut into slices so that few
 // rows fill the card, and the last workgroup of a row to finish draws its token: no launch
 // of its own for that. Few rows are bound by the launches and by chains of barriers (one
-// row of 128256: 15.4 us a call; kernels 3.6, 11.5 and 0.9, or 3.8 where the row is read
-// again), many by the vector instructions of the weights (256 rows, 131 MB: 27 us extents,
+// row of 128256: 15.2 us a call; kernels 3.6, 11.5 and 0.9, or 3.8 where the row is read
+// again; by the clock of the second one's last workgroup 1.7 until it has settings and extent,
+// 1.5 its weights, 2.4 its additions to the row's bins, 1.9 to read those back and scan
+// them, 0.8 to search, 1.7 to draw; of 64 rows with every limit, 27 us, 2.1, 6.0, 5.4, 2.9, 1.2
+// and 1.7), many by the vector instructions of the weights (256 rows, 131 MB: 27 us extents,
 // 49 weights, of which some 35 instructions an element make 29, 30 the second look at the
-// rows whose limits lie among unlikely tokens; 104 us a call, and 19 to read the logits
+// rows whose limits lie among unlikely tokens; 105 us a call, and 19 to read the logits
 // once).
 #include <algorithm>
 #include <cfloat>
@@ -264,7 +267,12 @@ __device__ __forceinline__ Scale scale_of(const Setting& g, const Extent& e, int
   if (c.far) c.cut = -FLT_MAX;
   // (the second rate: temperatures for which the logit next to the largest has no weight)
   c.weights = {(double)c.max, fmin(1.4426950408889634 * kSteps / (double)g.t, 65536.0 / ((double)c.max - (double)c.cut)), pow2};
-  const float used = fminf(c.max - e.lo, reach);  // (infinite, or next to nothing: one bin)
+  // The bins span the finite logits, as far as they have weight. (Infinite, or next to nothing:
+  // one bin. A mask of a finite value counts as a logit: the bins then span the whole reach, and
+  // as temperatures rise and limits lie far out, the bins looked into hold more than the list.
+  // One row of 128256 unit-normal logits, top_p 0.9, t = 1: 30 us, with one logit of -1e4 86;
+  // top_k 20000 too, t = 2, half of them masked: -infinity 32, -1e4 340.)
+  const float used = fminf(c.max - e.lo, reach);
   c.per = used > 1e-30f ? kBins / used : 0.f;
   c.near = min(kBins, (int)fminf(kNear * g.t * c.per, (float)kBins));
   c.shift = shift;
